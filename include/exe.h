@@ -49,6 +49,7 @@ enum { EXE_NORM_LAYERNORM = 0, EXE_NORM_RMSNORM = 1 };
 enum { EXE_POS_LEARNED = 0, EXE_POS_RELBIAS = 1, EXE_POS_NONE = 2 };
 enum { EXE_DTYPE_F32 = 0, EXE_DTYPE_BF16 = 1 };
 enum { EXE_SCALE_RSQRT_DH = 0, EXE_SCALE_NONE = 1 };
+enum { EXE_ROPE_UNSCALED = 0, EXE_ROPE_LINEAR = 1, EXE_ROPE_BASE = 2, EXE_ROPE_RAMP = 3 };      /* see exe_rotary_frequencies */
 
 typedef struct exe_config {
     int32_t arch;            /* EXE_ARCH_* */
@@ -177,7 +178,17 @@ int exe_seq_import(exe_model_t* m, int32_t seq_id, const void* host_buf, uint64_
 int exe_seq_reserve(exe_model_t* m, int32_t seq_id, int32_t reserve_length);
 int exe_kv_compact(exe_model_t* m, uint64_t* moved_bytes);
 
-/* Pool accounting (bytes). Any pointer may be NULL. */
+/*
+ * Forks a live sequence (several continuations of one prompt): admits n sequences under the free ids new_ids (host), each with the
+ * positions that seq_id has memoized, so that exe_decode_step continues every one of them on its own.  Paged pool: full blocks are
+ * shared (a block returns to the pool when the last sequence that holds it leaves; nothing ever writes to a full block), a last, partly
+ * filled one is copied.  Extents: the entries are copied, with the same capacity.  All or nothing: EXE_ERR_BAD_SEQ (seq_id not live,
+ * a new id out of range, live or twice), EXE_ERR_OOM_KV.  The copies are enqueued on the model's stream, in order with the model's
+ * kernels; the call does not wait for them.
+ */
+int exe_seq_fork(exe_model_t* m, int32_t seq_id, int32_t n, const int32_t* new_ids);
+
+/* Pool accounting (bytes; a block that several sequences share counts once). Any pointer may be NULL. */
 int exe_kv_stats(exe_model_t* m, uint64_t* pool_bytes, uint64_t* used_bytes, uint64_t* largest_free_bytes,
                  int32_t* live_seqs);
 
@@ -406,6 +417,59 @@ int exe_probe_peaks(void* hip_stream, uint64_t read_bytes, double* hbm_read_byte
  * buffer, synchronises the stream; host pointer. */
 int exe_probe_ingest(void* hip_stream, int32_t mode, uint64_t region_bytes, int32_t passes, int32_t waves,
                      int32_t loads_per_batch, int32_t row_bytes, double* bytes_per_s);
+/*
+ * A chunk of new tokens over a paged cache: rotary positions, append, attention, and copies of blocks.  Query heads may be a multiple
+ * of the key/value heads: query head h reads key/value head h / (H / Hkv).  One layer's cache is n_blocks blocks of
+ * [K|V][Hkv][block_size][dh] (block_size a power of two in [8, 4096], dh 64 or 128), as exe_op_decode_attention_paged has it with
+ * Hkv = H.  The new tokens of n_seqs sequences lie packed: those of sequence b are rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1
+ * (cu_seqlens [n_seqs + 1], DEVICE, from 0, not falling; a sequence may have none), and len[b] (device) counts b's positions
+ * with them, so row cu_seqlens[b] + i has position p = len[b] - n + i of n.  block_table [n_seqs, max_blocks] device; T: rows of the
+ * packed arrays, no less than cu_seqlens[n_seqs].  Rows behind the last sequence are neither read nor written.
+ * Lengths and tables stay on the device, so that a captured graph can be replayed with others.  What they name is checked there: a
+ * table entry outside of [0, n_blocks) and a position without an entry are never followed.  The calls allocate nothing and hold
+ * nothing back; q, out, the cache and workspaces are 16-byte aligned; no block may be written twice by one call.
+ */
+/* Angles of rotary positions, radians per position of each of the rot / 2 pairs: base^(-2 p / rot) (host function; inv_freq host
+ * [rot / 2], rot even, 2 .. 128), for contexts `factor` times as long as the original ones scaled by
+ *   EXE_ROPE_LINEAR: every frequency / factor;   EXE_ROPE_BASE: base * factor^(rot / (rot - 2)), which leaves the fastest pair and
+ *   divides the slowest by factor;   EXE_ROPE_RAMP: a pair that makes turns_fast turns or more over original_positions is left, one
+ *   of turns_slow or fewer divided by factor, linear in its turns between.
+ * *amplitude: 0.1 ln(factor) + 1 for EXE_ROPE_RAMP with factor > 1, else 1.  Arguments that a scaling does not name are not read. */
+int exe_rotary_frequencies(int32_t rot, double base, int32_t scaling, double factor, int32_t original_positions, double turns_slow,
+                           double turns_fast, double* inv_freq, float* amplitude);
+/* Turns heads of rows x [T, heads * dh] (dtype, rows x_stride elements apart): of the first rot elements of a head (even, 0 .. dh)
+ * pair p = (2p, 2p + 1) if interleaved else (p, p + rot / 2) becomes amplitude * (a cos - b sin, b cos + a sin) of the angle
+ * pos[t] * inv_freq[p]; the rest passes through.  pos [T] int32 device, any value (a negative position turns back, which is
+ * also the gradient: the same call on the incoming one with -pos), inv_freq [rot / 2] double device.  out: rows out_stride apart, x
+ * itself (in place, same stride) or memory that does not overlap it.  Angles in 64 bits, products in float, rounded once. */
+int exe_op_rotary(void* hip_stream, int32_t dtype, int32_t T, const void* x, int64_t x_stride, int32_t heads, int32_t dh, int32_t rot,
+                  int32_t interleaved, const int32_t* pos, const double* inv_freq, float amplitude, void* out, int64_t out_stride);
+/* Rows qkv [T, (H + 2 * Hkv) * dh] (queries, keys, values): keys are turned and stored with the values at their positions of the
+ * cache, queries are turned into q_out [T, H * dh] (nullable: they are not needed; may be qkv, same stride).  Turned as by
+ * exe_op_rotary, by pos [T] or (NULL) by the positions in the cache; rot = 0 appends only (inv_freq may be NULL). */
+int exe_op_rotary_append_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, const int32_t* cu_seqlens, int32_t T, const void* qkv,
+                               int64_t row_stride, int32_t H, int32_t Hkv, int32_t dh, int32_t rot, int32_t interleaved, const int32_t* pos,
+                               const double* inv_freq, float amplitude, void* kv_blocks, int32_t n_blocks, const int32_t* block_table,
+                               int32_t max_blocks, int32_t block_size, const int32_t* len, void* q_out, int64_t q_out_stride);
+/* Attention of the new tokens over the cache, which holds them already: row t of q [T, H * dh] (rows q_stride elements apart,
+ * multiples of 16 bytes) at position p sees keys 0 .. p, of these the last `window` if window > 0.  out [T, H * dh], rows out_stride
+ * apart, not q.  A row that sees no key (p < 0) is 0; one that would read a position without a block is NaN.  Scores and softmax in
+ * float; the probabilities are rounded to the storage type for the product with the values, the result once more.
+ * max_new (tokens of the longest chunk) and max_len (the largest len) size the launch and the workspace; where they are wrong, it is
+ * slower, not wrong.  workspace: exe_op_chunk_attention_paged_workspace bytes (0 for bad arguments), NULL if that is 0; nothing in it
+ * needs clearing; calls that may overlap need one each. */
+int exe_op_chunk_attention_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, const int32_t* cu_seqlens, int32_t T, int32_t max_new,
+                                 const void* q, int64_t q_stride, const void* kv_blocks, int32_t n_blocks, const int32_t* block_table,
+                                 int32_t max_blocks, int32_t block_size, const int32_t* len, int32_t max_len, int32_t H, int32_t Hkv,
+                                 int32_t dh, float scale, int32_t window, void* out, int64_t out_stride, void* workspace,
+                                 uint64_t workspace_bytes);
+uint64_t exe_op_chunk_attention_paged_workspace(int32_t dtype, int32_t n_seqs, int32_t T, int32_t max_new, int32_t max_len, int32_t H,
+                                                int32_t Hkv, int32_t dh, int32_t window);
+/* Copies positions between blocks of a pool [n_layers][n_blocks][K|V][Hkv][block_size][dh] (forks, compaction), in every layer: copies
+ * [n_copies][3] HOST, each (source, destination, leading positions copied, 0 .. block_size).  A source may serve several copies; a
+ * destination that is written twice or is another copy's source (or its own) is EXE_ERR_ARG.  The list travels with the launch. */
+int exe_op_kv_copy_blocks(void* hip_stream, int32_t dtype, void* kv_blocks, int32_t n_layers, int32_t n_blocks, int32_t block_size, int32_t Hkv,
+                          int32_t dh, int32_t n_copies, const int32_t* copies);
 /* argmax over each row of float logits [rows, n] -> int32 out [rows]; lowest index on ties */
 int exe_op_argmax(void* hip_stream, const float* logits, int32_t rows, int32_t n, int32_t* out);
 /* T5 bucket of rel = key - query as this library computes it (host function, exact integer arithmetic) */

@@ -14,9 +14,9 @@ _call = None                                     # csrc/call.c
 
 DECLARED_SYMBOLS = [
     "exe_expected_weights", "exe_model_load", "exe_model_free", "exe_encode", "exe_decode_step",
-    "exe_seq_release", "exe_seq_length", "exe_kv_stats", "exe_seq_export_bytes", "exe_seq_export", "exe_seq_import", "exe_seq_reserve", "exe_kv_compact", "exe_profile", "exe_run_rra", "exe_kernel_timing",
+    "exe_seq_release", "exe_seq_length", "exe_kv_stats", "exe_seq_export_bytes", "exe_seq_export", "exe_seq_import", "exe_seq_reserve", "exe_seq_fork", "exe_kv_compact", "exe_profile", "exe_run_rra", "exe_kernel_timing",
     "exe_kernel_times", "exe_op_gemm", "exe_op_gemm_workspace", "exe_op_gemm_plan", "exe_op_gemm_model_plan", "exe_op_gemm_kv_plan", "exe_op_kv_store_index", "exe_op_gemm_stream", "exe_op_gemm_model", "exe_op_gemm_ld", "exe_op_gemm_noalloc", "exe_op_gemm_noalloc_max_workspace", "exe_op_paged_index_check", "exe_op_norm", "exe_op_resid_norm", "exe_op_prefill_attention", "exe_op_prefill_tiles",
-    "exe_op_decode_attention", "exe_op_decode_attention_paged", "exe_probe_peaks", "exe_probe_ingest", "exe_op_argmax", "exe_rel_bucket", "exe_last_error", "exe_version",
+    "exe_op_decode_attention", "exe_op_decode_attention_paged", "exe_probe_peaks", "exe_probe_ingest", "exe_rotary_frequencies", "exe_op_rotary", "exe_op_rotary_append_paged", "exe_op_chunk_attention_paged", "exe_op_chunk_attention_paged_workspace", "exe_op_kv_copy_blocks", "exe_op_argmax", "exe_rel_bucket", "exe_last_error", "exe_version",
     # exe_sched.h (host only)
     "exe_sim_completion", "exe_sim_step_ms", "exe_sim_rra", "exe_sim_waa", "exe_sched_search", "exe_sched_rra",
 ]
@@ -133,6 +133,7 @@ def lib():
     L.exe_seq_export.argtypes = [vp, i32, vp, C.c_uint64, C.POINTER(SeqState)]
     L.exe_seq_import.argtypes = [vp, i32, vp, C.c_uint64, C.POINTER(SeqState), i32]
     L.exe_seq_reserve.argtypes = [vp, i32, i32]
+    L.exe_seq_fork.argtypes = [vp, i32, i32, ip]
     L.exe_kv_compact.argtypes = [vp, C.POINTER(C.c_uint64)]
     L.exe_profile.argtypes = [vp, i32, ip, i32, ip, i32, C.POINTER(LengthDist), i32, C.POINTER(ProfileRow), i32, ip]
     L.exe_run_rra.argtypes = [vp, C.POINTER(RraConfig), i32, ip, ip, ip, ip, C.POINTER(RraStats)]
@@ -158,11 +159,20 @@ def lib():
     L.exe_op_decode_attention.argtypes = [vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, i32, i32, C.c_float, vp, i32, vp]
     L.exe_op_decode_attention_paged.argtypes = [vp, i32, i32, vp, i32, vp, vp, i32, i32, vp, vp, i32, i32, C.c_float, vp, i32,
                                                 i32, vp]
+    i64, f64, dp = C.c_int64, C.c_double, C.POINTER(C.c_double)
+    L.exe_rotary_frequencies.argtypes = [i32, f64, i32, f64, i32, f64, f64, dp, C.POINTER(C.c_float)]
+    L.exe_op_rotary.argtypes = [vp, i32, i32, vp, i64, i32, i32, i32, i32, vp, vp, C.c_float, vp, i64]
+    L.exe_op_rotary_append_paged.argtypes = [vp, i32, i32, vp, i32, vp, i64, i32, i32, i32, i32, i32, vp, vp, C.c_float, vp, i32, vp, i32, i32,
+                                             vp, vp, i64]
+    L.exe_op_chunk_attention_paged.argtypes = [vp, i32, i32, vp, i32, i32, vp, i64, vp, i32, vp, i32, i32, vp, i32, i32, i32, i32, C.c_float, i32,
+                                               vp, i64, vp, C.c_uint64]
+    L.exe_op_chunk_attention_paged_workspace.argtypes = [i32] * 9
+    L.exe_op_chunk_attention_paged_workspace.restype = C.c_uint64
+    L.exe_op_kv_copy_blocks.argtypes = [vp, i32, vp, i32, i32, i32, i32, i32, i32, ip]
     L.exe_op_argmax.argtypes = [vp, vp, i32, i32, vp]
     L.exe_rel_bucket.argtypes = [i32, i32, i32, i32]
     L.exe_last_error.restype = C.c_char_p
     L.exe_version.restype = C.c_char_p
-    dp, f64 = C.POINTER(C.c_double), C.c_double
     L.exe_sim_completion.argtypes = [dp, i32, i32, dp, dp]
     L.exe_sim_step_ms.argtypes = [C.POINTER(SimTable), i32, f64, f64, dp]
     L.exe_sim_rra.argtypes = [C.POINTER(SimTable), dp, i32, dp, i32, f64, i32, i32, C.POINTER(SimRraResult)]
@@ -195,6 +205,28 @@ def _dev(t) -> Optional[int]:
     if isinstance(t, int):
         return t
     assert t.is_cuda and t.is_contiguous(), "expected a contiguous device tensor"
+    return t.data_ptr()
+
+
+def _typed(t, name: str, n: int) -> Optional[int]:
+    """_dev for an array that holds n elements of `name` (a torch type); of another type they would be misread."""
+    if t is None or isinstance(t, int):
+        return t
+    assert str(t.dtype) == "torch." + name, f"expected {name}, got {t.dtype}"
+    assert t.numel() >= n, f"expected {n} elements, got {t.numel()}"
+    return _dev(t)
+
+
+def _rows(t, dtype: int, rows: int, width: int, stride: int) -> Optional[int]:
+    """Device pointer of a tensor of the storage type that holds rows of `width` elements, `stride` apart from its first element on; it
+    need not be contiguous.  It lies on the current device, on whose stream the operation is enqueued."""
+    if t is None or isinstance(t, int):
+        return t
+    import torch
+    assert t.is_cuda and t.get_device() == torch.cuda.current_device(), "expected a tensor on the current device"
+    assert t.dtype == (torch.bfloat16 if dtype == 1 else torch.float32), f"expected the type {dtype}, got {t.dtype}"
+    need = (rows - 1) * stride + width if rows > 0 else 0
+    assert need <= t.numel() or need <= t.untyped_storage().nbytes() // t.element_size() - t.storage_offset(), f"expected {need} elements"
     return t.data_ptr()
 
 
@@ -308,6 +340,10 @@ class Model:
 
     def seq_reserve(self, seq_id: int, reserve_length: int) -> None:
         _check(lib().exe_seq_reserve(self._h, seq_id, reserve_length))
+
+    def seq_fork(self, seq_id: int, new_ids) -> None:
+        ids = _i32(new_ids)
+        _check(lib().exe_seq_fork(self._h, int(seq_id), len(ids), _ip(ids)))
 
     def kv_compact(self) -> int:
         """Returns the bytes moved."""
@@ -457,6 +493,60 @@ def exe_op_decode_attention_paged(dtype, B, q, q_stride, kv_blocks, block_table,
     _check(lib().exe_op_decode_attention_paged(_stream_ptr(stream), dtype, B, _dev(q), q_stride, _dev(kv_blocks),
                                                _dev(block_table), max_blocks, block_size, _dev(length), _dev(qpos), H, dh,
                                                scale, _dev(bias_by_dist), bias_radius, new_kv_offset, _dev(out)))
+
+
+# ---- a chunk of new tokens over a paged cache ----
+
+ROPE_UNSCALED, ROPE_LINEAR, ROPE_BASE, ROPE_RAMP = 0, 1, 2, 3
+
+
+def exe_rotary_frequencies(rot: int, base: float = 10000.0, scaling: int = ROPE_UNSCALED, factor: float = 1.0, original_positions: int = 0,
+                           turns_slow: float = 1.0, turns_fast: float = 32.0):
+    """(frequencies as a numpy array of doubles [rot / 2], amplitude); host only."""
+    f, a = np.zeros(max(rot // 2, 1), dtype=np.float64), C.c_float()
+    _check(lib().exe_rotary_frequencies(rot, base, scaling, factor, original_positions, turns_slow, turns_fast, _dp(f), C.byref(a)))
+    return f, a.value
+
+
+def exe_op_rotary(dtype, T, x, x_stride, heads, dh, rot, interleaved, pos, inv_freq, amplitude, out, out_stride, stream=None):
+    """x and out: device tensors (or addresses) whose rows are x_stride / out_stride elements apart."""
+    _check(lib().exe_op_rotary(_stream_ptr(stream), dtype, T, _rows(x, dtype, T, heads * dh, x_stride), x_stride, heads, dh, rot, interleaved,
+                               _typed(pos, "int32", T), _typed(inv_freq, "float64", rot // 2), amplitude,
+                               _rows(out, dtype, T, heads * dh, out_stride), out_stride))
+
+
+def exe_op_rotary_append_paged(dtype, n_seqs, cu_seqlens, T, qkv, row_stride, H, Hkv, dh, rot, interleaved, pos, inv_freq, amplitude, kv_blocks,
+                               n_blocks, block_table, max_blocks, block_size, length, q_out, q_out_stride, stream=None):
+    block = 2 * Hkv * block_size * dh
+    _check(lib().exe_op_rotary_append_paged(_stream_ptr(stream), dtype, n_seqs, _typed(cu_seqlens, "int32", n_seqs + 1), T,
+                                            _rows(qkv, dtype, T, (H + 2 * Hkv) * dh, row_stride), row_stride, H, Hkv, dh, rot, interleaved,
+                                            _typed(pos, "int32", T), _typed(inv_freq, "float64", rot // 2), amplitude,
+                                            _rows(kv_blocks, dtype, n_blocks, block, block), n_blocks,
+                                            _typed(block_table, "int32", n_seqs * max_blocks), max_blocks, block_size,
+                                            _typed(length, "int32", n_seqs), _rows(q_out, dtype, T, H * dh, q_out_stride), q_out_stride))
+
+
+def exe_op_chunk_attention_paged_workspace(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window=0) -> int:
+    return int(lib().exe_op_chunk_attention_paged_workspace(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window))
+
+
+def exe_op_chunk_attention_paged(dtype, n_seqs, cu_seqlens, T, max_new, q, q_stride, kv_blocks, n_blocks, block_table, max_blocks, block_size,
+                                 length, max_len, H, Hkv, dh, scale, window, out, out_stride, workspace=None, stream=None):
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    block = 2 * Hkv * block_size * dh
+    _check(lib().exe_op_chunk_attention_paged(_stream_ptr(stream), dtype, n_seqs, _typed(cu_seqlens, "int32", n_seqs + 1), T, max_new,
+                                              _rows(q, dtype, T, H * dh, q_stride), q_stride, _rows(kv_blocks, dtype, n_blocks, block, block), n_blocks,
+                                              _typed(block_table, "int32", n_seqs * max_blocks), max_blocks, block_size,
+                                              _typed(length, "int32", n_seqs), max_len, H, Hkv, dh, scale, window,
+                                              _rows(out, dtype, T, H * dh, out_stride), out_stride, _dev(workspace), ws_bytes))
+
+
+def exe_op_kv_copy_blocks(dtype, kv_blocks, n_layers, n_blocks, block_size, Hkv, dh, copies, stream=None):
+    """copies: (source, destination, leading positions) of every copy, on the host."""
+    c = np.ascontiguousarray(copies, dtype=np.int32).reshape(-1, 3)
+    block = 2 * Hkv * block_size * dh
+    _check(lib().exe_op_kv_copy_blocks(_stream_ptr(stream), dtype, _rows(kv_blocks, dtype, n_layers * n_blocks, block, block), n_layers, n_blocks,
+                                       block_size, Hkv, dh, len(c), _ip(c)))
 
 
 def exe_probe_peaks(read_bytes: int = 0, stream=None) -> dict:

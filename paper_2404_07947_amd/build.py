@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libexe.so")
 # csrc/call.c: host code against Python's headers, named for the Python that it is built for
 CALL = os.path.join(HERE, "_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 CC = os.environ.get("CC", "gcc")
-SOURCES = ["kernels_elementwise.hip", "kernels_gemm.hip", "kernels_gemm_large.hip", "kernels_gemm_stream.hip", "kernels_gemm_f32.hip", "kernels_attn.hip", "kernels_small.hip", "runtime.hip", "probe.hip", "sched.cpp"]
+SOURCES = ["kernels_elementwise.hip", "kernels_gemm.hip", "kernels_gemm_large.hip", "kernels_gemm_stream.hip", "kernels_gemm_f32.hip", "kernels_attn.hip", "kernels_small.hip", "kernels_cache.hip", "kernels_chunk.hip", "runtime.hip", "probe.hip", "sched.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Kernel arguments preloaded into scalar registers instead of fetched by each wave's first instructions: decode iterations of
 # small models run 1-3 % faster (0.3 us of a 4-6 us launch).

@@ -6,6 +6,8 @@
 #include <mutex>
 #include <vector>
 
+#include "paged.h"
+
 namespace exe {
 
 // Where a projection's key / value features go instead of `out`: straight into the cache.  Feature n >= first_col of row m is
@@ -202,6 +204,53 @@ struct AttnPagedArgs {       // as AttnCacheArgs, with the cache of one layer he
 hipError_t launch_attn_paged(const AttnPagedArgs& a, hipStream_t s);
 // host-side replay of the paged kernel's row indexing (0 = every row read lies in its block and is read once)
 int paged_index_check(int dtype, int dh, int block_shift, int nwv, int len);
+
+// ---- a chunk of new tokens over a paged cache (kernels_chunk.hip, kernels_cache.hip).  Sequence b's new tokens are rows cu[b] ..
+// cu[b + 1] - 1 of the packed ones, the last of them at position len[b] - 1.
+struct RotaryArgs {          // rows [tokens, heads * dh]; out may be x
+    int dtype, tokens, heads, dh, rot, interleaved;
+    const void* x; int64_t x_stride;
+    const int32_t* pos;
+    const double* inv_freq;                // radians per position of pair p, [rot / 2]
+    float amplitude;
+    void* out; int64_t out_stride;
+};
+hipError_t launch_rotary(const RotaryArgs& a, hipStream_t s);
+struct RotaryAppendArgs {    // rows [tokens, (H + 2 * Hkv) * dh]: queries, keys, values
+    int dtype, n_seqs, tokens, H, Hkv, dh, rot, interleaved;
+    const int32_t* cu;
+    const void* qkv; int64_t row_stride;
+    const int32_t* pos;                    // nullable: the positions in the cache
+    const double* inv_freq;
+    float amplitude;
+    void* kv_blocks;
+    PagedTable table;
+    const int32_t* len;                    // with the new tokens
+    void* q_out; int64_t q_out_stride;     // nullable
+};
+hipError_t launch_rotary_append(const RotaryAppendArgs& a, hipStream_t s);
+struct BlockCopy { int32_t src, dst, rows; };
+struct BlockCopyArgs {       // pool [layers][n_blocks][runs][block_rows] rows of row_bytes (a multiple of 16); a block less than 32 GB
+    void* pool;
+    int layers, n_blocks, block_rows, row_bytes, runs;
+    const BlockCopy* list; int n;          // host; no destination twice, or the source of another
+};
+hipError_t launch_copy_blocks(const BlockCopyArgs& a, hipStream_t s);
+struct ChunkAttnArgs {
+    int dtype, n_seqs, tokens, H, Hkv, dh;
+    int max_new, max_len;                  // size the launch; results do not depend on them
+    const int32_t* cu;
+    const void* q; int64_t q_stride;
+    const void* kv_blocks;
+    PagedTable table;
+    const int32_t* len;
+    float scale;
+    int window;                            // keys that a token sees, itself the last; 0: all
+    void* out; int64_t out_stride;
+    float* workspace;                      // chunk_attn_workspace bytes
+};
+size_t chunk_attn_workspace(const ChunkAttnArgs& a);
+hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s);
 
 constexpr int PREFILL_TILE_Q = 128, PREFILL_TILE_K = 64;
 struct PrefillWork {         // of one head over a batch

@@ -175,6 +175,7 @@ struct exe_model {
     int blk_rows = 0, blk_shift = 0, n_blocks = 0;
     int64_t blk_elems = 0;
     std::vector<int32_t> free_blocks;      // stack; the back is handed out next
+    std::vector<int32_t> block_refs;       // sequences that hold a block; full ones may have several (exe_seq_fork)
 
     // activation workspace
     int rows_cap = 0;
@@ -433,6 +434,7 @@ extern "C" int exe_model_load(const exe_config_t* cfg, const exe_tensor_t* weigh
         int64_t nb = m->pool.elems / ((int64_t)n_dec_layers(c) * m->blk_elems);
         m->n_blocks = (int)std::min<int64_t>(nb, 1 << 24);
         m->free_blocks.resize(m->n_blocks);
+        m->block_refs.assign(m->n_blocks, 0);
         for (int b = 0; b < m->n_blocks; ++b) m->free_blocks[b] = m->n_blocks - 1 - b;     // block 0 goes out first
         bool learned = c.has_embed && c.pos == EXE_POS_LEARNED;
         size_t width = learned ? (size_t)((c.max_pos + m->blk_rows - 1) >> sh) : (size_t)m->n_blocks;
@@ -660,9 +662,19 @@ static int run_head(exe_model* m, const int32_t* row_index_dev, int n, int32_t* 
     return EXE_OK;
 }
 
+// a sequence lets go of a block, which is free once none holds it
+static void give_block(exe_model* m, int32_t b)
+{
+    if (--m->block_refs[b] == 0) m->free_blocks.push_back(b);
+}
+static void give_blocks(exe_model* m, Seq& s)
+{
+    for (auto it = s.blocks.rbegin(); it != s.blocks.rend(); ++it) give_block(m, *it);
+    s.blocks.clear();
+}
 static void release_seq(exe_model* m, Seq& s)
 {
-    for (auto it = s.blocks.rbegin(); it != s.blocks.rend(); ++it) m->free_blocks.push_back(*it);
+    give_blocks(m, s);
     if (s.base >= 0) m->pool.release(s.base, s.elems);
     if (s.xbase >= 0) m->pool.release(s.xbase, s.xelems);
     if (s.live) m->live--;
@@ -681,6 +693,7 @@ static void take_blocks(exe_model* m, Seq& s, int count)
 {
     for (int i = 0; i < count; ++i) {
         s.blocks.push_back(m->free_blocks.back());
+        m->block_refs[m->free_blocks.back()] = 1;
         m->free_blocks.pop_back();
     }
     s.cap = (int)s.blocks.size() * m->blk_rows;
@@ -915,8 +928,7 @@ extern "C" int exe_encode(exe_model_t* m, int32_t n, const int32_t* seq_ids, con
     }
     auto rollback = [&]() {
         for (auto& s : fresh) {
-            for (auto it = s.blocks.rbegin(); it != s.blocks.rend(); ++it) m->free_blocks.push_back(*it);
-            s.blocks.clear();
+            give_blocks(m, s);
             if (s.base >= 0) m->pool.release(s.base, s.elems);
             if (s.xbase >= 0) m->pool.release(s.xbase, s.xelems);
         }
@@ -1377,7 +1389,7 @@ extern "C" int exe_seq_import(exe_model_t* m, int32_t seq_id, const void* host_b
         hipError_t e = copy_blocks(m, s, (char*)const_cast<void*>(host_buf), false);
         if (e == hipSuccess) e = hipStreamSynchronize(m->stream);
         if (e != hipSuccess) {
-            for (auto it = s.blocks.rbegin(); it != s.blocks.rend(); ++it) m->free_blocks.push_back(*it);
+            give_blocks(m, s);
             return fail(EXE_ERR_HIP, "K/V import copy: %s", hipGetErrorString(e));
         }
         s.live = true;
@@ -1436,7 +1448,7 @@ extern "C" int exe_seq_reserve(exe_model_t* m, int32_t seq_id, int32_t reserve_l
             return fail(EXE_ERR_OOM_KV, "K/V pool exhausted (%d blocks needed, %d of %d free)", want - have, (int)m->free_blocks.size(), m->n_blocks);
         if (want > have) take_blocks(m, s, want - have);
         while ((int)s.blocks.size() > want) {
-            m->free_blocks.push_back(s.blocks.back());
+            give_block(m, s.blocks.back());
             s.blocks.pop_back();
         }
         s.cap = (int)s.blocks.size() * m->blk_rows;
@@ -1514,6 +1526,85 @@ extern "C" int exe_kv_compact(exe_model_t* m, uint64_t* moved_bytes)
     }
     rebuild_free();
     if (moved_bytes) *moved_bytes = moved;
+    return EXE_OK;
+}
+
+// ---------------------------------------------------------------- forks of a sequence
+extern "C" int exe_seq_fork(exe_model_t* m, int32_t seq_id, int32_t n, const int32_t* new_ids)
+{
+    if (!m) return fail(EXE_ERR_ARG, "null model");
+    if (n < 0 || (n > 0 && !new_ids)) return fail(EXE_ERR_ARG, "bad arguments");
+    const exe_config_t& c = m->c;
+    if (seq_id < 0 || seq_id >= c.max_seqs || !m->seqs[seq_id].live) return fail(EXE_ERR_BAD_SEQ, "seq id %d is not live", seq_id);
+    ++m->mark_gen;
+    for (int i = 0; i < n; ++i) {
+        int id = new_ids[i];
+        if (id < 0 || id >= c.max_seqs) return fail(EXE_ERR_BAD_SEQ, "seq id %d out of range", id);
+        if (m->seqs[id].live) return fail(EXE_ERR_BAD_SEQ, "seq id %d is live", id);
+        if (m->mark[id] == m->mark_gen) return fail(EXE_ERR_BAD_SEQ, "seq id %d appears twice", id);
+        m->mark[id] = m->mark_gen;
+    }
+    const Seq& s = m->seqs[seq_id];
+    const int ndl = n_dec_layers(c);
+    std::vector<Seq> fresh(n);
+    hipError_t e = hipSuccess;
+    if (paged(m)) {
+        // Full blocks are shared: nothing writes to them again.  The last, partly filled one is the new sequence's own.
+        const int full = s.len >> m->blk_shift, rest = s.len & (m->blk_rows - 1);
+        if (rest && n > (int)m->free_blocks.size())
+            return fail(EXE_ERR_OOM_KV, "K/V pool exhausted (%d blocks needed, %d of %d free)", n, (int)m->free_blocks.size(), m->n_blocks);
+        std::vector<BlockCopy> copies;
+        for (Seq& f : fresh) {
+            for (int i = 0; i < full; ++i) {
+                f.blocks.push_back(s.blocks[i]);
+                ++m->block_refs[s.blocks[i]];
+            }
+            take_blocks(m, f, rest ? 1 : 0);
+            if (rest) copies.push_back({s.blocks[full], f.blocks.back(), rest});
+        }
+        BlockCopyArgs a{m->pool.ptr, ndl, m->n_blocks, m->blk_rows, c.head_dim * m->esz, 2 * c.n_heads, copies.data(), (int)copies.size()};
+        e = launch_copy_blocks(a, m->stream);
+    } else {
+        bool ok = true;
+        for (Seq& f : fresh) {
+            f.cap = s.cap;
+            f.elems = s.elems;
+            f.base = m->pool.alloc(f.elems);
+            if ((ok = f.base >= 0) && s.xbase >= 0) {
+                f.xelems = s.xelems;
+                f.xbase = m->pool.alloc(f.xelems);
+                ok = f.xbase >= 0;
+            }
+            if (!ok) break;
+        }
+        const size_t rows = (size_t)ndl * 2 * c.n_heads, rowb = (size_t)c.head_dim * m->esz;
+        char* pool = (char*)m->pool.ptr;
+        for (Seq& f : fresh) {
+            if (!ok || e != hipSuccess) break;
+            if (s.len > 0)
+                e = hipMemcpy2DAsync(pool + f.base * m->esz, s.cap * rowb, pool + s.base * m->esz, s.cap * rowb, s.len * rowb, rows,
+                                     hipMemcpyDeviceToDevice, m->stream);
+            if (e == hipSuccess && f.xbase >= 0)
+                e = hipMemcpyAsync(pool + f.xbase * m->esz, pool + s.xbase * m->esz, (size_t)s.xelems * m->esz, hipMemcpyDeviceToDevice, m->stream);
+        }
+        if (!ok) {
+            for (Seq& f : fresh) release_seq(m, f);
+            return fail(EXE_ERR_OOM_KV, "K/V pool exhausted (%lld of %lld elements in use)", (long long)m->pool.used, (long long)m->pool.elems);
+        }
+    }
+    if (e != hipSuccess) {
+        (void)hipStreamSynchronize(m->stream);
+        for (Seq& f : fresh) release_seq(m, f);
+        return fail(EXE_ERR_HIP, "K/V fork copy: %s", hipGetErrorString(e));
+    }
+    for (int i = 0; i < n; ++i) {
+        Seq& f = fresh[i];
+        f.live = true;
+        f.len = s.len;
+        f.n_in = s.n_in;
+        m->seqs[new_ids[i]] = f;
+        m->live++;
+    }
     return EXE_OK;
 }
 
@@ -2212,6 +2303,166 @@ extern "C" int exe_op_decode_attention_paged(void* hip_stream, int32_t dtype, in
         a.new_v_off = 2 * new_kv_offset;
     }
     HIP_TRY(launch_attn_paged(a, (hipStream_t)hip_stream));
+    return EXE_OK;
+}
+
+// ---------------------------------------------------------------- a chunk of new tokens over a paged cache
+static int block_shift_of(int block_size)
+{
+    int shift = 3;
+    while (shift < 12 && (1 << shift) < block_size) ++shift;
+    return (1 << shift) == block_size ? shift : -1;
+}
+static int check_paged(int dtype, int dh, int Hkv, int n_blocks, int max_blocks, int block_size)
+{
+    if (dtype != DT_F32 && dtype != DT_BF16) return fail(EXE_ERR_ARG, "bad dtype");
+    if (dh != 64 && dh != 128) return fail(EXE_ERR_SHAPE, "head_dim must be 64 or 128");
+    if (Hkv < 1 || n_blocks < 1 || max_blocks < 1) return fail(EXE_ERR_ARG, "a cache without heads or blocks");
+    if (block_shift_of(block_size) < 0) return fail(EXE_ERR_ARG, "block_size %d is not a power of two in [8, 4096]", block_size);
+    return EXE_OK;
+}
+static int esz_of_dtype(int dtype) { return dtype == DT_F32 ? 4 : 2; }
+
+extern "C" int exe_rotary_frequencies(int32_t rot, double base, int32_t scaling, double factor, int32_t original_positions,
+                                      double turns_slow, double turns_fast, double* inv_freq, float* amplitude)
+{
+    if (rot < 2 || rot > 128 || rot % 2 || !inv_freq || !amplitude) return fail(EXE_ERR_ARG, "bad rotary arguments");
+    if (!(base > 0.0) || !std::isfinite(base)) return fail(EXE_ERR_ARG, "a base of %g", base);
+    if (scaling < EXE_ROPE_UNSCALED || scaling > EXE_ROPE_RAMP) return fail(EXE_ERR_ARG, "unknown scaling %d", scaling);
+    if (scaling != EXE_ROPE_UNSCALED && (!(factor > 0.0) || !std::isfinite(factor))) return fail(EXE_ERR_ARG, "a factor of %g", factor);
+    if (scaling == EXE_ROPE_BASE && rot == 2) return fail(EXE_ERR_ARG, "one pair has no base to stretch");
+    if (scaling == EXE_ROPE_RAMP && (original_positions < 1 || !(turns_slow < turns_fast))) return fail(EXE_ERR_ARG, "bad ramp");
+    *amplitude = 1.f;
+    if (scaling == EXE_ROPE_BASE) base *= std::pow(factor, (double)rot / (rot - 2));
+    for (int p = 0; p < rot / 2; ++p) {
+        double f = std::pow(base, -2.0 * p / rot);
+        if (scaling == EXE_ROPE_LINEAR) f /= factor;
+        if (scaling == EXE_ROPE_RAMP) {
+            double turns = original_positions * f / (2.0 * M_PI);
+            double keep = std::min(1.0, std::max(0.0, (turns - turns_slow) / (turns_fast - turns_slow)));
+            f = f * keep + f / factor * (1.0 - keep);
+        }
+        inv_freq[p] = f;
+    }
+    if (scaling == EXE_ROPE_RAMP && factor > 1.0) *amplitude = (float)(0.1 * std::log(factor) + 1.0);
+    return EXE_OK;
+}
+
+extern "C" int exe_op_rotary(void* hip_stream, int32_t dtype, int32_t T, const void* x, int64_t x_stride, int32_t heads, int32_t dh,
+                             int32_t rot, int32_t interleaved, const int32_t* pos, const double* inv_freq, float amplitude, void* out,
+                             int64_t out_stride)
+{
+    if (dtype != DT_F32 && dtype != DT_BF16) return fail(EXE_ERR_ARG, "bad dtype");
+    if (T < 0 || heads < 1 || !x || !out || !pos || (rot > 0 && !inv_freq)) return fail(EXE_ERR_ARG, "bad rotary arguments");
+    if (dh != 64 && dh != 128) return fail(EXE_ERR_SHAPE, "head_dim must be 64 or 128");
+    if (rot < 0 || rot > dh || rot % 2) return fail(EXE_ERR_SHAPE, "cannot turn %d of %d elements", rot, dh);
+    if (interleaved != 0 && interleaved != 1) return fail(EXE_ERR_ARG, "interleaved must be 0 or 1");
+    if (x_stride < (int64_t)heads * dh || out_stride < (int64_t)heads * dh) return fail(EXE_ERR_SHAPE, "rows of %d heads overlap", heads);
+    if (x == out && x_stride != out_stride) return fail(EXE_ERR_ARG, "in place, both strides must be the same");
+    if ((uintptr_t)x % esz_of_dtype(dtype) || (uintptr_t)out % esz_of_dtype(dtype)) return fail(EXE_ERR_ARG, "operands must be aligned to their type");
+    RotaryArgs a{dtype, T, heads, dh, rot, interleaved, x, x_stride, pos, inv_freq, amplitude, out, out_stride};
+    HIP_TRY(launch_rotary(a, (hipStream_t)hip_stream));
+    return EXE_OK;
+}
+
+extern "C" int exe_op_rotary_append_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, const int32_t* cu_seqlens, int32_t T, const void* qkv,
+                                          int64_t row_stride, int32_t H, int32_t Hkv, int32_t dh, int32_t rot, int32_t interleaved,
+                                          const int32_t* pos, const double* inv_freq, float amplitude, void* kv_blocks, int32_t n_blocks,
+                                          const int32_t* block_table, int32_t max_blocks, int32_t block_size, const int32_t* len, void* q_out,
+                                          int64_t q_out_stride)
+{
+    int r = check_paged(dtype, dh, Hkv, n_blocks, max_blocks, block_size);
+    if (r) return r;
+    if (n_seqs < 0 || T < 0 || H < 0 || !cu_seqlens || !qkv || !kv_blocks || !block_table || !len || (rot > 0 && !inv_freq))
+        return fail(EXE_ERR_ARG, "bad rotary append arguments");
+    if (rot < 0 || rot > dh || rot % 2) return fail(EXE_ERR_SHAPE, "cannot turn %d of %d elements", rot, dh);
+    if (interleaved != 0 && interleaved != 1) return fail(EXE_ERR_ARG, "interleaved must be 0 or 1");
+    if (row_stride < ((int64_t)H + 2 * (int64_t)Hkv) * dh || (q_out && q_out_stride < (int64_t)H * dh)) return fail(EXE_ERR_SHAPE, "rows overlap");
+    if (q_out == qkv && q_out_stride != row_stride) return fail(EXE_ERR_ARG, "in place, both strides must be the same");
+    if ((uintptr_t)kv_blocks & 15) return fail(EXE_ERR_ARG, "the cache must be 16-byte aligned");
+    if ((uintptr_t)qkv % esz_of_dtype(dtype) || (uintptr_t)q_out % esz_of_dtype(dtype)) return fail(EXE_ERR_ARG, "operands must be aligned to their type");
+    RotaryAppendArgs a{dtype, n_seqs, T, H, Hkv, dh, rot, interleaved, cu_seqlens, qkv, row_stride, pos, inv_freq, amplitude, kv_blocks,
+                       PagedTable{block_table, max_blocks, block_shift_of(block_size), n_blocks}, len, q_out, q_out_stride};
+    HIP_TRY(launch_rotary_append(a, (hipStream_t)hip_stream));
+    return EXE_OK;
+}
+
+static ChunkAttnArgs chunk_args(int dtype, int n_seqs, int T, int max_new, int max_len, int H, int Hkv, int dh, int window)
+{
+    ChunkAttnArgs a{};
+    a.dtype = dtype; a.n_seqs = n_seqs; a.tokens = T; a.H = H; a.Hkv = Hkv; a.dh = dh;
+    a.max_new = std::min(max_new, T); a.max_len = max_len; a.window = window;
+    return a;
+}
+
+extern "C" uint64_t exe_op_chunk_attention_paged_workspace(int32_t dtype, int32_t n_seqs, int32_t T, int32_t max_new, int32_t max_len, int32_t H,
+                                                           int32_t Hkv, int32_t dh, int32_t window)
+{
+    if (n_seqs < 1 || T < 1 || max_new < 1 || max_len < 1 || Hkv < 1 || H < Hkv || H % Hkv || window < 0) return 0;
+    return chunk_attn_workspace(chunk_args(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window));
+}
+
+extern "C" int exe_op_chunk_attention_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, const int32_t* cu_seqlens, int32_t T, int32_t max_new,
+                                            const void* q, int64_t q_stride, const void* kv_blocks, int32_t n_blocks, const int32_t* block_table,
+                                            int32_t max_blocks, int32_t block_size, const int32_t* len, int32_t max_len, int32_t H, int32_t Hkv,
+                                            int32_t dh, float scale, int32_t window, void* out, int64_t out_stride, void* workspace,
+                                            uint64_t workspace_bytes)
+{
+    int r = check_paged(dtype, dh, Hkv, n_blocks, max_blocks, block_size);
+    if (r) return r;
+    if (n_seqs < 0 || T < 0 || !cu_seqlens || !q || !kv_blocks || !block_table || !len || !out) return fail(EXE_ERR_ARG, "bad chunk attention arguments");
+    if (max_new < 1 || max_len < 1 || window < 0) return fail(EXE_ERR_ARG, "max_new %d, max_len %d, window %d", max_new, max_len, window);
+    if (H < Hkv || H % Hkv) return fail(EXE_ERR_SHAPE, "%d query heads over %d key/value heads", H, Hkv);
+    const int esz = esz_of_dtype(dtype);
+    if (q_stride < (int64_t)H * dh || out_stride < (int64_t)H * dh) return fail(EXE_ERR_SHAPE, "rows of %d heads overlap", H);
+    if (q_stride * esz % 16 || out_stride * esz % 16) return fail(EXE_ERR_SHAPE, "rows must begin on 16 bytes");
+    const void* ptrs[] = {q, kv_blocks, out, workspace};
+    for (const void* p : ptrs)
+        if ((uintptr_t)p & 15) return fail(EXE_ERR_ARG, "operands must be 16-byte aligned");
+    if (n_seqs == 0 || T == 0) return EXE_OK;
+    ChunkAttnArgs a = chunk_args(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window);
+    uint64_t need = chunk_attn_workspace(a);
+    if (need > (workspace ? workspace_bytes : 0)) return fail(EXE_ERR_ARG, "workspace too small (%llu bytes needed)", (unsigned long long)need);
+    a.cu = cu_seqlens;
+    a.q = q;
+    a.q_stride = q_stride;
+    a.kv_blocks = kv_blocks;
+    a.table = PagedTable{block_table, max_blocks, block_shift_of(block_size), n_blocks};
+    a.len = len;
+    a.scale = scale;
+    a.out = out;
+    a.out_stride = out_stride;
+    a.workspace = (float*)workspace;
+    HIP_TRY(launch_chunk_attn(a, (hipStream_t)hip_stream));
+    return EXE_OK;
+}
+
+extern "C" int exe_op_kv_copy_blocks(void* hip_stream, int32_t dtype, void* kv_blocks, int32_t n_layers, int32_t n_blocks, int32_t block_size, int32_t Hkv,
+                                     int32_t dh, int32_t n_copies, const int32_t* copies)
+{
+    int r = check_paged(dtype, dh, Hkv, n_blocks, 1, block_size);
+    if (r) return r;
+    if (!kv_blocks || n_layers < 1 || n_copies < 0 || (n_copies > 0 && !copies)) return fail(EXE_ERR_ARG, "bad block copy arguments");
+    if ((uintptr_t)kv_blocks & 15) return fail(EXE_ERR_ARG, "the cache must be 16-byte aligned");
+    const int row_bytes = dh * esz_of_dtype(dtype);
+    if (n_copies > n_blocks) return fail(EXE_ERR_ARG, "%d copies into %d blocks write one twice", n_copies, n_blocks);
+    if ((int64_t)2 * Hkv * block_size * row_bytes >= ((int64_t)1 << 32)) return fail(EXE_ERR_SHAPE, "a block of 4 GB or more");
+    std::vector<BlockCopy> list(n_copies);
+    std::vector<int32_t> to(n_copies);
+    for (int i = 0; i < n_copies; ++i) {
+        BlockCopy& k = list[i] = BlockCopy{copies[3 * i], copies[3 * i + 1], copies[3 * i + 2]};
+        if (k.src < 0 || k.src >= n_blocks || k.dst < 0 || k.dst >= n_blocks)
+            return fail(EXE_ERR_ARG, "copy %d: block %d to %d of %d blocks", i, k.src, k.dst, n_blocks);
+        if (k.rows < 0 || k.rows > block_size) return fail(EXE_ERR_BAD_LENGTH, "copy %d: %d positions of a block of %d", i, k.rows, block_size);
+        to[i] = k.dst;
+    }
+    // copies run side by side: none may write what another one reads or writes
+    std::sort(to.begin(), to.end());
+    if (std::adjacent_find(to.begin(), to.end()) != to.end()) return fail(EXE_ERR_ARG, "block %d is written twice", *std::adjacent_find(to.begin(), to.end()));
+    for (const BlockCopy& k : list)
+        if (std::binary_search(to.begin(), to.end(), k.src)) return fail(EXE_ERR_ARG, "block %d is read and written", k.src);
+    BlockCopyArgs a{kv_blocks, n_layers, n_blocks, block_size, row_bytes, 2 * Hkv, list.data(), n_copies};
+    HIP_TRY(launch_copy_blocks(a, (hipStream_t)hip_stream));
     return EXE_OK;
 }
 
