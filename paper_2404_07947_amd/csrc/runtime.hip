@@ -2398,7 +2398,7 @@ static ChunkAttnArgs chunk_args(int dtype, int n_seqs, int T, int max_new, int m
 extern "C" uint64_t exe_op_chunk_attention_paged_workspace(int32_t dtype, int32_t n_seqs, int32_t T, int32_t max_new, int32_t max_len, int32_t H,
                                                            int32_t Hkv, int32_t dh, int32_t window)
 {
-    if (n_seqs < 1 || T < 1 || max_new < 1 || max_len < 1 || Hkv < 1 || H < Hkv || H % Hkv || window < 0) return 0;
+    if (n_seqs < 1 || T < 1 || max_new < 1 || max_len < 1 || Hkv < 1 || H < Hkv || H % Hkv || window < 0 || (int64_t)T * H > 0x7fffffff) return 0;
     return chunk_attn_workspace(chunk_args(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window));
 }
 
@@ -2413,6 +2413,7 @@ extern "C" int exe_op_chunk_attention_paged(void* hip_stream, int32_t dtype, int
     if (n_seqs < 0 || T < 0 || !cu_seqlens || !q || !kv_blocks || !block_table || !len || !out) return fail(EXE_ERR_ARG, "bad chunk attention arguments");
     if (max_new < 1 || max_len < 1 || window < 0) return fail(EXE_ERR_ARG, "max_new %d, max_len %d, window %d", max_new, max_len, window);
     if (H < Hkv || H % Hkv) return fail(EXE_ERR_SHAPE, "%d query heads over %d key/value heads", H, Hkv);
+    if ((int64_t)T * H > 0x7fffffff) return fail(EXE_ERR_SHAPE, "%d rows of %d heads", T, H);
     const int esz = esz_of_dtype(dtype);
     if (q_stride < (int64_t)H * dh || out_stride < (int64_t)H * dh) return fail(EXE_ERR_SHAPE, "rows of %d heads overlap", H);
     if (q_stride * esz % 16 || out_stride * esz % 16) return fail(EXE_ERR_SHAPE, "rows must begin on 16 bytes");
