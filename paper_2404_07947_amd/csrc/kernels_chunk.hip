@@ -85,7 +85,15 @@ struct ChunkKernelArgs {
     float *acc, *ml;
 };
 
-constexpr int STREAM_ROWS = 16;
+// Row (t, h) of sequence b, by one wave (see chunk_row)
+template <typename T, int DH> __device__ __forceinline__ void row_again(const ChunkKernelArgs& a, int b, int t, int h, KeyRange r, int lane)
+{
+    const int64_t head = (int64_t)DH << a.table.shift;
+    chunk_row<T, DH>((const T*)a.q + (int64_t)t * a.q_stride + h * DH, (const T*)a.kv_blocks + h / a.G * head, 2 * a.Hkv * head, a.Hkv * head, a.table, b, r,
+                     a.scale * LOG2E, lane, (T*)a.out + (int64_t)t * a.out_stride + h * DH);
+}
+
+constexpr int STREAM_ROWS = 16, MAX_PARTS = 64;
 // Keys that the rows r0 .. r1 - 1 of a sequence see, the first one rounded down to a multiple of `align`; first >= last: none.
 // p0: position of the first new token.
 __device__ __forceinline__ KeyRange tile_keys(int p0, int G, int r0, int r1, int window, int limit, int align)
@@ -105,45 +113,113 @@ __device__ __forceinline__ KeyRange part_of(KeyRange k, ChunkKernelArgs::Cut cut
     return KeyRange{first, part + 1 < parts ? first + cut.keys : k.last};
 }
 
-// What the loads of a position without a block read in its place: NaN keys make the scores of the rows that see it NaN.
-static __device__ __align__(16) uint32_t no_block[256] = {
-#define EXE_NAN4 0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu
-#define EXE_NAN16 EXE_NAN4, EXE_NAN4, EXE_NAN4, EXE_NAN4
-#define EXE_NAN64 EXE_NAN16, EXE_NAN16, EXE_NAN16, EXE_NAN16
-    EXE_NAN64, EXE_NAN64, EXE_NAN64, EXE_NAN64
-#undef EXE_NAN64
-#undef EXE_NAN16
-#undef EXE_NAN4
+// What the loads of a position without a block read in its place, 16 rows: NaN keys make the scores of the rows that see it NaN.
+struct NanRows {
+    uint32_t v[16 * 512 / 4];
+    constexpr NanRows() : v() { for (uint32_t& x : v) x = 0xffffffffu; }
 };
+static __device__ const __align__(16) NanRows no_block;
 
-// 1 KB from global memory to LDS by one wave, 16 bytes a lane: from src + voff (per lane) to dst + 16 * lane.  Inline assembly, so that
-// the compiler does not order every later LDS read behind it; whoever reads the tile waits.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void load_to_lds(const void* src, unsigned voff, unsigned dst)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(voff), "s"(src) : "memory", "m0");
-}
-#pragma clang diagnostic pop
 template <int N> __device__ __forceinline__ void wait_loads()        // all but the last N
 {
     asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory");
 }
 
-// The block table of one sequence, read by scalar loads: they do not wait behind the tile loads in flight.
-struct SeqTable {
-    const __attribute__((address_space(4))) int32_t* entry;
-    int max_blocks, shift, n_blocks;
-    __device__ __forceinline__ SeqTable(const PagedTable& t, int b)
-        : entry((const __attribute__((address_space(4))) int32_t*)(uintptr_t)(t.entry + (int64_t)b * t.max_blocks)), max_blocks(t.max_blocks), shift(t.shift),
-          n_blocks(t.n_blocks) {}
-    // entry of the block with position pos >= 0; pos is the same in all lanes
-    __device__ __forceinline__ int at(int pos) const
+// Moves 16 positions (a multiple of 16 on) of one head's keys or values from the cache to LDS, by one wave: LOADS direct loads of 1 KB, RPL rows each,
+// row-major, chunks swizzled (see attn_tile.h).  The loads are inline assembly, so that the compiler does not order every later LDS read
+// behind them; whoever reads the rows waits.  The table is read by scalar loads, which do not wait behind the loads in flight.
+// NT: nontemporal, for rows that no other workgroup reads.
+template <typename T, int DH, bool NT> struct RowLoader {
+    static constexpr int RB = DH * (int)sizeof(T), RPL = 1024 / RB, CPR = RB / 16, LOADS = 16 / RPL, HALF = LOADS / 2;
+    typedef const __attribute__((address_space(4))) int32_t* ScalarPtr;
+    const char* kv;                       // this head's keys of block 0
+    int64_t v_off;                        // bytes from a row's key to its value
+    unsigned block_bytes;
+    ScalarPtr entry;
+    int max_blocks, shift, n_blocks, limit, last, lane;
+    unsigned voff;                        // of load 0; load p's is this one with other chunk bits
+    __device__ __forceinline__ RowLoader(const PagedTable& t, const void* pool, int b, int kvh, int Hkv, int limit_, int last_, int lane_)
+        : entry((ScalarPtr)(uintptr_t)(t.entry + (int64_t)b * t.max_blocks)), max_blocks(t.max_blocks), shift(t.shift), n_blocks(t.n_blocks), limit(limit_), last(last_), lane(lane_)
     {
-        int i = pos >> shift;
-        int e = entry[i < max_blocks ? i : max_blocks - 1];
-        return i < max_blocks && (unsigned)e < (unsigned)n_blocks ? e : -1;
+        const int64_t head = (int64_t)RB << shift;
+        kv = (const char*)pool + kvh * head;
+        v_off = Hkv * head;
+        block_bytes = (unsigned)(2 * v_off);
+        voff = lane / CPR * RB + (((lane & (CPR - 1)) ^ pf_swz<RB>(lane / CPR)) << 4);
     }
+    // Table entries of positions j and j + 8, as they stand: looked at where they are used, so that nothing waits for them before.
+    struct Entries { int e0, e1; };
+    __device__ __forceinline__ Entries lookup(int j) const
+    {
+        const int j0 = j < last ? j : last - 1, j1 = j + 8 < last ? j + 8 : last - 1, i0 = j0 >> shift, i1 = j1 >> shift;
+        return Entries{entry[i0 < max_blocks ? i0 : max_blocks - 1], entry[i1 < max_blocks ? i1 : max_blocks - 1]};
+    }
+    // Where the keys of a position lie, and its value behind them (0 for NaN rows).
+    struct Row { const char* key; int64_t value; };
+    __device__ __forceinline__ Row row(int e, int pos) const
+    {
+        const bool ok = (unsigned)e < (unsigned)n_blocks && pos < limit;
+        const uint64_t at = (uint64_t)(unsigned)e * block_bytes + (unsigned)((pos & ((1 << shift) - 1)) * RB);
+        return Row{ok ? kv + at : (const char*)no_block.v, ok ? v_off : 0};
+    }
+    struct Rows { Row r0, r1; };          // of positions j .. j + 7 and j + 8 .. j + 15; of the last one where those are beyond it
+    __device__ __forceinline__ Rows rows(int j, Entries en) const
+    {
+        if (shift > 3 && j + 8 < last) {                               // one block
+            const Row r = row(en.e0, j);
+            return Rows{r, Row{r.key + 8 * RB, r.value}};
+        }
+        return Rows{row(en.e0, j < last ? j : last - 1), row(en.e1, j + 8 < last ? j + 8 : last - 1)};
+    }
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    // Loads P .. P + HALF - 1, of 8 rows that follow each other from src on.  The immediate offset counts for the source and for LDS.
+    template <int P> __device__ __forceinline__ void half(const char* src, unsigned dst_rows) const
+    {
+        const unsigned dst = dst_rows + P * 1024;
+        auto v = [&](int p) { return voff ^ (pf_swz<RB>(p * RPL) << 4); };
+        if constexpr (HALF == 1) {
+            load_one(src, v(P), dst);
+        } else if constexpr (HALF == 2) {
+#define EXE_HALF2(FLAG)                                                                                                                     \
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3" FLAG "\n\tglobal_load_lds_dwordx4 %2, %3 offset:%4" FLAG   \
+                 ::"s"(dst), "v"(v(P)), "v"(v(P + 1)), "s"(src), "i"(1024) : "memory", "m0")
+            if (NT) EXE_HALF2(" nt");
+            else EXE_HALF2("");
+#undef EXE_HALF2
+        } else {
+#define EXE_HALF4(FLAG)                                                                                                                     \
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5" FLAG "\n\tglobal_load_lds_dwordx4 %2, %5 offset:%6" FLAG   \
+                 "\n\tglobal_load_lds_dwordx4 %3, %5 offset:%7" FLAG "\n\tglobal_load_lds_dwordx4 %4, %5 offset:%8" FLAG                    \
+                 ::"s"(dst), "v"(v(P)), "v"(v(P + 1)), "v"(v(P + 2)), "v"(v(P + 3)), "s"(src), "i"(1024), "i"(2 * 1024), "i"(3 * 1024) : "memory", "m0")
+            if (NT) EXE_HALF4(" nt");
+            else EXE_HALF4("");
+#undef EXE_HALF4
+        }
+    }
+    __device__ __forceinline__ void load_one(const char* src, unsigned v, unsigned dst) const
+    {
+        if (NT) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(dst), "v"(v), "s"(src) : "memory", "m0");
+        else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(v), "s"(src) : "memory", "m0");
+    }
+#pragma clang diagnostic pop
+    // 16 rows from s0 (8 rows) and s1 on; rows of positions from `last` on are last - 1 again
+    __device__ __forceinline__ void move(int j, const char* s0, const char* s1, unsigned dst) const
+    {
+        if (j + 16 <= last) {
+            half<0>(s0, dst);
+            half<HALF>(s1, dst);
+            return;
+        }
+#pragma unroll
+        for (int p = 0; p < LOADS; ++p) {
+            const int half_at = p < HALF ? j : j + 8, in = lane / CPR, row = p % HALF * RPL + in, most = half_at < last ? last - 1 - half_at : 0;
+            const unsigned v = (row < most ? row : most) * RB + (((lane & (CPR - 1)) ^ pf_swz<RB>(p * RPL + in)) << 4);
+            load_one(p < HALF ? s0 : s1, v, dst + p * 1024);
+        }
+    }
+    __device__ __forceinline__ void keys(int j, const Rows& r, unsigned dst) const { move(j, r.r0.key, r.r1.key, dst); }
+    __device__ __forceinline__ void values(int j, const Rows& r, unsigned dst) const { move(j, r.r0.key + r.r0.value, r.r1.key + r.r1.value, dst); }
 };
 
 // A row's query fragments (B operand of the first product): lane (row qi, group g) holds 16-byte chunks 4 * ds + g.  The sign of the
@@ -167,29 +243,25 @@ __device__ __forceinline__ float exponent_scale(float scale) { return scale == 0
 // one a CU).  Per step and wave: S^T = K . Q^T and O^T += V^T . P^T by MFMAs with the 16 rows as columns (see prefill_mfma_kernel); idle
 // columns cost nothing that the loads do not hide.  Probabilities enter the second product as two bf16 parts, 2^-17 relative.
 constexpr int ST_WAVES = 4, ST_STEP = 16;
-template <typename T, int DH> struct Stream {
+template <typename T, int DH, int WAVES> struct Stream {
     static constexpr int RB = DH * (int)sizeof(T), TILE = ST_STEP * RB, STAGE = 2 * TILE;
-    static constexpr int FIT = 65536 / (ST_WAVES * STAGE), STAGES = FIT < 2 ? 2 : FIT;
+    static constexpr int FIT = 16384 / STAGE, STAGES = FIT < 2 ? 2 : FIT;
     static constexpr int LOADS = TILE / 1024;
-    static constexpr int MERGE = ST_WAVES * 16 * (DH + 4) * 4;            // bytes of the waves' results, over the stages
-    static constexpr int LDS = ST_WAVES * STAGES * STAGE > MERGE ? ST_WAVES * STAGES * STAGE : MERGE;
+    static constexpr int MERGE = WAVES * 16 * (DH + 4) * 4;               // bytes of the waves' results, over the stages
+    static constexpr int LDS = WAVES * STAGES * STAGE > MERGE ? WAVES * STAGES * STAGE : MERGE;
 };
 
-template <typename T, int DH>
-__global__ __launch_bounds__(ST_WAVES * 64, 2) void chunk_stream_kernel(ChunkKernelArgs a)
+template <typename T, int DH, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void chunk_stream_kernel(ChunkKernelArgs a)
 {
-    typedef Stream<T, DH> S;
-    constexpr int RB = S::RB, DS = RB / 64, DT = DH / 16, RPL = 1024 / RB, CPR = RB / 16;
+    typedef Stream<T, DH, WAVES> S;
+    constexpr int RB = S::RB, DS = RB / 64, DT = DH / 16;
     extern __shared__ __align__(16) unsigned char st_smem[];
-    __shared__ float s_ml[ST_WAVES][16][2];
+    __shared__ float s_ml[WAVES][16][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), qi = lane & 15, g = lane >> 4;
     const int b = blockIdx.x / a.Hkv, kvh = blockIdx.x - b * a.Hkv, part = blockIdx.y, G = a.G;
     const int t0 = a.cu[b], end = a.cu[b + 1], n = end - t0 < a.tokens ? end - t0 : a.tokens, rows = n * G, p0 = a.len[b] - n, limit = table_limit(a.table);
     if (n <= 0 || rows > a.stream_rows) return;
-    const SeqTable tbl(a.table, b);
-    const int64_t head = (int64_t)DH << a.table.shift, block_elems = 2 * a.Hkv * head;
-    const T* kv = (const T*)a.kv_blocks + kvh * head;
-    const int64_t v_off = a.Hkv * head;
     const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)st_smem + wave * (S::STAGES * S::STAGE);
     const unsigned char* mine = st_smem + wave * (S::STAGES * S::STAGE);
     const float mul = exponent_scale(a.scale);
@@ -202,36 +274,22 @@ __global__ __launch_bounds__(ST_WAVES * 64, 2) void chunk_stream_kernel(ChunkKer
         const KeyRange k = part_of(all, a.stream, part, parts);
         const int row = r0 + qi < r1 ? r0 + qi : r1 - 1, tok = row / G, t = t0 + tok;
         const KeyRange sees = keys_of(p0 + tok, a.window, limit);
+        const int p_min = p0 + r0 / G, p_max = p0 + (r1 - 1) / G;
         // a token beyond the packed ones is none of this call's
         const bool live = r0 + qi < r1 && t >= 0 && t < a.tokens;
         u32x4 qf[DS];
         load_query<T, DS>((const T*)a.q + (int64_t)(live ? t : 0) * a.q_stride + (kvh * G + row % G) * DH, g, a.scale, qf);
 
-        const int steps = k.last > k.first ? (k.last - k.first + ST_STEP - 1) / ST_STEP : 0, own = steps > wave ? (steps - wave + ST_WAVES - 1) / ST_WAVES : 0;
-        int e0 = 0, e1 = 0;
-        auto first_of = [&](int i) { return k.first + (wave + i * ST_WAVES) * ST_STEP; };
-        // a load takes RPL <= 8 rows of one block; rows from k.last on are row k.last - 1 again
-        auto lookup = [&](int i) {
-            int j = first_of(i), j1 = j + 8 < k.last ? j + 8 : j;
-            e0 = tbl.at(j);
-            e1 = tbl.at(j1);
-        };
+        const int steps = k.last > k.first ? (k.last - k.first + ST_STEP - 1) / ST_STEP : 0, own = steps > wave ? (steps - wave + WAVES - 1) / WAVES : 0;
+        typedef RowLoader<T, DH, true> Loader;
+        const Loader from(a.table, a.kv_blocks, b, kvh, a.Hkv, limit, k.last, lane);
+        auto first_of = [&](int i) { return k.first + (wave + i * WAVES) * ST_STEP; };
+        typename Loader::Entries en{-1, -1};
         auto issue = [&](int i) {
-            const int j = first_of(i), block_mask = (1 << tbl.shift) - 1;
             const unsigned dst = lds + i % S::STAGES * S::STAGE;
-#pragma unroll
-            for (int p = 0; p < S::LOADS; ++p) {
-                int key = p * RPL, at = j + key;                       // first row of this load in the step, its position
-                at = at < k.last ? at : (k.last - 1) & -RPL;
-                const int e = key < 8 || at < j + 8 ? e0 : e1;
-                const T* src = e < 0 ? (const T*)no_block : kv + e * block_elems + (int64_t)(at & block_mask) * DH;
-                int in = lane / CPR;
-                const unsigned chunk = ((lane & (CPR - 1)) ^ pf_swz<RB>(key + in)) << 4;
-                in = at + in < k.last ? in : k.last - 1 - at;
-                const unsigned voff = in * RB + chunk;
-                load_to_lds(src, voff, dst + key * RB);
-                load_to_lds(e < 0 ? src : src + v_off, voff, dst + S::TILE + key * RB);
-            }
+            const typename Loader::Rows r = from.rows(first_of(i), en);
+            from.keys(first_of(i), r, dst);
+            from.values(first_of(i), r, dst + S::TILE);
         };
 
         float m = -INFINITY, l = 0.f;                                  // l: this lane's share of the sum
@@ -240,15 +298,15 @@ __global__ __launch_bounds__(ST_WAVES * 64, 2) void chunk_stream_kernel(ChunkKer
         for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         const int ahead = S::STAGES - 1;
         for (int i = 0; i < ahead && i < own; ++i) {
-            lookup(i);
+            en = from.lookup(first_of(i));
             issue(i);
         }
-        if (ahead < own) lookup(ahead);
+        if (ahead < own) en = from.lookup(first_of(ahead));
         for (int i = 0; i < own; ++i) {
             if (i + ahead < own) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // step i - 1 has left its stage
                 issue(i + ahead);
-                if (i + ahead + 1 < own) lookup(i + ahead + 1);
+                if (i + ahead + 1 < own) en = from.lookup(first_of(i + ahead + 1));
                 wait_loads<2 * S::LOADS * (S::STAGES - 1)>();
             } else {
                 wait_loads<0>();
@@ -261,9 +319,20 @@ __global__ __launch_bounds__(ST_WAVES * 64, 2) void chunk_stream_kernel(ChunkKer
                 s[ds & 1] = HalfUnit<T>::mma(fk, qf[ds], s[ds & 1]);
             }
             f32x4 sc = s[0] + s[1];
-            const int key0 = first_of(i) + 4 * g;
+            const unsigned char* sV = sK + S::TILE;
+            const int v_row = 4 * g + (qi >> 2), v_q = qi & 3;
+            uint2 fv[sizeof(T) == 2 ? DT : 1];                         // on their way while the softmax is made
+            if constexpr (sizeof(T) == 2) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sc[r] = key0 + r >= sees.first && key0 + r < sees.last ? sc[r] : -INFINITY;
+                for (int dt = 0; dt < DT; ++dt) fv[dt] = pf_read_tr(sV + v_row * RB + (((2 * dt + (v_q >> 1)) ^ pf_swz<RB>(v_row)) << 4) + (v_q & 1) * 8);
+            }
+            const int j = first_of(i);
+            if (j + ST_STEP - 1 > p_min || (a.window && j <= p_max - a.window)) {
+                int key0 = j + 4 * g;
+                asm volatile("" : "+v"(key0));                         // keeps the mask arithmetic inside this branch
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sc[r] = key0 + r >= sees.first && key0 + r < sees.last ? sc[r] : -INFINITY;
+            }
             float mx = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])) * mul;
             // the maximum follows only where it grew by more than 2^8: sums stay far from a float's ends
             if (__builtin_amdgcn_ballot_w64(mx > m + 8.f)) {
@@ -279,7 +348,6 @@ __global__ __launch_bounds__(ST_WAVES * 64, 2) void chunk_stream_kernel(ChunkKer
                 sc[r] = fast_exp2(fmaf(sc[r], mul, -ref));
                 l += sc[r];
             }
-            const unsigned char* sV = sK + S::TILE;
             if constexpr (sizeof(T) == 2) {
                 typedef __attribute__((ext_vector_type(4))) short v4s;
                 bf16x4 hi, lo;
@@ -288,12 +356,10 @@ __global__ __launch_bounds__(ST_WAVES * 64, 2) void chunk_stream_kernel(ChunkKer
                     hi[r] = (bf16_t)sc[r];
                     lo[r] = (bf16_t)(sc[r] - (float)hi[r]);
                 }
-                const int v_row = 4 * g + (qi >> 2), v_q = qi & 3;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
-                    uint2 v = pf_read_tr(sV + v_row * RB + (((2 * dt + (v_q >> 1)) ^ pf_swz<RB>(v_row)) << 4) + (v_q & 1) * 8);
-                    o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, v), __builtin_bit_cast(v4s, hi), o[dt], 0, 0, 0);
-                    o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, v), __builtin_bit_cast(v4s, lo), o[dt], 0, 0, 0);
+                    o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, fv[dt]), __builtin_bit_cast(v4s, lo), o[dt], 0, 0, 0);
+                    o[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, fv[dt]), __builtin_bit_cast(v4s, hi), o[dt], 0, 0, 0);
                 }
             } else {
 #pragma unroll
@@ -320,15 +386,15 @@ __global__ __launch_bounds__(ST_WAVES * 64, 2) void chunk_stream_kernel(ChunkKer
             s_ml[wave][qi][1] = l;
         }
         __syncthreads();
-        const int r = tid >> 4, c = tid & 15;                          // 16 threads a row, features 4 * c .. +3 of every 64
+        const int r = tid >> 4 & 15, c = tid & 15;                     // 16 threads a row (of the first 256), features 4 * c .. +3 of every 64
         const int wtok = (r0 + r) / G, wt = t0 + wtok, h = kvh * G + (r0 + r) % G;
-        const bool write = r0 + r < r1 && wt >= 0 && wt < a.tokens;
-        float M = -INFINITY, L = 0.f, w[ST_WAVES];
+        const bool write = tid < 256 && r0 + r < r1 && wt >= 0 && wt < a.tokens;
+        float M = -INFINITY, L = 0.f, w[WAVES];
 #pragma unroll
-        for (int i = 0; i < ST_WAVES; ++i) M = fmaxf(M, s_ml[i][r][0]);
+        for (int i = 0; i < WAVES; ++i) M = fmaxf(M, s_ml[i][r][0]);
         const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
-        for (int i = 0; i < ST_WAVES; ++i) {
+        for (int i = 0; i < WAVES; ++i) {
             w[i] = fast_exp2(s_ml[i][r][0] - ref);
             L += s_ml[i][r][1] * w[i];
         }
@@ -337,7 +403,7 @@ __global__ __launch_bounds__(ST_WAVES * 64, 2) void chunk_stream_kernel(ChunkKer
         for (int f = 0; f < DH / 64; ++f) {
             v[f] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < ST_WAVES; ++i) v[f] += *(const f32x4*)(s_o + (i * 16 + r) * (DH + 4) + f * 64 + 4 * c) * w[i];
+            for (int i = 0; i < WAVES; ++i) v[f] += *(const f32x4*)(s_o + (i * 16 + r) * (DH + 4) + f * 64 + 4 * c) * w[i];
         }
         if (parts > 1) {
             if (write) {
@@ -372,8 +438,7 @@ __global__ __launch_bounds__(ST_WAVES * 64, 2) void chunk_stream_kernel(ChunkKer
             for (int i = 0; i < 4; ++i)
                 if (again >> (16 * i) & 0xffff) {
                     const int rr = r0 + wave * 4 + i, tk = rr / G, hh = kvh * G + rr % G;
-                    chunk_row<T, DH>((const T*)a.q + (int64_t)(t0 + tk) * a.q_stride + hh * DH, kv, block_elems, v_off, a.table, b, keys_of(p0 + tk, a.window, limit),
-                                     a.scale * LOG2E, lane, (T*)a.out + (int64_t)(t0 + tk) * a.out_stride + hh * DH);
+                    row_again<T, DH>(a, b, t0 + tk, hh, keys_of(p0 + tk, a.window, limit), lane);
                 }
         }
         __syncthreads();                                               // before the next tile's loads overwrite the results
@@ -385,50 +450,60 @@ __global__ __launch_bounds__(ST_WAVES * 64, 2) void chunk_stream_kernel(ChunkKer
 // for keys, two for values, filled by direct global-to-LDS loads a tile ahead, one barrier a tile.  The products are those of
 // prefill_mfma_kernel.  A wave computes the scores of tile kt + 1 before it needs those of tile kt's successor: the MFMAs of the one
 // and the exponentials of the other do not depend on each other.
-constexpr int CT_WAVES = 4, CT_KEYS = 64;
-template <typename T, int DH> constexpr int ct_lds() { return 4 * CT_KEYS * DH * (int)sizeof(T); }
-template <typename T, int DH, int QB> constexpr int ct_per_cu() { return QB == 4 ? 1 : sizeof(T) == 4 && DH == 128 ? 1 : QB == 2 || DH == 128 ? 2 : 3; }
+constexpr int CT_WAVES = 4, CT_ALIGN = 64;
+template <typename T, int DH, int QB> constexpr int ct_keys() { return QB == 1 && DH * (int)sizeof(T) > 128 ? 32 : 64; }
+template <typename T, int DH, int QB> constexpr int ct_lds() { return 4 * ct_keys<T, DH, QB>() * DH * (int)sizeof(T); }
+template <typename T, int DH, int QB> constexpr int ct_per_cu()
+{
+    if (sizeof(T) == 4) return DH == 128 ? 2 : 3;
+    return QB == 2 ? DH == 128 ? 2 : 3 : 4;
+}
+
+// Workgroup -> (slot, head), see prefill_mfma_kernel: the tiles of one sequence and head run side by side on one XCD.  Last rows (most
+// keys) first.  Slot -> tile: those of sequence b begin at slot floor(cu[b] * G / tile_rows) + b, which leaves room for every sequence's
+// last, partly filled tile whatever the lengths are.  b = -1: no tile, or a sequence of the streaming kernel's.
+struct ChunkTile { int b, kvh, t0, rows, p0, r0; };
+__device__ __forceinline__ ChunkTile find_tile(const ChunkKernelArgs& a, unsigned wg, int slots, int tile_rows, int lane)
+{
+    int slot, kvh;
+    if ((a.Hkv & 7) == 0) {
+        int hpx = a.Hkv >> 3, j = wg >> 3;
+        slot = j / hpx;
+        kvh = (wg & 7) + 8 * (j - slot * hpx);
+    } else {
+        slot = wg / a.Hkv;
+        kvh = wg - slot * a.Hkv;
+    }
+    slot = slots - 1 - slot;
+    auto first_slot = [&](int64_t t, int b) { return (int)(t * a.G / tile_rows) + b; };
+    const int b = __builtin_amdgcn_readfirstlane(wave_search(0, a.n_seqs, lane, [&](int i) { return first_slot(a.cu[i], i) <= slot; }));
+    if (b < 0) return ChunkTile{-1};
+    const int t0 = a.cu[b], end = a.cu[b + 1], n = end - t0 < a.tokens ? end - t0 : a.tokens, rows = n * a.G;
+    const int r0 = (slot - first_slot(t0, b)) * tile_rows;
+    return ChunkTile{n <= 0 || r0 >= rows || rows <= a.stream_rows ? -1 : b, kvh, t0, rows, a.len[b] - n, r0};
+}
 
 template <typename T, int DH, int QB>
 __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk_tile_kernel(ChunkKernelArgs a, int slots)
 {
-    constexpr int RB = DH * (int)sizeof(T), DS = RB / 64, DT = DH / 16, RPL = 1024 / RB, CPR = RB / 16, LOADS = 16 / RPL, TILE = CT_KEYS * RB;
+    constexpr int RB = DH * (int)sizeof(T), DS = RB / 64, DT = DH / 16, KT = ct_keys<T, DH, QB>(), KB = KT / 16, TILE = KT * RB;
     constexpr int ROWS = 16 * QB * CT_WAVES;
     extern __shared__ __align__(16) unsigned char ct_smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), qi = lane & 15, g = lane >> 4;
     const int G = a.G, part = blockIdx.y;
-    // Workgroup -> (slot, head), see prefill_mfma_kernel: the tiles of one sequence and head run side by side on one XCD.  Last rows
-    // (most keys) first.
-    int slot, kvh;
-    if ((a.Hkv & 7) == 0) {
-        int hpx = a.Hkv >> 3, j = blockIdx.x >> 3;
-        slot = j / hpx;
-        kvh = (blockIdx.x & 7) + 8 * (j - slot * hpx);
-    } else {
-        slot = blockIdx.x / a.Hkv;
-        kvh = blockIdx.x - slot * a.Hkv;
-    }
-    slot = slots - 1 - slot;
-    // Slot -> tile: those of sequence b begin at slot floor(cu[b] * G / ROWS) + b, which leaves room for every sequence's last, partly
-    // filled tile whatever the lengths are.
-    const int b = __builtin_amdgcn_readfirstlane(wave_search(0, a.n_seqs, lane, [&](int i) { return (int)((int64_t)a.cu[i] * G / ROWS) + i <= slot; }));
-    if (b < 0) return;
-    const int t0 = a.cu[b], end = a.cu[b + 1], n = end - t0 < a.tokens ? end - t0 : a.tokens, rows = n * G, p0 = a.len[b] - n, limit = table_limit(a.table);
-    const int r0 = (slot - ((int)((int64_t)t0 * G / ROWS) + b)) * ROWS;
-    if (n <= 0 || r0 >= rows || rows <= a.stream_rows) return;
-    const KeyRange all = tile_keys(p0, G, r0, r0 + ROWS < rows ? r0 + ROWS : rows, a.window, limit, CT_KEYS);
+    const ChunkTile tile = find_tile(a, blockIdx.x, slots, ROWS, lane);
+    if (tile.b < 0) return;
+    const int b = tile.b, kvh = tile.kvh, t0 = tile.t0, rows = tile.rows, p0 = tile.p0, r0 = tile.r0, limit = table_limit(a.table);
+    const KeyRange all = tile_keys(p0, G, r0, r0 + ROWS < rows ? r0 + ROWS : rows, a.window, limit, CT_ALIGN);
     const int parts = parts_of(all, a.tile);
     if (part >= parts) return;
     const KeyRange k = part_of(all, a.tile, part, parts);
-    const SeqTable tbl(a.table, b);
-    const int64_t head = (int64_t)DH << a.table.shift, block_elems = 2 * a.Hkv * head, v_off = a.Hkv * head;
-    const T* kv = (const T*)a.kv_blocks + kvh * head;
     const float mul = exponent_scale(a.scale);
     const int w0 = r0 + wave * (16 * QB);                              // this wave's first row
     const int wl = w0 + 16 * QB < rows ? w0 + 16 * QB - 1 : rows - 1;  // and last one
     const bool active = w0 < rows;
     const int p_min = p0 + w0 / G, p_max = p0 + wl / G;
-    const int n_tiles = k.last > k.first ? (k.last - k.first + CT_KEYS - 1) / CT_KEYS : 0;
+    const int n_tiles = k.last > k.first ? (k.last - k.first + KT - 1) / KT : 0;
 
     u32x4 qf[QB][DS];
     KeyRange sees[QB];
@@ -441,32 +516,37 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
         load_query<T, DS>((const T*)a.q + (int64_t)(t >= 0 && t < a.tokens ? t : 0) * a.q_stride + (kvh * G + row % G) * DH, g, a.scale, qf[qb]);
     }
 
-    // ---- loaders: wave w fills rows 16 * w .. +15 of a tile
+    // ---- loaders.  Tiles of 64 keys: wave w fills rows 16 * w .. +15 of keys and of values; of 32: waves 0 and 1 the keys, 2 and 3 the values
     const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)ct_smem;
-    struct Entries { int e0, e1; };
-    auto lookup = [&](int kt) {
-        int j = k.first + kt * CT_KEYS + wave * 16;
-        j = j < k.last ? j : k.last - 1;
-        int j1 = j + 8 < k.last ? j + 8 : k.last - 1;
-        return Entries{tbl.at(j), tbl.at(j1)};
-    };
-    auto load_tile = [&](int kt, Entries en, int64_t off, unsigned dst) {
-        const int j = k.first + kt * CT_KEYS + wave * 16, block_mask = (1 << tbl.shift) - 1;
-#pragma unroll
-        for (int p = 0; p < LOADS; ++p) {
-            int key = p * RPL, at = j + key;
-            // rows from k.last on are row k.last - 1 again; the second entry is of row j + 8 or of the last one
-            const int e = key < 8 ? en.e0 : en.e1;
-            at = at < k.last ? at : (k.last - 1) & -RPL;
-            const T* src = e < 0 ? (const T*)no_block : kv + e * block_elems + off + (int64_t)(at & block_mask) * DH;
-            int in = lane / CPR;
-            const unsigned chunk = ((lane & (CPR - 1)) ^ pf_swz<RB>(key + in)) << 4;
-            in = at + in < k.last ? in : k.last - 1 - at;
-            load_to_lds(src, in * RB + chunk, dst + (wave * 16 + key) * RB);
+    typedef RowLoader<T, DH, false> Loader;
+    typedef typename Loader::Entries Entries;
+    typedef typename Loader::Rows Rows;
+    const Loader from(a.table, a.kv_blocks, b, kvh, a.Hkv, limit, k.last, lane);
+    const int my_rows = wave % KB * 16;
+    const unsigned dst = lds + my_rows * RB;
+    auto first_of = [&](int kt) { return k.first + kt * KT + my_rows; };
+    auto lookup = [&](int kt) { return from.lookup(first_of(kt)); };
+    auto load_k = [&](int kt, const Rows& r) { from.keys(first_of(kt), r, dst + (kt & 1) * TILE); };
+    auto load_v = [&](int kt, const Rows& r) { from.values(first_of(kt), r, dst + (2 + (kt & 1)) * TILE); };
+    // brings values of tile kt and keys of kt + 1
+    Entries en;
+    Rows rv;                                                           // tiles of 64: the next values' rows, those that the keys came from
+    auto bring = [&](int kt) {
+        if constexpr (KT == 64) {
+            if (kt >= 0) load_v(kt, rv);
+            if (kt + 1 < n_tiles) {
+                rv = from.rows(first_of(kt + 1), en);
+                load_k(kt + 1, rv);
+            }
+            en = lookup(kt + 2);
+        } else if (wave < 2) {
+            if (kt + 1 < n_tiles) load_k(kt + 1, from.rows(first_of(kt + 1), en));
+            en = lookup(kt + 2);
+        } else if (kt >= 0) {
+            load_v(kt, from.rows(first_of(kt), en));
+            en = lookup(kt + 1);
         }
     };
-    auto load_k = [&](int kt, Entries en) { load_tile(kt, en, 0, lds + (kt & 1) * TILE); };
-    auto load_v = [&](int kt, Entries en) { load_tile(kt, en, v_off, lds + (2 + (kt & 1)) * TILE); };
 
     f32x4 o[QB][DT];
     float m[QB], l[QB];                                                // l: this lane's share
@@ -478,11 +558,11 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
         for (int dt = 0; dt < DT; ++dt) o[qb][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    typedef f32x4 Scores[QB][4];
+    typedef f32x4 Scores[QB][KB];
     auto scores = [&](int kt, Scores& s) {
         const unsigned char* sK = ct_smem + (kt & 1) * TILE;
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
+        for (int kb = 0; kb < KB; ++kb) {
             f32x4 c[QB][2];
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) c[qb][0] = c[qb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -497,31 +577,44 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
             for (int qb = 0; qb < QB; ++qb) s[qb][kb] = sizeof(T) == 4 ? c[qb][0] + c[qb][1] : c[qb][0];
         }
     };
+    // the largest raw score of this lane's
+    auto largest = [&](Scores& s, float (&mx)[QB]) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            mx[qb] = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) mx[qb] = fmaxf(mx[qb], s[qb][kb][r]);
+        }
+    };
     // masks, and moves the running maxima where a score passes one by more than 2^8
-    auto look = [&](int kt, Scores& s) {
-        const int j = k.first + kt * CT_KEYS;
-        if (j + CT_KEYS - 1 > p_min || j + CT_KEYS > k.last || (a.window && j <= p_max - a.window)) {
+    auto look = [&](int kt, Scores& s, float (&mx)[QB]) {
+        const int j = k.first + kt * KT;
+        if (j + KT - 1 > p_min || j + KT > k.last || (a.window && j <= p_max - a.window)) {
             int key0 = j + 4 * g;
             asm volatile("" : "+v"(key0));                             // keeps the mask arithmetic inside this branch
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-                for (int kb = 0; kb < 4; ++kb)
+                for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        int key = key0 + kb * 16 + r;
-                        s[qb][kb][r] = key >= sees[qb].first && key < sees[qb].last && key < k.last ? s[qb][kb][r] : -INFINITY;
-                    }
+                    for (int r = 0; r < 4; ++r)
+                        s[qb][kb][r] = key0 + kb * 16 + r < (sees[qb].last < k.last ? sees[qb].last : k.last) ? s[qb][kb][r] : -INFINITY;
+            if (a.window) {
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            s[qb][kb][r] = key0 + kb * 16 + r >= sees[qb].first ? s[qb][kb][r] : -INFINITY;
+            }
+            largest(s, mx);
         }
-        float mx[QB];
         bool grew = false;
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
-            mx[qb] = -INFINITY;
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) mx[qb] = fmaxf(mx[qb], s[qb][kb][r]);
             mx[qb] *= mul;
             grew |= mx[qb] > m[qb] + 8.f;
         }
@@ -541,7 +634,7 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
         for (int qb = 0; qb < QB; ++qb) {
             const float ref = m[qb] == -INFINITY ? 0.f : m[qb];
 #pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     s[qb][kb][r] = fast_exp2(fmaf(s[qb][kb][r], mul, -ref));
@@ -558,7 +651,7 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) c[qb][0] = c[qb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int kb = 0; kb < 4; ++kb)
+                for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         float v = *(const float*)(tV + (kb * 16 + 4 * g + r) * RB + (((4 * dt + (qi >> 2)) ^ pf_swz<RB>(4 * g + r)) << 4) + (qi & 3) * 4);
@@ -572,7 +665,7 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
             const int v_row = 4 * g + (qi >> 2), v_q = qi & 3;
             const unsigned char* sV = tV + v_row * RB + (v_q & 1) * 8;
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
+            for (int ks = 0; ks < KB / 2; ++ks) {
                 // one rounding to bf16 per probability, half a step of the result's own type
                 bf16x8 pf[QB];
 #pragma unroll
@@ -592,34 +685,48 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
     };
 
     if (n_tiles > 0) {
-        // tile kt's values are loaded an iteration before its second product, its keys two before that
+        // Tile kt's values are loaded an iteration before its second product, its keys an iteration before that.
         Scores s[2];
-        Entries ek = lookup(0), ev = ek;
-        load_k(0, ek);
+        float mx[QB];
+        en = lookup(0);
+        bring(-1);
         wait_loads<0>();
         __syncthreads();
-        load_v(0, ek);
-        ek = lookup(n_tiles > 1 ? 1 : 0);
-        if (n_tiles > 1) load_k(1, ek);
-        ev = ek;
-        ek = lookup(n_tiles > 2 ? 2 : 0);
-        if (active) scores(0, s[0]);
+        bring(0);
+        if (active) {
+            scores(0, s[0]);
+            largest(s[0], mx);
+            look(0, s[0], mx);
+        }
         auto iteration = [&](int kt, Scores& now, Scores& next) {
             wait_loads<0>();                                           // values of tile kt, keys of kt + 1
             __syncthreads();
-            if (kt + 1 < n_tiles) load_v(kt + 1, ev);
-            if (kt + 2 < n_tiles) load_k(kt + 2, ek);
-            ev = ek;
-            ek = lookup(kt + 3 < n_tiles ? kt + 3 : 0);
+            bring(kt + 1);
             if (!active) return;
-            look(kt, now);
-            if (kt + 1 < n_tiles) scores(kt + 1, next);
+            scores(kt + 1, next);
             exponentials(now);
             values(kt, now);
+            largest(next, mx);
+            look(kt + 1, next, mx);
         };
-        for (int kt = 0; kt < n_tiles; kt += 2) {
+        int kt = 0;
+        for (; kt + 2 < n_tiles; kt += 2) {
             iteration(kt, s[0], s[1]);
-            if (kt + 1 < n_tiles) iteration(kt + 1, s[1], s[0]);
+            iteration(kt + 1, s[1], s[0]);
+        }
+        if (kt + 1 < n_tiles) {
+            iteration(kt, s[0], s[1]);
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb) s[0][qb][kb] = s[1][qb][kb];
+            ++kt;
+        }
+        wait_loads<0>();
+        __syncthreads();
+        if (active) {
+            exponentials(s[0]);
+            values(kt, s[0]);
         }
     }
     if (!active) return;
@@ -664,28 +771,15 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
         }
         for (; again; again &= again - 1) {
             const int rr = w0 + qb * 16 + __builtin_ctz(again), tk = rr / G, hh = kvh * G + rr % G;
-            chunk_row<T, DH>((const T*)a.q + (int64_t)(t0 + tk) * a.q_stride + hh * DH, kv, block_elems, v_off, a.table, b, keys_of(p0 + tk, a.window, limit), a.scale * LOG2E,
-                             lane, (T*)a.out + (int64_t)(t0 + tk) * a.out_stride + hh * DH);
+            row_again<T, DH>(a, b, t0 + tk, hh, keys_of(p0 + tk, a.window, limit), lane);
         }
     }
 }
 
 // ---------------------------------------------------------------- parts of the keys, joined
-// A wave per row: sum over the parts of 2^(m_i - M) times their sums, in the order of the parts.  Rows of a single part are complete.
-template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_kernel(ChunkKernelArgs a)
+// Row (t, h) of sequence b at position p, by one wave: sum over the parts of 2^(m_i - M) times their sums, in the order of the parts.
+template <typename T, int DH> __device__ __forceinline__ void join_row(const ChunkKernelArgs& a, int b, int t, int h, int p, int parts, int lane)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int t = (int)(unit / a.H), h = (int)(unit - (int64_t)t * a.H), G = a.G;
-    if (t >= a.tokens) return;
-    const ChunkSeq sq = seq_of_token(a.cu, a.n_seqs, t, lane);
-    if (sq.b < 0) return;
-    const int rows = sq.n * G, p0 = a.len[sq.b] - sq.n, limit = table_limit(a.table), row = (t - sq.t0) * G + h % G;
-    const bool streamed = rows <= a.stream_rows;
-    const ChunkKernelArgs::Cut cut = streamed ? a.stream : a.tile;
-    const int tile = streamed ? STREAM_ROWS : a.tile_rows, r0 = row / tile * tile;
-    const int parts = parts_of(tile_keys(p0, G, r0, r0 + tile < rows ? r0 + tile : rows, a.window, limit, streamed ? ST_STEP : CT_KEYS), cut);
-    if (parts <= 1) return;
     const int64_t at = (int64_t)t * a.H + h, step = (int64_t)a.tokens * a.H;
     float M = -INFINITY;
     for (int i = lane; i < parts; i += 64) M = fmaxf(M, a.ml[(at + i * step) * 2]);
@@ -700,7 +794,7 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_
 #pragma unroll
         for (int f = 0; f < DH / 64; ++f) v[f] = fmaf(a.acc[(at + i * step) * DH + f * 64 + lane], w, v[f]);
     }
-    const KeyRange ks = keys_of(p0 + (t - sq.t0), a.window, limit);
+    const KeyRange ks = keys_of(p, a.window, table_limit(a.table));
     T* op = (T*)a.out + (int64_t)t * a.out_stride + h * DH;
     float most = 0.f;
 #pragma unroll
@@ -709,18 +803,95 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_
         most = __builtin_elementwise_maximum(most, v[f]);
     }
     if (__builtin_amdgcn_ballot_w64(most != most)) {                   // as in the kernels above
-        const int64_t head = (int64_t)DH << a.table.shift;
-        chunk_row<T, DH>((const T*)a.q + (int64_t)t * a.q_stride + h * DH, (const T*)a.kv_blocks + h / G * head, 2 * a.Hkv * head, a.Hkv * head, a.table, sq.b, ks,
-                         a.scale * LOG2E, lane, op);
+        row_again<T, DH>(a, b, t, h, ks, lane);
         return;
     }
 #pragma unroll
     for (int f = 0; f < DH / 64; ++f) op[f * 64 + lane] = from_f32<T>(v[f]);
 }
 
+// Of the streaming kernel's sequences: a workgroup per (sequence, key/value head), as that kernel.  Rows of a single part are complete.
+template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_stream_kernel(ChunkKernelArgs a)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = a.G;
+    const int b = blockIdx.x / a.Hkv, kvh = blockIdx.x - b * a.Hkv;
+    const int t0 = a.cu[b], end = a.cu[b + 1], n = end - t0 < a.tokens ? end - t0 : a.tokens, rows = n * G, p0 = a.len[b] - n, limit = table_limit(a.table);
+    if (n <= 0 || rows > a.stream_rows) return;
+    for (int r = wave; r < rows; r += 4) {
+        const int r0 = r & -STREAM_ROWS, t = t0 + r / G;
+        const int parts = parts_of(tile_keys(p0, G, r0, r0 + STREAM_ROWS < rows ? r0 + STREAM_ROWS : rows, a.window, limit, ST_STEP), a.stream);
+        if (parts > 1 && t >= 0 && t < a.tokens) join_row<T, DH>(a, b, t, kvh * G + r % G, p0 + r / G, parts, lane);
+    }
+}
+// Of the tile kernel's: 1024 / DH rows a workgroup, DH / 4 threads each.
+template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_tile_kernel(ChunkKernelArgs a, int slots)
+{
+    constexpr int PER = DH / 4;
+    const int tid = threadIdx.x, lane = tid & 63, G = a.G;
+    const ChunkTile tile = find_tile(a, blockIdx.x, slots, a.tile_rows, lane);
+    if (tile.b < 0) return;
+    const int limit = table_limit(a.table), r1 = tile.r0 + a.tile_rows < tile.rows ? tile.r0 + a.tile_rows : tile.rows;
+    const int parts = parts_of(tile_keys(tile.p0, G, tile.r0, r1, a.window, limit, CT_ALIGN), a.tile);
+    if (parts <= 1) return;
+    const int64_t step = (int64_t)a.tokens * a.H;
+    const int row = tile.r0 + (blockIdx.y * 256 + tid) / PER, f = tid % PER * 4, tok = row / G, t = tile.t0 + tok, h = tile.kvh * G + row % G;
+    const bool live = row < r1 && t >= 0 && t < a.tokens;
+    const int64_t at = live ? (int64_t)t * a.H + h : 0;
+    const float* ml = a.ml + at * 2;
+    const float* acc = a.acc + at * DH + f;
+    // the parts' weights: a lane of the row takes a part
+    constexpr int EACH = MAX_PARTS / PER;
+    __shared__ float s_w[1024 / DH][MAX_PARTS];
+    float2 x[EACH];
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int k = i * PER + tid % PER;
+        x[i] = k < parts ? *(const float2*)(ml + k * step * 2) : float2{-INFINITY, 0.f};
+        M = fmaxf(M, x[i].x);
+    }
+#pragma unroll
+    for (int d = PER / 2; d; d >>= 1) M = fmaxf(M, __shfl_xor(M, d, WAVE));
+    const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const float w = fast_exp2(x[i].x - ref);
+        s_w[tid / PER][i * PER + tid % PER] = w;
+        L = fmaf(x[i].y, w, L);
+    }
+#pragma unroll
+    for (int d = PER / 2; d; d >>= 1) L += __shfl_xor(L, d, WAVE);
+    __syncthreads();
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int k = 0; k < parts; ++k) v += *(const f32x4*)(acc + k * step * DH) * s_w[tid / PER][k];
+    const KeyRange ks = keys_of(tile.p0 + tok, a.window, limit);
+    float most = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[e] = ks.last > ks.first ? v[e] / L : 0.f;
+        most = __builtin_elementwise_maximum(most, v[e]);
+    }
+    // as in the kernels above; the rows of a wave are whole ones
+    const unsigned long long again = __builtin_amdgcn_ballot_w64(live && most != most);
+    const unsigned long long mine = PER == 32 ? 0xffffffffull << (lane & 32) : 0xffffull << (lane & 48);
+    if (live && !(again & mine)) {
+        typename Vec4<T>::type x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = from_f32<T>(v[e]);
+        *(typename Vec4<T>::type*)((T*)a.out + (int64_t)t * a.out_stride + h * DH + f) = x;
+    }
+    for (int j = 0; j < 64 / PER; ++j)
+        if (again >> (j * PER) & (PER == 32 ? 0xffffffffull : 0xffffull)) {
+            const int rr = __builtin_amdgcn_readfirstlane(row - lane / PER) + j, tk = rr / G;
+            row_again<T, DH>(a, tile.b, tile.t0 + tk, tile.kvh * G + rr % G, keys_of(tile.p0 + tk, a.window, limit), lane);
+        }
+}
+
 // ---------------------------------------------------------------- launches
 struct ChunkPlan {
     bool stream, tile;               // which kernels run
+    int waves;                       // of the streaming kernel's workgroups
     int qb;                          // row blocks per wave of the tile kernel
     int64_t slots;
     ChunkKernelArgs::Cut stream_cut, tile_cut;
@@ -728,12 +899,12 @@ struct ChunkPlan {
 };
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Parts for `wgs` workgroups that each would take up to max_len keys: enough workgroups to fill the chip `rounds` times over, no part
-// shorter than `least` keys.
+// Parts for `wgs` workgroups that each would take up to max_len keys, so that `want` come of them, no part shorter than `least` keys.
 static ChunkKernelArgs::Cut cut_keys(int64_t wgs, int64_t max_len, int64_t want, int least, int align)
 {
     int64_t parts = want / wgs, most = ceil_div(max_len, least);
     parts = parts < most ? parts : most;
+    parts = parts < MAX_PARTS ? parts : MAX_PARTS;
     if (parts <= 1) return {1, 0x7fffffff};
     int64_t keys = ceil_div(ceil_div(max_len, parts), align) * align;
     return {(int)ceil_div(max_len, keys), (int)keys};
@@ -742,16 +913,40 @@ static ChunkKernelArgs::Cut cut_keys(int64_t wgs, int64_t max_len, int64_t want,
 static ChunkPlan chunk_plan(const ChunkAttnArgs& a)
 {
     ChunkPlan p{};
-    const int64_t G = a.H / a.Hkv, rows = (int64_t)a.max_new * G, seen = a.window && a.window + (int64_t)a.max_new < a.max_len ? a.window + (int64_t)a.max_new : a.max_len;
+    const int64_t G = a.H / a.Hkv, rows = (int64_t)a.max_new * G, T = a.tokens;
+    const int64_t seen = a.window && (int64_t)a.window + a.max_new < a.max_len ? (int64_t)a.window + a.max_new : a.max_len;
+    const bool f32 = a.dtype == DT_F32;
+    const ChunkKernelArgs::Cut whole{1, 0x7fffffff};
     p.tile = rows > STREAM_ROWS;
-    // a sequence of up to 16 rows beside longer ones: not where there is one sequence, or all bring max_new tokens
-    p.stream = !p.tile || (a.n_seqs > 1 && (int64_t)a.tokens <= (int64_t)(a.n_seqs - 1) * a.max_new + STREAM_ROWS / G);
-    if (p.stream) p.stream_cut = cut_keys((int64_t)a.n_seqs * a.Hkv, seen, 2048, 256, ST_STEP);
+    // Beside longer sequences one of up to 16 rows goes to the streaming kernel, not where there can be none (one sequence, or all bring
+    // max_new tokens), and not where they are few and none is long: the tile kernel then takes it along, in the time that its other
+    // sequences take, and a launch or two are saved (8 chunks of 97 to 256 tokens, 40 heads: 59 us, of them 9).
+    p.stream = !p.tile || (a.n_seqs > 1 && T <= (int64_t)(a.n_seqs - 1) * a.max_new + STREAM_ROWS / G && (T * G < (int64_t)64 * a.n_seqs || seen > 4096));
+    if (p.stream) {
+        const int64_t wgs = (int64_t)a.n_seqs * a.Hkv;
+        // At most one workgroup a CU: of 8 waves (float x 128 fills a CU's LDS with 4), as many parts as CUs are left.  Short ones whole: a
+        // second launch takes longer than the keys (1 x 40 heads of 512 keys: 10.3 us, in 4 parts 10.0 and a launch; of 1024: 15.4, 11.4).
+        // 6 x 40 heads of 2048 keys: 41.7 us, with 4 waves in 8 parts 47.2.
+        // More: two of 4 waves a CU; four times as many workgroups even out lengths that differ (64 x 8 heads of 500 to 8100 keys 182 us, whole
+        // 200; of 4096 each 169 and 161).
+        if (wgs <= 256) {
+            p.waves = f32 && a.dh == 128 ? ST_WAVES : 8;
+            p.stream_cut = seen <= 640 ? whole : cut_keys(wgs, seen, 256, 128, ST_STEP);
+        } else {
+            p.waves = ST_WAVES;
+            p.stream_cut = cut_keys(wgs, seen, 2048, 256, ST_STEP);
+        }
+    }
     if (p.tile) {
-        auto wgs = [&](int qb) { return (ceil_div((int64_t)a.tokens * G, 64 * qb) + (a.n_seqs - 1)) * a.Hkv; };
-        p.qb = a.dtype == DT_BF16 && wgs(4) >= 224 ? 4 : wgs(2) >= 320 ? 2 : 1;
-        p.slots = (int64_t)a.tokens * G / (64 * p.qb) + a.n_seqs;
-        p.tile_cut = cut_keys(wgs(p.qb), seen, 640, 512, CT_KEYS);
+        auto wgs = [&](int qb) { return (ceil_div(T * G, 64 * qb) + (a.n_seqs - 1)) * a.Hkv; };
+        // 128 rows a workgroup where several of its tiles share their keys, with 64 features only where the chip is full of them: bf16, us of
+        // 64 / 128 rows: x 128, 40 heads of 128 tokens over 1024, 12 sequences 67 / 93, 50 261 / 268; 32 heads over 8, 512 tokens over 4096, 1
+        // sequence 79 / 72, 16 668 / 568; the same x 64, 8 sequences 177 / 197, 16 345 / 322.  Float: registers leave room for 64.
+        p.qb = !f32 && rows >= 512 && wgs(2) >= (a.dh == 64 ? 2048 : 128) ? 2 : 1;
+        p.slots = T * G / (64 * p.qb) + a.n_seqs;
+        // Parts as for short calls above; float MFMAs are slow enough to pay for them from 128 keys on (8 heads of 100 tokens over 1000: 23 us,
+        // parts of 256 keys 34).
+        p.tile_cut = seen <= (f32 ? 128 : 640) ? whole : cut_keys(wgs(p.qb), seen, 640, f32 ? 128 : 256, CT_ALIGN);
     }
     return p;
 }
@@ -767,11 +962,25 @@ template <typename T, int DH, int QB> static hipError_t launch_tile(const ChunkK
     static LdsLimit limit[MAX_DEVICES];
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) dev = 0;
-    hipError_t e = limit[dev].raise((const void*)chunk_tile_kernel<T, DH, QB>, ct_lds<T, DH>());
+    hipError_t e = limit[dev].raise((const void*)chunk_tile_kernel<T, DH, QB>, ct_lds<T, DH, QB>());
     if (e != hipSuccess) return e;
     const int64_t wgs = p.slots * k.Hkv;
     if (p.slots > 0x7fffffff || wgs * CT_WAVES * 64 * p.tile_cut.parts > MAX_LAUNCH_THREADS) return hipErrorInvalidValue;
-    chunk_tile_kernel<T, DH, QB><<<dim3((unsigned)wgs, p.tile_cut.parts), CT_WAVES * 64, ct_lds<T, DH>(), s>>>(k, (int)p.slots);
+    chunk_tile_kernel<T, DH, QB><<<dim3((unsigned)wgs, p.tile_cut.parts), CT_WAVES * 64, ct_lds<T, DH, QB>(), s>>>(k, (int)p.slots);
+    return hipGetLastError();
+}
+
+template <typename T, int DH, int WAVES> static hipError_t launch_stream(const ChunkKernelArgs& k, const ChunkPlan& p, hipStream_t s)
+{
+    typedef Stream<T, DH, WAVES> S;
+    static LdsLimit limit[MAX_DEVICES];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) dev = 0;
+    hipError_t e = limit[dev].raise((const void*)chunk_stream_kernel<T, DH, WAVES>, S::LDS);
+    if (e != hipSuccess) return e;
+    const int64_t wgs = (int64_t)k.n_seqs * k.Hkv;
+    if (wgs * WAVES * 64 * p.stream_cut.parts > MAX_LAUNCH_THREADS) return hipErrorInvalidValue;
+    chunk_stream_kernel<T, DH, WAVES><<<dim3((unsigned)wgs, p.stream_cut.parts), WAVES * 64, S::LDS, s>>>(k);
     return hipGetLastError();
 }
 
@@ -785,28 +994,21 @@ template <typename T, int DH> static hipError_t launch_chunk(const ChunkAttnArgs
     k.stream_rows = !p.tile ? 0x7fffffff : p.stream ? STREAM_ROWS : 0;
     hipError_t e;
     if (p.stream) {
-        static LdsLimit limit[MAX_DEVICES];
-        int dev = 0;
-        if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) dev = 0;
-        e = limit[dev].raise((const void*)chunk_stream_kernel<T, DH>, Stream<T, DH>::LDS);
+        if constexpr (sizeof(T) == 2 || DH == 64) e = p.waves == 8 ? launch_stream<T, DH, 8>(k, p, s) : launch_stream<T, DH, ST_WAVES>(k, p, s);
+        else e = launch_stream<T, DH, ST_WAVES>(k, p, s);
         if (e != hipSuccess) return e;
-        const int64_t wgs = (int64_t)a.n_seqs * a.Hkv;
-        if (wgs * ST_WAVES * 64 * p.stream_cut.parts > MAX_LAUNCH_THREADS) return hipErrorInvalidValue;
-        chunk_stream_kernel<T, DH><<<dim3((unsigned)wgs, p.stream_cut.parts), ST_WAVES * 64, Stream<T, DH>::LDS, s>>>(k);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (p.tile) {
-        if constexpr (sizeof(T) == 2) {
-            if (p.qb == 4) e = launch_tile<T, DH, 4>(k, p, s);
-        }
-        if (p.qb == 2) e = launch_tile<T, DH, 2>(k, p, s);
-        if (p.qb == 1) e = launch_tile<T, DH, 1>(k, p, s);
+        if constexpr (sizeof(T) == 2) e = p.qb == 2 ? launch_tile<T, DH, 2>(k, p, s) : launch_tile<T, DH, 1>(k, p, s);
+        else e = launch_tile<T, DH, 1>(k, p, s);
         if (e != hipSuccess) return e;
     }
-    if (p.parts() > 1) {
-        const int64_t wgs = ceil_div((int64_t)a.tokens * a.H, 4);
-        if (wgs * 256 > MAX_LAUNCH_THREADS) return hipErrorInvalidValue;
-        chunk_join_kernel<T, DH><<<(unsigned)wgs, 256, 0, s>>>(k);
+    if (p.stream && p.stream_cut.parts > 1) {
+        chunk_join_stream_kernel<T, DH><<<(unsigned)(a.n_seqs * a.Hkv), 256, 0, s>>>(k);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (p.tile && p.tile_cut.parts > 1) {
+        chunk_join_tile_kernel<T, DH><<<dim3((unsigned)(p.slots * a.Hkv), k.tile_rows * DH / 1024), 256, 0, s>>>(k, (int)p.slots);
         e = hipGetLastError();
     }
     return e;

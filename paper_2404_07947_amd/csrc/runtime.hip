@@ -2319,6 +2319,7 @@ static int check_paged(int dtype, int dh, int Hkv, int n_blocks, int max_blocks,
     if (dh != 64 && dh != 128) return fail(EXE_ERR_SHAPE, "head_dim must be 64 or 128");
     if (Hkv < 1 || n_blocks < 1 || max_blocks < 1) return fail(EXE_ERR_ARG, "a cache without heads or blocks");
     if (block_shift_of(block_size) < 0) return fail(EXE_ERR_ARG, "block_size %d is not a power of two in [8, 4096]", block_size);
+    if ((int64_t)2 * Hkv * block_size * dh * (dtype == DT_F32 ? 4 : 2) >= ((int64_t)1 << 32)) return fail(EXE_ERR_SHAPE, "a block of 4 GB or more");
     return EXE_OK;
 }
 static int esz_of_dtype(int dtype) { return dtype == DT_F32 ? 4 : 2; }
@@ -2447,7 +2448,6 @@ extern "C" int exe_op_kv_copy_blocks(void* hip_stream, int32_t dtype, void* kv_b
     if ((uintptr_t)kv_blocks & 15) return fail(EXE_ERR_ARG, "the cache must be 16-byte aligned");
     const int row_bytes = dh * esz_of_dtype(dtype);
     if (n_copies > n_blocks) return fail(EXE_ERR_ARG, "%d copies into %d blocks write one twice", n_copies, n_blocks);
-    if ((int64_t)2 * Hkv * block_size * row_bytes >= ((int64_t)1 << 32)) return fail(EXE_ERR_SHAPE, "a block of 4 GB or more");
     std::vector<BlockCopy> list(n_copies);
     std::vector<int32_t> to(n_copies);
     for (int i = 0; i < n_copies; ++i) {
