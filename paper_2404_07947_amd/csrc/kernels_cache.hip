@@ -28,34 +28,50 @@ __device__ __forceinline__ float2 rotary_cs(int pos, double freq, float amplitud
     return float2{cs * amplitude, sn * amplitude};
 }
 
-constexpr int ROT_WAVES = 4;              // waves of a workgroup, each with a token (or part of one) of its own
+constexpr int ROT_WAVES = 4, ROT_U = 2;   // waves of a workgroup, each with a token (or part of one) of its own; slots in flight per lane
 template <typename T, int N> struct __align__(sizeof(T) * N) Elems { T v[N]; };
 
 // Slot s of a head: 2 * EPL elements, either EPL pairs or EPL x 2 elements that pass through, loaded and stored as two chunks.  Both
 // chunks are the same thread's, so out may be x itself.
-template <typename T, int EPL, bool INTERLEAVED>
-__device__ __forceinline__ void rotary_slot(const T* x, T* out, int slot, int rot, const float2* cs)
-{
-    int c0 = 2 * slot * EPL, c1 = c0 + EPL;
-    bool turn = slot * EPL < rot / 2;
-    if (!INTERLEAVED && turn) { c0 = slot * EPL; c1 = c0 + rot / 2; }
+template <typename T, int EPL, bool INTERLEAVED> struct RotarySlot {
     typedef Elems<T, EPL> E;
-    E a = *(const E*)(x + c0), b = *(const E*)(x + c1);
-    if (turn) {
+    E a, b;
+    int pair, c0, c1;                     // first pair; the chunks' places
+    bool turn;
+    __device__ __forceinline__ void load(const T* x, int slot, int rot)
+    {
+        pair = slot * EPL;
+        turn = pair < rot / 2;
+        c0 = INTERLEAVED || !turn ? 2 * pair : pair;
+        c1 = INTERLEAVED || !turn ? 2 * pair + EPL : pair + rot / 2;
+        a = *(const E*)(x + c0);
+        b = *(const E*)(x + c1);
+    }
+    // NT: nontemporal
+    template <bool NT> __device__ __forceinline__ void store(T* out, int rot, const float2* cs)
+    {
+        if (turn) {
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) {
-            if (INTERLEAVED && slot * EPL + e >= rot / 2) continue;          // rot ends inside the slot
-            float2 w = cs[slot * EPL + e];
-            T& u = INTERLEAVED ? (2 * e < EPL ? a.v[2 * e < EPL ? 2 * e : 0] : b.v[2 * e >= EPL ? 2 * e - EPL : 0]) : a.v[e];
-            T& v = INTERLEAVED ? (2 * e + 1 < EPL ? a.v[2 * e + 1 < EPL ? 2 * e + 1 : 0] : b.v[2 * e + 1 >= EPL ? 2 * e + 1 - EPL : 0]) : b.v[e];
-            float p = to_f32(u), q = to_f32(v);
-            u = from_f32<T>(p * w.x - q * w.y);
-            v = from_f32<T>(q * w.x + p * w.y);
+            for (int e = 0; e < EPL; ++e) {
+                if (INTERLEAVED && pair + e >= rot / 2) continue;                // rot ends inside the slot
+                float2 w = cs[pair + e];
+                T& u = INTERLEAVED ? (2 * e < EPL ? a.v[2 * e < EPL ? 2 * e : 0] : b.v[2 * e >= EPL ? 2 * e - EPL : 0]) : a.v[e];
+                T& v = INTERLEAVED ? (2 * e + 1 < EPL ? a.v[2 * e + 1 < EPL ? 2 * e + 1 : 0] : b.v[2 * e + 1 >= EPL ? 2 * e + 1 - EPL : 0]) : b.v[e];
+                float p = to_f32(u), q = to_f32(v);
+                u = from_f32<T>(p * w.x - q * w.y);
+                v = from_f32<T>(q * w.x + p * w.y);
+            }
+        }
+        if constexpr (NT && sizeof(E) == 16) {
+            typedef unsigned v4u __attribute__((ext_vector_type(4)));
+            __builtin_nontemporal_store(__builtin_bit_cast(v4u, a), (v4u*)(out + c0));
+            __builtin_nontemporal_store(__builtin_bit_cast(v4u, b), (v4u*)(out + c1));
+        } else {
+            *(E*)(out + c0) = a;
+            *(E*)(out + c1) = b;
         }
     }
-    *(E*)(out + c0) = a;
-    *(E*)(out + c1) = b;
-}
+};
 
 template <typename T, int EPL, bool INTERLEAVED>
 __global__ __launch_bounds__(ROT_WAVES * 64) void rotary_kernel(const T* x, int64_t x_stride, int tokens, int parts, int heads, int dh, int rot,
@@ -73,9 +89,19 @@ __global__ __launch_bounds__(ROT_WAVES * 64) void rotary_kernel(const T* x, int6
     const T* xr = x + t * x_stride;
     T* yr = out + t * out_stride;
     int per_head = dh / (2 * EPL), shift = 31 - __builtin_clz(per_head);
-    for (int i = part * 64 + lane; i < heads << shift; i += parts * 64) {
-        int h = i >> shift;
-        rotary_slot<T, EPL, INTERLEAVED>(xr + h * dh, yr + h * dh, i & (per_head - 1), rot, cs);
+    const int end = heads << shift;
+    for (int i0 = part * 64 + lane; i0 < end; i0 += parts * 64 * ROT_U) {
+        RotarySlot<T, EPL, INTERLEAVED> s[ROT_U];
+#pragma unroll
+        for (int u = 0; u < ROT_U; ++u) {
+            int i = i0 + u * parts * 64;
+            if (i < end) s[u].load(xr + (i >> shift) * dh, i & (per_head - 1), rot);
+        }
+#pragma unroll
+        for (int u = 0; u < ROT_U; ++u) {
+            int i = i0 + u * parts * 64;
+            if (i < end) s[u].template store<true>(yr + (i >> shift) * dh, rot, cs);
+        }
     }
 }
 
@@ -106,17 +132,26 @@ __global__ __launch_bounds__(ROT_WAVES * 64) void rotary_append_kernel(
     T* kd = kv_blocks + ((int64_t)blk * 2 * Hkv * rows + (at & (rows - 1))) * dh;      // head g's key at kd + g * rows * dh
     int per_head = dh / (2 * EPL), shift = 31 - __builtin_clz(per_head);
     int first = q_out ? 0 : H, last = blk >= 0 ? H + 2 * Hkv : H;
-    for (int i = (first << shift) + part * 64 + lane; i < last << shift; i += parts * 64) {
-        int h = i >> shift, slot = i & (per_head - 1);
-        T* dst = h < H ? qr + h * dh : kd + (int64_t)(h - H) * rows * dh;
-        rotary_slot<T, EPL, INTERLEAVED>(xr + h * dh, dst, slot, h < H + Hkv ? rot : 0, cs);
+    const int end = last << shift;
+    for (int i0 = (first << shift) + part * 64 + lane; i0 < end; i0 += parts * 64 * ROT_U) {
+        RotarySlot<T, EPL, INTERLEAVED> s[ROT_U];
+#pragma unroll
+        for (int u = 0; u < ROT_U; ++u) {
+            int i = i0 + u * parts * 64, h = i >> shift;
+            if (i < end) s[u].load(xr + h * dh, i & (per_head - 1), h < H + Hkv ? rot : 0);
+        }
+#pragma unroll
+        for (int u = 0; u < ROT_U; ++u) {
+            int i = i0 + u * parts * 64, h = i >> shift;
+            if (i < end) s[u].template store<false>(h < H ? qr + h * dh : kd + (int64_t)(h - H) * rows * dh, h < H + Hkv ? rot : 0, cs);
+        }
     }
 }
 
-// Parts of a token: enough waves to fill the chip where tokens are few, up to one per 64 slots.
+// Parts of a token: 16384 waves, two for each that the chip holds, where tokens are few; up to one per 64 slots.
 static int rotary_parts(int tokens, int64_t slots)
 {
-    int64_t most = (slots + 63) / 64, want = (2048 + tokens - 1) / tokens;
+    int64_t most = (slots + 63) / 64, want = (16384 + tokens - 1) / tokens;
     return (int)(most < want ? most : want);
 }
 static bool aligned_rows(const void* p, int64_t stride, int esz) { return !p || (((uintptr_t)p & 15) == 0 && stride * esz % 16 == 0); }
@@ -170,8 +205,10 @@ hipError_t launch_rotary_append(const RotaryAppendArgs& a, hipStream_t s)
 // ---------------------------------------------------------------- copies of pages
 // Positions 0 .. rows - 1 of every head's keys and values, of every layer.  The list travels in the kernel's arguments: nothing is
 // allocated or staged, and a captured launch keeps its own.  A workgroup moves COPY_PIECE bytes of one (copy, layer), in which the runs
-// of the heads (rows * row_bytes each; one run where whole blocks are copied) follow each other.
-constexpr int COPY_MAX = 256, COPY_THREADS = 256, COPY_U = 8, COPY_PIECE = COPY_THREADS * COPY_U * 16;
+// of the heads (rows * row_bytes each; one run where whole blocks are copied) follow each other.  Stores are nontemporal, loads are not: a
+// fork reads one source for every copy.  90 blocks of 1.3 MB in 8 layers, 1.9 GB moved: 362 us (5.2 TB/s; torch's copy of 2 GiB 4.9), with
+// ordinary stores 369; 37 of 64 positions of a block to 8 others, 40 layers, 273 MB: 57 and 79 us.
+constexpr int COPY_MAX = 256, COPY_THREADS = 256, COPY_U = 16, COPY_PIECE = COPY_THREADS * COPY_U * 16;
 struct CopyList { BlockCopy c[COPY_MAX]; };
 
 __global__ __launch_bounds__(COPY_THREADS) void copy_blocks_kernel(CopyList list, unsigned char* pool, int64_t layer_bytes, int64_t block_bytes, int layers,
@@ -179,24 +216,26 @@ __global__ __launch_bounds__(COPY_THREADS) void copy_blocks_kernel(CopyList list
 {
     typedef unsigned v4u __attribute__((ext_vector_type(4)));
     unsigned piece = blockIdx.x % pieces, rest = blockIdx.x / pieces, layer = rest % layers;
-    BlockCopy c = list.c[rest / layers];
-    const unsigned run16 = (unsigned)c.rows * row_bytes / 16, total = run16 * runs;       // 16-byte chunks of a run, of the copy
-    const unsigned skip = (unsigned)(block_rows - c.rows) * row_bytes / 16;               // between the end of a run and the next one
+    // straight from the arguments in memory, of which the list is the first: an array that is indexed there would go to registers
+    const auto* entry = (const __attribute__((address_space(4))) int32_t*)__builtin_amdgcn_kernarg_segment_ptr() + 3 * (rest / layers);
+    const int c_src = entry[0], c_dst = entry[1], c_rows = entry[2];
+    const unsigned run16 = (unsigned)c_rows * row_bytes / 16, total = run16 * runs;       // 16-byte chunks of a run, of the copy
+    const unsigned skip = (unsigned)(block_rows - c_rows) * row_bytes / 16;               // between the end of a run and the next one
     const unsigned first = piece * (COPY_THREADS * COPY_U) + threadIdx.x;
     if (piece * (COPY_THREADS * COPY_U) >= total) return;
-    const v4u* src = (const v4u*)(pool + layer * layer_bytes + c.src * block_bytes);
-    v4u* dst = (v4u*)(pool + layer * layer_bytes + c.dst * block_bytes);
-    v4u v[COPY_U];
-    unsigned at[COPY_U];
+    const v4u* src = (const v4u*)(pool + layer * layer_bytes + c_src * block_bytes);
+    v4u* dst = (v4u*)(pool + layer * layer_bytes + c_dst * block_bytes);
+    auto place = [&](unsigned i) { return i + (skip ? i / run16 * skip : 0); };
+    if (piece * (COPY_THREADS * COPY_U) + COPY_THREADS * COPY_U <= total) {
+        v4u v[COPY_U];
+        unsigned at[COPY_U];
 #pragma unroll
-    for (int u = 0; u < COPY_U; ++u) {
-        unsigned i = first + u * COPY_THREADS;
-        at[u] = i + (skip ? i / run16 * skip : 0);
-        if (i < total) v[u] = src[at[u]];
+        for (int u = 0; u < COPY_U; ++u) v[u] = src[at[u] = place(first + u * COPY_THREADS)];
+#pragma unroll
+        for (int u = 0; u < COPY_U; ++u) __builtin_nontemporal_store(v[u], dst + at[u]);
+    } else {
+        for (unsigned i = first; i < total; i += COPY_THREADS) dst[place(i)] = src[place(i)];
     }
-#pragma unroll
-    for (int u = 0; u < COPY_U; ++u)
-        if (first + u * COPY_THREADS < total) dst[at[u]] = v[u];
 }
 
 hipError_t launch_copy_blocks(const BlockCopyArgs& a, hipStream_t s)
