@@ -504,6 +504,8 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
     const bool active = w0 < rows;
     const int p_min = p0 + w0 / G, p_max = p0 + wl / G;
     const int n_tiles = k.last > k.first ? (k.last - k.first + KT - 1) / KT : 0;
+    // of these, the leading ones that hold a key which a row of this wave sees; in the others it only moves its share
+    const int mine = active ? keys_of(p_max, a.window, limit).last - k.first : 0, n_mine = mine <= 0 ? 0 : (mine + KT - 1) / KT < n_tiles ? (mine + KT - 1) / KT : n_tiles;
 
     u32x4 qf[QB][DS];
     KeyRange sees[QB];
@@ -693,28 +695,32 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
         wait_loads<0>();
         __syncthreads();
         bring(0);
-        if (active) {
+        if (n_mine > 0) {
             scores(0, s[0]);
             largest(s[0], mx);
             look(0, s[0], mx);
         }
-        auto iteration = [&](int kt, Scores& now, Scores& next) {
+        auto arrive = [&](int kt) {
             wait_loads<0>();                                           // values of tile kt, keys of kt + 1
             __syncthreads();
-            bring(kt + 1);
-            if (!active) return;
-            scores(kt + 1, next);
+            if (kt + 1 < n_tiles) bring(kt + 1);
+        };
+        auto iteration = [&](int kt, Scores& now, Scores& next) {
+            arrive(kt);
             exponentials(now);
+            __builtin_amdgcn_s_setprio(1);                             // MFMAs go before another wave's softmax
+            scores(kt + 1, next);
             values(kt, now);
+            __builtin_amdgcn_s_setprio(0);
             largest(next, mx);
             look(kt + 1, next, mx);
         };
         int kt = 0;
-        for (; kt + 2 < n_tiles; kt += 2) {
+        for (; kt + 2 < n_mine; kt += 2) {
             iteration(kt, s[0], s[1]);
             iteration(kt + 1, s[1], s[0]);
         }
-        if (kt + 1 < n_tiles) {
+        if (kt + 1 < n_mine) {
             iteration(kt, s[0], s[1]);
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb)
@@ -722,12 +728,13 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
                 for (int kb = 0; kb < KB; ++kb) s[0][qb][kb] = s[1][qb][kb];
             ++kt;
         }
-        wait_loads<0>();
-        __syncthreads();
-        if (active) {
+        if (kt < n_mine) {
+            arrive(kt);
             exponentials(s[0]);
             values(kt, s[0]);
+            ++kt;
         }
+        for (; kt < n_tiles; ++kt) arrive(kt);
     }
     if (!active) return;
 

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from chunk_util import DEV, Batch, check
+from chunk_util import DEV, HALF, U, Batch, check
 
 pytestmark = pytest.mark.gpu
 
@@ -26,6 +26,47 @@ def test_lengths(dtype, dh, lengths):
     for i, (H, Hkv) in enumerate([(4, 4), (8, 2)]):
         b = Batch(LENGTHS[lengths], H, Hkv, dh, (16, 64)[i], dtype, seed=i, extra_rows=3).fill().device()
         check(b.attend(), *b.want(), (H, Hkv))
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("bf16", 64), ("f32", 64), ("f32", 128)])
+def test_single_tokens_beside_chunks(dtype, dh):
+    """Many single tokens and one longer chunk (both kernels in one call, long ones in parts), and few single tokens among chunks (one)."""
+    for seqs in ([(1, 1000 + 90 * i) for i in range(9)] + [(40, 900), (1, 3)], [(1, 5000), (30, 40), (1, 4500)], [(100, 300), (1, 800), (70, 70), (2, 2)]):
+        b = Batch(seqs, 4, 2, dh, 16, dtype, seed=len(seqs), extra_rows=1).fill().device()
+        check(b.attend(), *b.want(), seqs)
+
+
+@pytest.mark.parametrize("G,n,L,Hkv", [(8, 128, 400, 8), (8, 64, 300, 2), (1, 600, 600, 3), (4, 300, 1500, 1)])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_tiles_that_share_their_keys(G, n, L, Hkv, dh):
+    """Tiles of 64 and of 128 rows, with and without a window, a second sequence that ends inside a tile."""
+    for window in (0, 100):
+        b = Batch([(n, L), (n // 2 + 1, n)], G * Hkv, Hkv, dh, 16, "bf16", seed=G).fill().device()
+        check(b.attend(window=window), *b.want(window=window), window)
+
+
+@pytest.mark.parametrize("dh,H,Hkv,n,L", [(64, 512, 64, 512, 520), (128, 64, 8, 300, 700), (128, 32, 8, 1100, 2300)])
+@pytest.mark.parametrize("window", [0, 130])
+def test_full_chips(dh, H, Hkv, n, L, window):
+    """Launches that fill the chip with tiles of 128 rows; the reference is computed on the device, in 64 bits and 4 heads at a time."""
+    b = Batch([(n, L)], H, Hkv, dh, 32, "bf16").fill().device()
+    got = b.attend(window=window).double().view(n, H, dh)
+    key, pos = torch.arange(L, device=DEV)[None], torch.arange(L - n, L, device=DEV)[:, None]
+    seen = (key <= pos) & ((key > pos - window) if window else True)
+    count = seen.sum(1).double()[:, None, None]
+    for h in range(0, H, 4):
+        kv = [h // (H // Hkv), (h + 3) // (H // Hkv) + 1]
+        rep = 4 // (kv[1] - kv[0])
+        k, v = (t[0][kv[0]:kv[1]].to(DEV).double().repeat_interleave(rep, 0) for t in (b.k, b.v))
+        q = b.d_q.double().view(n, H, dh)[:, h:h + 4].transpose(0, 1).contiguous()
+        s = torch.matmul(q, k.transpose(1, 2).contiguous()) * b.scale
+        mag = (torch.matmul(q.abs(), k.abs().transpose(1, 2).contiguous()) * b.scale).masked_fill(~seen, 0).amax(-1)
+        top = s.abs().masked_fill(~seen, 0).amax(-1)
+        p = torch.softmax(s.masked_fill(~seen, -float("inf")), -1)
+        want = torch.matmul(p, v).transpose(0, 1)
+        e = (2 * (dh + 8) * U * mag + 8 * U * (1 + top)).t()[..., None] + (count + 16) * 2 * U + HALF["bf16"]
+        tol = e * torch.matmul(p, v.abs()).transpose(0, 1) + HALF["bf16"] * want.abs() + 1e-30         # as Batch.want has it
+        assert bool(((got[:, h:h + 4] - want).abs() <= tol * (1 + 1e-6)).all()), h
 
 
 @pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("f32", 64)])
