@@ -208,42 +208,53 @@ def _dev(t) -> Optional[int]:
     return t.data_ptr()
 
 
-_raw_stream = None                               # torch's own look-up of a device's current stream, without the objects
+_torch = _raw_stream = None                      # set by _current, so that importing this module does not import torch
 
 
 def _current():
     """(current device, its current stream's address)."""
-    global _raw_stream
-    import torch
-    if _raw_stream is None:
+    global _torch, _raw_stream
+    if _torch is None:
+        import torch
         torch.cuda.init()
+        # torch's own look-up, without the objects
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
-    dev = torch.cuda.current_device()
+        _torch = torch
+    dev = _torch.cuda.current_device()
     return dev, _raw_stream(dev) or None
 
 
-def _typed(t, name: str, n: int) -> Optional[int]:
-    """_dev for an array that holds n elements of `name` (a torch type); of another type they would be misread."""
+def _array(t, dev: int, kind: str, n: int) -> Optional[int]:
+    """Device pointer of a contiguous array of n elements of `kind` (a torch type; of another one they would be misread)."""
     if t is None or isinstance(t, int):
         return t
-    assert str(t.dtype) == "torch." + name, f"expected {name}, got {t.dtype}"
-    assert t.numel() >= n, f"expected {n} elements, got {t.numel()}"
-    return _dev(t)
+    assert t.get_device() == dev, "expected a tensor on the current device"
+    assert t.dtype is getattr(_torch, kind), f"expected {kind}, got {t.dtype}"
+    assert t.numel() >= n and t.is_contiguous(), f"expected {n} elements that follow each other, got {t.numel()}"
+    return t.data_ptr()
 
 
-_ROW_TYPES = ("torch.float32", "torch.bfloat16")
-
-
-def _rows(t, dtype: int, rows: int, width: int, stride: int) -> Optional[int]:
+def _rows(t, dev: int, dtype: int, rows: int, width: int, stride: int) -> Optional[int]:
     """Device pointer of a tensor of the storage type that holds rows of `width` elements, `stride` apart from its first element on; it
     need not be contiguous.  It lies on the current device, on whose stream the operation is enqueued."""
     if t is None or isinstance(t, int):
         return t
-    assert t.is_cuda and t.get_device() == _current()[0], "expected a tensor on the current device"
-    assert str(t.dtype) == _ROW_TYPES[dtype], f"expected the type {dtype}, got {t.dtype}"
+    assert t.get_device() == dev, "expected a tensor on the current device"
+    assert t.dtype is (_torch.bfloat16 if dtype else _torch.float32), f"expected the type {dtype}, got {t.dtype}"
     need = (rows - 1) * stride + width if rows > 0 else 0
     assert need <= t.numel() or need <= t.untyped_storage().nbytes() // t.element_size() - t.storage_offset(), f"expected {need} elements"
     return t.data_ptr()
+
+
+def _where(stream):
+    """(current device, stream's address); without a GPU or with addresses only, torch is not asked."""
+    if stream is None or _torch is not None:
+        dev, current = _current()
+        return dev, current if stream is None else _stream_ptr(stream)
+    try:
+        return _current()[0], _stream_ptr(stream)
+    except (RuntimeError, AssertionError):
+        return None, _stream_ptr(stream)
 
 
 def _stream_ptr(stream) -> Optional[int]:
@@ -525,20 +536,22 @@ def exe_rotary_frequencies(rot: int, base: float = 10000.0, scaling: int = ROPE_
 
 def exe_op_rotary(dtype, T, x, x_stride, heads, dh, rot, interleaved, pos, inv_freq, amplitude, out, out_stride, stream=None):
     """x and out: device tensors (or addresses) whose rows are x_stride / out_stride elements apart."""
-    _check(lib().exe_op_rotary(_stream_ptr(stream), dtype, T, _rows(x, dtype, T, heads * dh, x_stride), x_stride, heads, dh, rot, interleaved,
-                               _typed(pos, "int32", T), _typed(inv_freq, "float64", rot // 2), amplitude,
-                               _rows(out, dtype, T, heads * dh, out_stride), out_stride))
+    dev, s = _where(stream)
+    _check(lib().exe_op_rotary(s, dtype, T, _rows(x, dev, dtype, T, heads * dh, x_stride), x_stride, heads, dh, rot, interleaved,
+                               _array(pos, dev, "int32", T), _array(inv_freq, dev, "float64", rot // 2), amplitude,
+                               _rows(out, dev, dtype, T, heads * dh, out_stride), out_stride))
 
 
 def exe_op_rotary_append_paged(dtype, n_seqs, cu_seqlens, T, qkv, row_stride, H, Hkv, dh, rot, interleaved, pos, inv_freq, amplitude, kv_blocks,
                                n_blocks, block_table, max_blocks, block_size, length, q_out, q_out_stride, stream=None):
+    dev, s = _where(stream)
     block = 2 * Hkv * block_size * dh
-    _check(lib().exe_op_rotary_append_paged(_stream_ptr(stream), dtype, n_seqs, _typed(cu_seqlens, "int32", n_seqs + 1), T,
-                                            _rows(qkv, dtype, T, (H + 2 * Hkv) * dh, row_stride), row_stride, H, Hkv, dh, rot, interleaved,
-                                            _typed(pos, "int32", T), _typed(inv_freq, "float64", rot // 2), amplitude,
-                                            _rows(kv_blocks, dtype, n_blocks, block, block), n_blocks,
-                                            _typed(block_table, "int32", n_seqs * max_blocks), max_blocks, block_size,
-                                            _typed(length, "int32", n_seqs), _rows(q_out, dtype, T, H * dh, q_out_stride), q_out_stride))
+    _check(lib().exe_op_rotary_append_paged(s, dtype, n_seqs, _array(cu_seqlens, dev, "int32", n_seqs + 1), T,
+                                            _rows(qkv, dev, dtype, T, (H + 2 * Hkv) * dh, row_stride), row_stride, H, Hkv, dh, rot, interleaved,
+                                            _array(pos, dev, "int32", T), _array(inv_freq, dev, "float64", rot // 2), amplitude,
+                                            _rows(kv_blocks, dev, dtype, n_blocks, block, block), n_blocks,
+                                            _array(block_table, dev, "int32", n_seqs * max_blocks), max_blocks, block_size,
+                                            _array(length, dev, "int32", n_seqs), _rows(q_out, dev, dtype, T, H * dh, q_out_stride), q_out_stride))
 
 
 def exe_op_chunk_attention_paged_workspace(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window=0) -> int:
@@ -547,20 +560,23 @@ def exe_op_chunk_attention_paged_workspace(dtype, n_seqs, T, max_new, max_len, H
 
 def exe_op_chunk_attention_paged(dtype, n_seqs, cu_seqlens, T, max_new, q, q_stride, kv_blocks, n_blocks, block_table, max_blocks, block_size,
                                  length, max_len, H, Hkv, dh, scale, window, out, out_stride, workspace=None, stream=None):
+    dev, s = _where(stream)
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     block = 2 * Hkv * block_size * dh
-    _check(lib().exe_op_chunk_attention_paged(_stream_ptr(stream), dtype, n_seqs, _typed(cu_seqlens, "int32", n_seqs + 1), T, max_new,
-                                              _rows(q, dtype, T, H * dh, q_stride), q_stride, _rows(kv_blocks, dtype, n_blocks, block, block), n_blocks,
-                                              _typed(block_table, "int32", n_seqs * max_blocks), max_blocks, block_size,
-                                              _typed(length, "int32", n_seqs), max_len, H, Hkv, dh, scale, window,
-                                              _rows(out, dtype, T, H * dh, out_stride), out_stride, _dev(workspace), ws_bytes))
+    _check(lib().exe_op_chunk_attention_paged(s, dtype, n_seqs, _array(cu_seqlens, dev, "int32", n_seqs + 1), T, max_new,
+                                              _rows(q, dev, dtype, T, H * dh, q_stride), q_stride,
+                                              _rows(kv_blocks, dev, dtype, n_blocks, block, block), n_blocks,
+                                              _array(block_table, dev, "int32", n_seqs * max_blocks), max_blocks, block_size,
+                                              _array(length, dev, "int32", n_seqs), max_len, H, Hkv, dh, scale, window,
+                                              _rows(out, dev, dtype, T, H * dh, out_stride), out_stride, _dev(workspace), ws_bytes))
 
 
 def exe_op_kv_copy_blocks(dtype, kv_blocks, n_layers, n_blocks, block_size, Hkv, dh, copies, stream=None):
     """copies: (source, destination, leading positions) of every copy, on the host."""
+    dev, s = _where(stream)
     c = np.ascontiguousarray(copies, dtype=np.int32).reshape(-1, 3)
     block = 2 * Hkv * block_size * dh
-    _check(lib().exe_op_kv_copy_blocks(_stream_ptr(stream), dtype, _rows(kv_blocks, dtype, n_layers * n_blocks, block, block), n_layers, n_blocks,
+    _check(lib().exe_op_kv_copy_blocks(s, dtype, _rows(kv_blocks, dev, dtype, n_layers * n_blocks, block, block), n_layers, n_blocks,
                                        block_size, Hkv, dh, len(c), _ip(c)))
 
 

@@ -112,3 +112,17 @@ def test_frequency_refusals(kw):
         exe.exe_rotary_frequencies(**kw)
     assert e.value.code == -1
     assert exe.lib().exe_rotary_frequencies(64, C.c_double(1e4), 0, C.c_double(1), 0, C.c_double(1), C.c_double(2), None, None) == -1
+
+
+def test_tensors_of_the_host_are_refused():
+    torch = pytest.importorskip("torch")
+    x = torch.zeros((4, 256), dtype=torch.bfloat16)
+    f = torch.zeros(32, dtype=torch.float64)
+    pos = torch.zeros(4, dtype=torch.int32)
+    for change in (dict(x=x), dict(out=x), dict(pos=pos), dict(inv_freq=f)):
+        with pytest.raises(AssertionError):
+            exe.exe_op_rotary(*{**ROTARY, **change}.values(), stream=1)
+    with pytest.raises(AssertionError):
+        exe.exe_op_kv_copy_blocks(*{**COPY, "pool": x}.values(), stream=1)
+    with pytest.raises(AssertionError):
+        exe.exe_op_chunk_attention_paged(*{**ATTEND, "table": pos}.values(), stream=1)

@@ -179,3 +179,14 @@ def test_positions_without_a_block_are_not_stored(entry):
             changed[int(b.table[0, p // 16]), p % 16] = True
     same = ((b.d_pool == before) | (b.d_pool.isnan() & before.isnan())).all(-1).all(1).all(1).cpu()
     assert torch.equal(~same, changed)
+
+
+def test_tensors_that_would_be_misread_are_refused():
+    x = torch.zeros((4, 256), dtype=torch.bfloat16, device=DEV)
+    pos, f = torch.zeros(4, dtype=torch.int32, device=DEV), torch.zeros(32, dtype=torch.float64, device=DEV)
+    good = dict(dtype=1, T=4, x=x, x_stride=256, heads=4, dh=64, rot=64, interleaved=0, pos=pos, inv_freq=f, amplitude=1.0, out=x, out_stride=256)
+    exe.exe_op_rotary(**good)
+    for change in (dict(x=x.float(), out=x.float()), dict(dtype=0), dict(pos=pos.long()), dict(inv_freq=f.float()), dict(pos=pos[:3]), dict(inv_freq=f[:31]), dict(T=5, pos=torch.zeros(5, dtype=torch.int32, device=DEV)),
+                   dict(x=x[:, 1:]), dict(pos=torch.zeros(8, dtype=torch.int32, device=DEV)[::2]), dict(x=x.cpu()), dict(pos=pos.cpu())):
+        with pytest.raises(AssertionError):
+            exe.exe_op_rotary(**{**good, **change})
