@@ -387,7 +387,7 @@ int exe_op_decode_attention(void* hip_stream, int32_t dtype, int32_t B, const vo
  * key / value rows of (b, head) are read from q + b*q_stride + new_kv_offset + head*dh and
  * q + b*q_stride + 2*new_kv_offset + head*dh and stored into the cache by this call (q then is the packed output of
  * the QKV projection).  The caller guarantees that every table entry a sequence needs names a block inside the pool
- * and that no block is shared between sequences. */
+ * and that no sequence holds the block of another one's newest position (sequences may share full blocks). */
 int exe_op_decode_attention_paged(void* hip_stream, int32_t dtype, int32_t B, const void* q, int32_t q_stride,
                                   const void* kv_blocks, const int32_t* block_table, int32_t max_blocks,
                                   int32_t block_size, const int32_t* len, const int32_t* qpos, int32_t H, int32_t dh,

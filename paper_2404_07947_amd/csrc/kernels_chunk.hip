@@ -26,7 +26,7 @@ __device__ __forceinline__ KeyRange keys_of(int p, int window, int limit)
 __device__ __forceinline__ int table_limit(const PagedTable& t)
 {
     int64_t n = (int64_t)t.max_blocks << t.shift;
-    return n < 0x7fffff00 ? (int)n : 0x7fffff00;
+    return n < 0x7ffff000 ? (int)n : 0x7ffff000;
 }
 
 // One query row by one wave over keys first .. last - 1, 64 at a time: a lane takes a key for the scores, and features lane, lane + 64
@@ -78,11 +78,16 @@ struct ChunkKernelArgs {
     int window;
     void* out; int64_t out_stride;
     // Keys go to workgroups in parts: `keys` of them each, at most `parts` (the last takes what is left), for the streaming and for the
-    // tile kernel.  Part i of row (t, h) lies at acc[(i * tokens + t) * H + h][DH], ml[(i * tokens + t) * H + h][maximum, sum].
-    struct Cut { int parts, keys; } stream, tile;
+    // tile kernel.  What part i makes of row r lies at acc[i * rows + r][DH], ml[i * rows + r][maximum, sum].
+    struct Cut { int parts, keys; int64_t rows; float *acc, *ml; } stream, tile;
     int stream_rows;          // sequences of up to so many rows are the streaming kernel's, the others the tile kernel's
     int tile_rows;            // rows of a tile of the tile kernel
-    float *acc, *ml;
+    __device__ __forceinline__ int64_t row(int t, int h) const { return (int64_t)t * H + h; }
+    // of the streaming kernel's: beside the tile kernel, where its sequences have few of the tokens, 16 for each
+    __device__ __forceinline__ int64_t stream_row(int b, int kvh, int r, int t, int h) const
+    {
+        return stream_rows == 16 ? ((int64_t)b * Hkv + kvh) * 16 + r : row(t, h);
+    }
 };
 
 // Row (t, h) of sequence b, by one wave (see chunk_row)
@@ -93,7 +98,7 @@ template <typename T, int DH> __device__ __forceinline__ void row_again(const Ch
                      a.scale * LOG2E, lane, (T*)a.out + (int64_t)t * a.out_stride + h * DH);
 }
 
-constexpr int STREAM_ROWS = 16, MAX_PARTS = 64;
+constexpr int STREAM_ROWS = 16, MAX_PARTS = WAVE;
 // Keys that the rows r0 .. r1 - 1 of a sequence see, the first one rounded down to a multiple of `align`; first >= last: none.
 // p0: position of the first new token.
 __device__ __forceinline__ KeyRange tile_keys(int p0, int G, int r0, int r1, int window, int limit, int align)
@@ -101,13 +106,13 @@ __device__ __forceinline__ KeyRange tile_keys(int p0, int G, int r0, int r1, int
     KeyRange a = keys_of(p0 + r0 / G, window, limit), b = keys_of(p0 + (r1 - 1) / G, window, limit);
     return KeyRange{a.first & -align, b.last};
 }
-__device__ __forceinline__ int parts_of(KeyRange k, ChunkKernelArgs::Cut cut)
+__device__ __forceinline__ int parts_of(KeyRange k, const ChunkKernelArgs::Cut& cut)
 {
     if (k.last <= k.first) return 1;
     int n = (int)(((int64_t)k.last - k.first + cut.keys - 1) / cut.keys);
     return n < cut.parts ? n : cut.parts;
 }
-__device__ __forceinline__ KeyRange part_of(KeyRange k, ChunkKernelArgs::Cut cut, int part, int parts)
+__device__ __forceinline__ KeyRange part_of(KeyRange k, const ChunkKernelArgs::Cut& cut, int part, int parts)
 {
     int first = k.first + part * cut.keys;
     return KeyRange{first, part + 1 < parts ? first + cut.keys : k.last};
@@ -407,10 +412,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_stream_kernel(ChunkKernel
         }
         if (parts > 1) {
             if (write) {
-                const int64_t at = ((int64_t)part * a.tokens + wt) * a.H + h;
+                const int64_t at = part * a.stream.rows + a.stream_row(b, kvh, r0 + r, wt, h);
 #pragma unroll
-                for (int f = 0; f < DH / 64; ++f) *(f32x4*)(a.acc + at * DH + f * 64 + 4 * c) = v[f];
-                if (c == 0) *(float2*)(a.ml + at * 2) = float2{M, L};
+                for (int f = 0; f < DH / 64; ++f) *(f32x4*)(a.stream.acc + at * DH + f * 64 + 4 * c) = v[f];
+                if (c == 0) *(float2*)(a.stream.ml + at * 2) = float2{M, L};
             }
         } else {
             const KeyRange ks = keys_of(p0 + wtok, a.window, limit);
@@ -746,10 +751,10 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
         const float sum = rows_sum(l[qb]);
         if (parts > 1) {
             if (!write) continue;
-            const int64_t at = ((int64_t)part * a.tokens + t) * a.H + h;
+            const int64_t at = part * a.tile.rows + a.row(t, h);
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) *(f32x4*)(a.acc + at * DH + dt * 16 + 4 * g) = o[qb][dt];
-            if (g == 0) *(float2*)(a.ml + at * 2) = float2{m[qb], sum};
+            for (int dt = 0; dt < DT; ++dt) *(f32x4*)(a.tile.acc + at * DH + dt * 16 + 4 * g) = o[qb][dt];
+            if (g == 0) *(float2*)(a.tile.ml + at * 2) = float2{m[qb], sum};
             continue;
         }
         const bool any = sees[qb].last > sees[qb].first;
@@ -784,40 +789,8 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
 }
 
 // ---------------------------------------------------------------- parts of the keys, joined
-// Row (t, h) of sequence b at position p, by one wave: sum over the parts of 2^(m_i - M) times their sums, in the order of the parts.
-template <typename T, int DH> __device__ __forceinline__ void join_row(const ChunkKernelArgs& a, int b, int t, int h, int p, int parts, int lane)
-{
-    const int64_t at = (int64_t)t * a.H + h, step = (int64_t)a.tokens * a.H;
-    float M = -INFINITY;
-    for (int i = lane; i < parts; i += 64) M = fmaxf(M, a.ml[(at + i * step) * 2]);
-    M = wave_max(M);
-    const float ref = M == -INFINITY ? 0.f : M;
-    float L = 0.f, v[DH / 64] = {};
-#pragma unroll 4
-    for (int i = 0; i < parts; ++i) {
-        const float2 ml = *(const float2*)(a.ml + (at + i * step) * 2);
-        const float w = fast_exp2(ml.x - ref);
-        L = fmaf(ml.y, w, L);
-#pragma unroll
-        for (int f = 0; f < DH / 64; ++f) v[f] = fmaf(a.acc[(at + i * step) * DH + f * 64 + lane], w, v[f]);
-    }
-    const KeyRange ks = keys_of(p, a.window, table_limit(a.table));
-    T* op = (T*)a.out + (int64_t)t * a.out_stride + h * DH;
-    float most = 0.f;
-#pragma unroll
-    for (int f = 0; f < DH / 64; ++f) {
-        v[f] = ks.last > ks.first ? v[f] / L : 0.f;
-        most = __builtin_elementwise_maximum(most, v[f]);
-    }
-    if (__builtin_amdgcn_ballot_w64(most != most)) {                   // as in the kernels above
-        row_again<T, DH>(a, b, t, h, ks, lane);
-        return;
-    }
-#pragma unroll
-    for (int f = 0; f < DH / 64; ++f) op[f * 64 + lane] = from_f32<T>(v[f]);
-}
-
-// Of the streaming kernel's sequences: a workgroup per (sequence, key/value head), as that kernel.  Rows of a single part are complete.
+// The sum over the parts of 2^(m_i - M) times their sums, in the order of the parts.  Rows of a single part are complete.
+// Of the streaming kernel's sequences: a workgroup per (sequence, key/value head), as that kernel, a wave per row.
 template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_stream_kernel(ChunkKernelArgs a)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = a.G;
@@ -825,9 +798,34 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_
     const int t0 = a.cu[b], end = a.cu[b + 1], n = end - t0 < a.tokens ? end - t0 : a.tokens, rows = n * G, p0 = a.len[b] - n, limit = table_limit(a.table);
     if (n <= 0 || rows > a.stream_rows) return;
     for (int r = wave; r < rows; r += 4) {
-        const int r0 = r & -STREAM_ROWS, t = t0 + r / G;
+        const int r0 = r & -STREAM_ROWS, t = t0 + r / G, h = kvh * G + r % G;
         const int parts = parts_of(tile_keys(p0, G, r0, r0 + STREAM_ROWS < rows ? r0 + STREAM_ROWS : rows, a.window, limit, ST_STEP), a.stream);
-        if (parts > 1 && t >= 0 && t < a.tokens) join_row<T, DH>(a, b, t, kvh * G + r % G, p0 + r / G, parts, lane);
+        if (parts <= 1 || t < 0 || t >= a.tokens) continue;
+        const int64_t at = a.stream_row(b, kvh, r, t, h), step = a.stream.rows;
+        // MAX_PARTS is a wave's lanes
+        const float2 x = lane < parts ? *(const float2*)(a.stream.ml + (at + lane * step) * 2) : float2{-INFINITY, 0.f};
+        const float M = wave_max(x.x), w = fast_exp2(x.x - (M == -INFINITY ? 0.f : M)), L = wave_sum(x.y * w);
+        float v[DH / 64] = {};
+#pragma unroll 4
+        for (int i = 0; i < parts; ++i) {
+            const float wi = __shfl(w, i, WAVE);
+#pragma unroll
+            for (int f = 0; f < DH / 64; ++f) v[f] = fmaf(a.stream.acc[(at + i * step) * DH + f * 64 + lane], wi, v[f]);
+        }
+        const KeyRange ks = keys_of(p0 + r / G, a.window, limit);
+        T* op = (T*)a.out + (int64_t)t * a.out_stride + h * DH;
+        float most = 0.f;
+#pragma unroll
+        for (int f = 0; f < DH / 64; ++f) {
+            v[f] = ks.last > ks.first ? v[f] / L : 0.f;
+            most = __builtin_elementwise_maximum(most, v[f]);
+        }
+        if (__builtin_amdgcn_ballot_w64(most != most)) {               // as in the kernels above
+            row_again<T, DH>(a, b, t, h, ks, lane);
+        } else {
+#pragma unroll
+            for (int f = 0; f < DH / 64; ++f) op[f * 64 + lane] = from_f32<T>(v[f]);
+        }
     }
 }
 // Of the tile kernel's: 1024 / DH rows a workgroup, DH / 4 threads each.
@@ -840,12 +838,12 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_
     const int limit = table_limit(a.table), r1 = tile.r0 + a.tile_rows < tile.rows ? tile.r0 + a.tile_rows : tile.rows;
     const int parts = parts_of(tile_keys(tile.p0, G, tile.r0, r1, a.window, limit, CT_ALIGN), a.tile);
     if (parts <= 1) return;
-    const int64_t step = (int64_t)a.tokens * a.H;
+    const int64_t step = a.tile.rows;
     const int row = tile.r0 + (blockIdx.y * 256 + tid) / PER, f = tid % PER * 4, tok = row / G, t = tile.t0 + tok, h = tile.kvh * G + row % G;
     const bool live = row < r1 && t >= 0 && t < a.tokens;
-    const int64_t at = live ? (int64_t)t * a.H + h : 0;
-    const float* ml = a.ml + at * 2;
-    const float* acc = a.acc + at * DH + f;
+    const int64_t at = live ? a.row(t, h) : 0;
+    const float* ml = a.tile.ml + at * 2;
+    const float* acc = a.tile.acc + at * DH + f;
     // the parts' weights: a lane of the row takes a part
     constexpr int EACH = MAX_PARTS / PER;
     __shared__ float s_w[1024 / DH][MAX_PARTS];
@@ -902,7 +900,6 @@ struct ChunkPlan {
     int qb;                          // row blocks per wave of the tile kernel
     int64_t slots;
     ChunkKernelArgs::Cut stream_cut, tile_cut;
-    int parts() const { int a = stream ? stream_cut.parts : 1, b = tile ? tile_cut.parts : 1; return a > b ? a : b; }
 };
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -912,9 +909,9 @@ static ChunkKernelArgs::Cut cut_keys(int64_t wgs, int64_t max_len, int64_t want,
     int64_t parts = want / wgs, most = ceil_div(max_len, least);
     parts = parts < most ? parts : most;
     parts = parts < MAX_PARTS ? parts : MAX_PARTS;
-    if (parts <= 1) return {1, 0x7fffffff};
+    if (parts <= 1) return {1, 0x7fffffff, 0, nullptr, nullptr};
     int64_t keys = ceil_div(ceil_div(max_len, parts), align) * align;
-    return {(int)ceil_div(max_len, keys), (int)keys};
+    return {(int)ceil_div(max_len, keys), (int)keys, 0, nullptr, nullptr};
 }
 
 static ChunkPlan chunk_plan(const ChunkAttnArgs& a)
@@ -923,7 +920,8 @@ static ChunkPlan chunk_plan(const ChunkAttnArgs& a)
     const int64_t G = a.H / a.Hkv, rows = (int64_t)a.max_new * G, T = a.tokens;
     const int64_t seen = a.window && (int64_t)a.window + a.max_new < a.max_len ? (int64_t)a.window + a.max_new : a.max_len;
     const bool f32 = a.dtype == DT_F32;
-    const ChunkKernelArgs::Cut whole{1, 0x7fffffff};
+    const ChunkKernelArgs::Cut whole{1, 0x7fffffff, 0, nullptr, nullptr};
+    p.stream_cut = p.tile_cut = whole;
     p.tile = rows > STREAM_ROWS;
     // Beside longer sequences one of up to 16 rows goes to the streaming kernel, not where there can be none (one sequence, or all bring
     // max_new tokens), and not where they are few and none is long: the tile kernel then takes it along, in the time that its other
@@ -955,13 +953,17 @@ static ChunkPlan chunk_plan(const ChunkAttnArgs& a)
         // parts of 256 keys 34).
         p.tile_cut = seen <= (f32 ? 128 : 640) ? whole : cut_keys(wgs(p.qb), seen, 640, f32 ? 128 : 256, CT_ALIGN);
     }
+    // rows of the parts: those of the packed tokens, or see stream_row
+    p.tile_cut.rows = T * a.H;
+    p.stream_cut.rows = p.tile ? (int64_t)a.n_seqs * a.Hkv * STREAM_ROWS : T * a.H;
     return p;
 }
+static size_t cut_floats(const ChunkKernelArgs::Cut& c, int dh) { return c.parts <= 1 ? 0 : (size_t)c.parts * c.rows * (dh + 2); }
 
 size_t chunk_attn_workspace(const ChunkAttnArgs& a)
 {
     const ChunkPlan p = chunk_plan(a);
-    return p.parts() <= 1 ? 0 : (size_t)p.parts() * a.tokens * a.H * (a.dh + 2) * sizeof(float);
+    return (cut_floats(p.stream_cut, a.dh) + cut_floats(p.tile_cut, a.dh)) * sizeof(float);
 }
 
 template <typename T, int DH, int QB> static hipError_t launch_tile(const ChunkKernelArgs& k, const ChunkPlan& p, hipStream_t s)
@@ -995,8 +997,14 @@ template <typename T, int DH> static hipError_t launch_chunk(const ChunkAttnArgs
 {
     const ChunkPlan p = chunk_plan(a);
     ChunkKernelArgs k{a.cu, a.len, a.n_seqs, a.tokens, a.q, a.q_stride, a.kv_blocks, a.table, a.H, a.Hkv, a.H / a.Hkv, a.scale, a.window, a.out, a.out_stride,
-                      p.stream_cut, p.tile_cut, 0, 64 * p.qb, a.workspace, nullptr};
-    k.ml = a.workspace ? a.workspace + (size_t)p.parts() * a.tokens * a.H * a.dh : nullptr;
+                      p.stream_cut, p.tile_cut, 0, 64 * p.qb};
+    float* w = a.workspace;
+    for (ChunkKernelArgs::Cut* c : {&k.stream, &k.tile}) {
+        if (c->parts <= 1) continue;
+        c->acc = w;
+        c->ml = w + (size_t)c->parts * c->rows * DH;
+        w += cut_floats(*c, DH);
+    }
     // without a tile kernel the streaming one takes every sequence, in tiles of 16 rows
     k.stream_rows = !p.tile ? 0x7fffffff : p.stream ? STREAM_ROWS : 0;
     hipError_t e;

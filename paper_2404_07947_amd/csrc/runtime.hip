@@ -10,6 +10,7 @@
 #include <cmath>
 #include <map>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -1546,14 +1547,21 @@ extern "C" int exe_seq_fork(exe_model_t* m, int32_t seq_id, int32_t n, const int
     }
     const Seq& s = m->seqs[seq_id];
     const int ndl = n_dec_layers(c);
-    std::vector<Seq> fresh(n);
+    std::vector<Seq> fresh;
+    std::vector<BlockCopy> copies;
+    try {
+        fresh.resize(n);
+        copies.reserve(n);
+        for (Seq& f : fresh) f.blocks.reserve(s.blocks.size());
+    } catch (const std::bad_alloc&) {
+        return fail(EXE_ERR_ARG, "no host memory for %d forks", n);
+    }
     hipError_t e = hipSuccess;
     if (paged(m)) {
         // Full blocks are shared: nothing writes to them again.  The last, partly filled one is the new sequence's own.
         const int full = s.len >> m->blk_shift, rest = s.len & (m->blk_rows - 1);
         if (rest && n > (int)m->free_blocks.size())
             return fail(EXE_ERR_OOM_KV, "K/V pool exhausted (%d blocks needed, %d of %d free)", n, (int)m->free_blocks.size(), m->n_blocks);
-        std::vector<BlockCopy> copies;
         for (Seq& f : fresh) {
             for (int i = 0; i < full; ++i) {
                 f.blocks.push_back(s.blocks[i]);
@@ -1602,7 +1610,7 @@ extern "C" int exe_seq_fork(exe_model_t* m, int32_t seq_id, int32_t n, const int
         f.live = true;
         f.len = s.len;
         f.n_in = s.n_in;
-        m->seqs[new_ids[i]] = f;
+        m->seqs[new_ids[i]] = std::move(f);
         m->live++;
     }
     return EXE_OK;
@@ -2358,6 +2366,7 @@ extern "C" int exe_op_rotary(void* hip_stream, int32_t dtype, int32_t T, const v
     if (dh != 64 && dh != 128) return fail(EXE_ERR_SHAPE, "head_dim must be 64 or 128");
     if (rot < 0 || rot > dh || rot % 2) return fail(EXE_ERR_SHAPE, "cannot turn %d of %d elements", rot, dh);
     if (interleaved != 0 && interleaved != 1) return fail(EXE_ERR_ARG, "interleaved must be 0 or 1");
+    if ((int64_t)heads * dh > 0x7fffffff) return fail(EXE_ERR_SHAPE, "%d heads in a row", heads);
     if (x_stride < (int64_t)heads * dh || out_stride < (int64_t)heads * dh) return fail(EXE_ERR_SHAPE, "rows of %d heads overlap", heads);
     if (x == out && x_stride != out_stride) return fail(EXE_ERR_ARG, "in place, both strides must be the same");
     if ((uintptr_t)x % esz_of_dtype(dtype) || (uintptr_t)out % esz_of_dtype(dtype)) return fail(EXE_ERR_ARG, "operands must be aligned to their type");
@@ -2378,6 +2387,7 @@ extern "C" int exe_op_rotary_append_paged(void* hip_stream, int32_t dtype, int32
         return fail(EXE_ERR_ARG, "bad rotary append arguments");
     if (rot < 0 || rot > dh || rot % 2) return fail(EXE_ERR_SHAPE, "cannot turn %d of %d elements", rot, dh);
     if (interleaved != 0 && interleaved != 1) return fail(EXE_ERR_ARG, "interleaved must be 0 or 1");
+    if (((int64_t)H + 2 * (int64_t)Hkv) * dh > 0x7fffffff) return fail(EXE_ERR_SHAPE, "%d and %d heads in a row", H, Hkv);
     if (row_stride < ((int64_t)H + 2 * (int64_t)Hkv) * dh || (q_out && q_out_stride < (int64_t)H * dh)) return fail(EXE_ERR_SHAPE, "rows overlap");
     if (q_out == qkv && q_out_stride != row_stride) return fail(EXE_ERR_ARG, "in place, both strides must be the same");
     if ((uintptr_t)kv_blocks & 15) return fail(EXE_ERR_ARG, "the cache must be 16-byte aligned");
@@ -2399,6 +2409,7 @@ static ChunkAttnArgs chunk_args(int dtype, int n_seqs, int T, int max_new, int m
 extern "C" uint64_t exe_op_chunk_attention_paged_workspace(int32_t dtype, int32_t n_seqs, int32_t T, int32_t max_new, int32_t max_len, int32_t H,
                                                            int32_t Hkv, int32_t dh, int32_t window)
 {
+    if ((dtype != DT_F32 && dtype != DT_BF16) || (dh != 64 && dh != 128)) return 0;
     if (n_seqs < 1 || T < 1 || max_new < 1 || max_len < 1 || Hkv < 1 || H < Hkv || H % Hkv || window < 0 || (int64_t)T * H > 0x7fffffff) return 0;
     return chunk_attn_workspace(chunk_args(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window));
 }
@@ -2448,8 +2459,14 @@ extern "C" int exe_op_kv_copy_blocks(void* hip_stream, int32_t dtype, void* kv_b
     if ((uintptr_t)kv_blocks & 15) return fail(EXE_ERR_ARG, "the cache must be 16-byte aligned");
     const int row_bytes = dh * esz_of_dtype(dtype);
     if (n_copies > n_blocks) return fail(EXE_ERR_ARG, "%d copies into %d blocks write one twice", n_copies, n_blocks);
-    std::vector<BlockCopy> list(n_copies);
-    std::vector<int32_t> to(n_copies);
+    std::vector<BlockCopy> list;
+    std::vector<int32_t> to;
+    try {
+        list.resize(n_copies);
+        to.resize(n_copies);
+    } catch (const std::bad_alloc&) {
+        return fail(EXE_ERR_ARG, "no host memory for %d copies", n_copies);
+    }
     for (int i = 0; i < n_copies; ++i) {
         BlockCopy& k = list[i] = BlockCopy{copies[3 * i], copies[3 * i + 1], copies[3 * i + 2]};
         if (k.src < 0 || k.src >= n_blocks || k.dst < 0 || k.dst >= n_blocks)

@@ -33,14 +33,14 @@ def test_what_both_refuse(change, code):
 
 @pytest.mark.parametrize("change,code", [
     (dict(qkv=None), -1), (dict(inv_freq=None), -1), (dict(rot=65), -2), (dict(rot=-2), -2), (dict(rot=66), -2), (dict(interleaved=2), -1), (dict(H=-1), -1),
-    (dict(row_stride=511), -2), (dict(q_stride=255), -2), (dict(qkv=P + 1), -1), (dict(q_out=P + 1), -1), (dict(qkv=P, q_out=P, q_stride=256), -1)])
+    (dict(row_stride=511), -2), (dict(H=1 << 26, row_stride=1 << 40, q_stride=1 << 40), -2), (dict(q_stride=255), -2), (dict(qkv=P + 1), -1), (dict(q_out=P + 1), -1), (dict(qkv=P, q_out=P, q_stride=256), -1)])
 def test_append_refusals(change, code):
     refused(exe.exe_op_rotary_append_paged, {**APPEND, "q_out": 2 * P}, code, **change)
 
 
 @pytest.mark.parametrize("change,code", [
     (dict(q=None), -1), (dict(out=None), -1), (dict(max_new=0), -1), (dict(max_len=0), -1), (dict(window=-1), -1), (dict(H=3), -2), (dict(H=1), -2),
-    (dict(q_stride=255), -2), (dict(q_stride=257), -2), (dict(out_stride=252), -2), (dict(q=P + 4), -1), (dict(out=P + 2), -1)])
+    (dict(q_stride=255), -2), (dict(q_stride=257), -2), (dict(T=1 << 30), -2), (dict(out_stride=252), -2), (dict(q=P + 4), -1), (dict(out=P + 2), -1)])
 def test_attention_refusals(change, code):
     refused(exe.exe_op_chunk_attention_paged, ATTEND, code, **change)
 
@@ -48,7 +48,7 @@ def test_attention_refusals(change, code):
 @pytest.mark.parametrize("change,code", [
     (dict(dtype=-1), -1), (dict(T=-1), -1), (dict(x=None), -1), (dict(out=None), -1), (dict(pos=None), -1), (dict(inv_freq=None), -1), (dict(heads=0), -1), (dict(dh=32), -2),
     (dict(rot=3), -2), (dict(rot=66), -2), (dict(interleaved=-1), -1), (dict(x_stride=255), -2), (dict(out_stride=255), -2), (dict(out=P, out_stride=300), -1),
-    (dict(x=P + 1), -1), (dict(out=P + 1), -1)])
+    (dict(x=P + 1), -1), (dict(out=P + 1), -1), (dict(heads=1 << 26, x_stride=1 << 40, out_stride=1 << 40), -2)])
 def test_rotary_refusals(change, code):
     refused(exe.exe_op_rotary, ROTARY, code, **change)
 
@@ -72,7 +72,7 @@ def test_nothing_to_do_is_no_error():
 
 def test_workspace_of_bad_arguments_is_none():
     good = (1, 4, 8, 2, 5000, 8, 2, 128, 0)
-    for i, v in ((1, 0), (2, 0), (3, 0), (4, 0), (5, 0), (5, 3), (6, 0), (6, -1), (8, -1)):
+    for i, v in ((0, 2), (7, 96), (1, 0), (2, 0), (3, 0), (4, 0), (5, 0), (5, 3), (6, 0), (6, -1), (8, -1)):
         assert exe.exe_op_chunk_attention_paged_workspace(*good[:i], v, *good[i + 1:]) == 0
 
 
