@@ -465,10 +465,10 @@ template <typename T, int DH, int QB> constexpr int ct_per_cu()
 }
 
 // Workgroup -> (slot, head), see prefill_mfma_kernel: the tiles of one sequence and head run side by side on one XCD.  Last rows (most
-// keys) first.  Slot -> tile: those of sequence b begin at slot floor(cu[b] * G / tile_rows) + b, which leaves room for every sequence's
+// keys) first.  Slot -> tile: those of sequence b begin at slot floor(cu[b] * G / rows of a tile) + b, which leaves room for every sequence's
 // last, partly filled tile whatever the lengths are.  b = -1: no tile, or a sequence of the streaming kernel's.
 struct ChunkTile { int b, kvh, t0, rows, p0, r0; };
-__device__ __forceinline__ ChunkTile find_tile(const ChunkKernelArgs& a, unsigned wg, int slots, int tile_rows, int lane)
+__device__ __forceinline__ ChunkTile find_tile(const ChunkKernelArgs& a, unsigned wg, int slots, int tile_shift, int lane)
 {
     int slot, kvh;
     if ((a.Hkv & 7) == 0) {
@@ -480,12 +480,24 @@ __device__ __forceinline__ ChunkTile find_tile(const ChunkKernelArgs& a, unsigne
         kvh = wg - slot * a.Hkv;
     }
     slot = slots - 1 - slot;
-    auto first_slot = [&](int64_t t, int b) { return (int)(t * a.G / tile_rows) + b; };
-    const int b = __builtin_amdgcn_readfirstlane(wave_search(0, a.n_seqs, lane, [&](int i) { return first_slot(a.cu[i], i) <= slot; }));
-    if (b < 0) return ChunkTile{-1};
-    const int t0 = a.cu[b], end = a.cu[b + 1], n = end - t0 < a.tokens ? end - t0 : a.tokens, rows = n * a.G;
-    const int r0 = (slot - first_slot(t0, b)) * tile_rows;
-    return ChunkTile{n <= 0 || r0 >= rows || rows <= a.stream_rows ? -1 : b, kvh, t0, rows, a.len[b] - n, r0};
+    auto first_slot = [&](int64_t t, int b) { return (int)(t * a.G >> tile_shift) + b; };
+    int b, t0, end, len;
+    if (a.n_seqs < WAVE) {                                             // all of it in one trip to memory
+        const int c = a.cu[lane < a.n_seqs ? lane : a.n_seqs], l = a.len[lane < a.n_seqs ? lane : a.n_seqs - 1];
+        b = __popcll(__builtin_amdgcn_ballot_w64(lane < a.n_seqs && first_slot(c, lane) <= slot)) - 1;
+        if (b < 0) return ChunkTile{-1};
+        t0 = __builtin_amdgcn_readlane(c, b);
+        end = __builtin_amdgcn_readlane(c, b + 1);
+        len = __builtin_amdgcn_readlane(l, b);
+    } else {
+        b = __builtin_amdgcn_readfirstlane(wave_search(0, a.n_seqs, lane, [&](int i) { return first_slot(a.cu[i], i) <= slot; }));
+        if (b < 0) return ChunkTile{-1};
+        t0 = a.cu[b];
+        end = a.cu[b + 1];
+        len = a.len[b];
+    }
+    const int n = end - t0 < a.tokens ? end - t0 : a.tokens, rows = n * a.G, r0 = (slot - first_slot(t0, b)) << tile_shift;
+    return ChunkTile{n <= 0 || r0 >= rows || rows <= a.stream_rows ? -1 : b, kvh, t0, rows, len - n, r0};
 }
 
 template <typename T, int DH, int QB>
@@ -496,7 +508,7 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
     extern __shared__ __align__(16) unsigned char ct_smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), qi = lane & 15, g = lane >> 4;
     const int G = a.G, part = blockIdx.y;
-    const ChunkTile tile = find_tile(a, blockIdx.x, slots, ROWS, lane);
+    const ChunkTile tile = find_tile(a, blockIdx.x, slots, QB == 2 ? 7 : 6, lane);
     if (tile.b < 0) return;
     const int b = tile.b, kvh = tile.kvh, t0 = tile.t0, rows = tile.rows, p0 = tile.p0, r0 = tile.r0, limit = table_limit(a.table);
     const KeyRange all = tile_keys(p0, G, r0, r0 + ROWS < rows ? r0 + ROWS : rows, a.window, limit, CT_ALIGN);
@@ -833,7 +845,7 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_
 {
     constexpr int PER = DH / 4;
     const int tid = threadIdx.x, lane = tid & 63, G = a.G;
-    const ChunkTile tile = find_tile(a, blockIdx.x, slots, a.tile_rows, lane);
+    const ChunkTile tile = find_tile(a, blockIdx.x, slots, a.tile_rows == 128 ? 7 : 6, lane);
     if (tile.b < 0) return;
     const int limit = table_limit(a.table), r1 = tile.r0 + a.tile_rows < tile.rows ? tile.r0 + a.tile_rows : tile.rows;
     const int parts = parts_of(tile_keys(tile.p0, G, tile.r0, r1, a.window, limit, CT_ALIGN), a.tile);
