@@ -1,11 +1,15 @@
 // Attention of a chunk of new tokens over a paged cache.
 //
-// The query rows of one sequence that share a key/value head are its new tokens times the H / Hkv heads of the group, row r = token
+// The query rows of one sequence that share a key/value head are its new tokens times the G = H / Hkv heads of the group, row r = token
 // r / G, head r % G: they read the same keys, so they are packed into one tile.
 //  * chunk_stream_kernel: up to 16 rows a sequence (single tokens, a few drafted ones).  Bound by reading the cache once.
-//  * chunk_tile_kernel: 64 to 256 rows a workgroup.  Bound by the MFMAs and by what feeds them.
-//  * chunk_join_kernel: where the keys of a tile were cut into parts for several workgroups, adds the parts up.
-// All hold scores and softmax in float, with the running maximum and sum of one pass over the keys.
+//  * chunk_tile_kernel: 64 or 128 rows a workgroup.  Bound by MFMAs and softmax, which overlap in part; with few rows to a sequence and
+//    many heads by the cache, again.
+//  * chunk_join_stream_kernel, chunk_join_tile_kernel: where the keys of a tile were cut into parts for several workgroups, add them up.
+//  * chunk_row: a wave per row, for rows that a hidden infinity or NaN has spoilt.
+// All hold scores and softmax in float, with the running maximum and sum of one pass over the keys.  Which run is chunk_plan's choice,
+// from what the host knows (bounds of the lengths); which sequence is whose, and how many parts a tile has, each kernel finds from the
+// lengths on the device, so that a captured launch follows them.
 #include <type_traits>
 
 #include "attn_row.h"
@@ -242,11 +246,14 @@ template <typename T, int DS> __device__ __forceinline__ void load_query(const T
 __device__ __forceinline__ float exponent_scale(float scale) { return scale == 0.f ? 1.f : fabsf(scale) * LOG2E; }
 
 // ---------------------------------------------------------------- few rows: the cache streams by
-// A workgroup of 4 waves takes the 16 rows of one (sequence, key/value head) and a part of its keys.  Every wave takes steps of 16 keys of
-// its own (wave w steps w, w + 4, ..), through a ring of stages in LDS that it fills itself by direct global-to-LDS loads, so no wave
-// waits for another one before the end.  64 KB of stages a workgroup, two workgroups a CU, keep 64 KB a CU in flight (float x 128: 128 KB,
-// one a CU).  Per step and wave: S^T = K . Q^T and O^T += V^T . P^T by MFMAs with the 16 rows as columns (see prefill_mfma_kernel); idle
-// columns cost nothing that the loads do not hide.  Probabilities enter the second product as two bf16 parts, 2^-17 relative.
+// A workgroup of 4 or 8 waves takes the 16 rows of one (sequence, key/value head) and a part of its keys.  Every wave takes steps of 16 keys
+// of its own (wave w steps w, w + WAVES, ..), through a ring of stages in LDS that it fills itself by direct global-to-LDS loads, so no
+// wave waits for another one before the end.  16 KB of stages a wave (float x 128: 32 KB), 8 waves a CU: half of that is in flight while
+// the rest is computed on.  (4 waves a CU with 32 KB each took 230 us where 8 take 182: a step is 400 instructions, most of them not
+// the matrix's.)  Per step and wave: S^T = K . Q^T and O^T += V^T . P^T by MFMAs with the 16 rows as columns (see prefill_mfma_kernel);
+// idle columns cost nothing that the loads do not hide.  Probabilities enter the second product as two bf16 parts, 2^-17 relative.
+// Bound by memory.  Nontemporal loads: 200 -> 182 us for 64 sequences of 500 to 8100 keys, 8 heads x 128 (1.1 GB, 6.1 TB/s); of 4096 keys
+// each 161 us (6.66 TB/s, where a plain read reaches 7.1): the difference is the cut into parts, which lengths that differ want.
 constexpr int ST_WAVES = 4, ST_STEP = 16;
 template <typename T, int DH, int WAVES> struct Stream {
     static constexpr int RB = DH * (int)sizeof(T), TILE = ST_STEP * RB, STAGE = 2 * TILE;
@@ -451,11 +458,24 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_stream_kernel(ChunkKernel
 }
 
 // ---------------------------------------------------------------- many rows: tiles
-// A workgroup of 4 waves owns 64 * QB rows, 16 * QB a wave, and a part of their keys, which pass through LDS in tiles of 64: two buffers
-// for keys, two for values, filled by direct global-to-LDS loads a tile ahead, one barrier a tile.  The products are those of
-// prefill_mfma_kernel.  A wave computes the scores of tile kt + 1 before it needs those of tile kt's successor: the MFMAs of the one
-// and the exponentials of the other do not depend on each other.
+// A workgroup of 4 waves owns 64 * QB rows, 16 * QB a wave, and a part of their keys, which pass through LDS in tiles of 64 (or 32): two
+// buffers for keys, two for values, filled by direct global-to-LDS loads a tile ahead, one barrier a tile.  The products are those of
+// prefill_mfma_kernel; what is taken otherwise than there:
+//  * The running maximum moves only where a score passes it by more than 2^8, so most tiles reduce nothing across lanes and rescale
+//    nothing; probabilities stay below 2^8, which costs no precision.  Rows of bf16 sum their probabilities, as rounded for the second
+//    product, by one more MFMA with ones (64 features 3 % faster than additions); float ones leave the sum spread over four lanes.
+//  * Table entries are read a tile before their rows' addresses are made, and stay scalar; 4 (64-wide heads 2) loads follow one base.
+//  * A wave stops at the last key that its rows see and then moves only its share.
+//  * LDS reads of a product go before its MFMAs, 8 fragments ahead, by scheduling groups (128 rows): placed by the compiler, each right
+//    before its use, the MFMAs waited for them: 975 us at the size below.  12 ahead are no better.
+// 2048 tokens behind 30720, 32 heads over 8 x 128: 905 us, 1170 TFLOP/s (a matrix product of 8192^3 reaches 1400 here); 4
+// prompts of 2048 x 40 heads 213 us, 810 TFLOP/s, where prefill_mfma_kernel takes 236.  What is left are MFMAs and softmax that take turns: two waves a
+// SIMD overlap by chance, MFMAs at a raised priority gave 3 %, exponentials of one half tile between the MFMAs of the other -2 to -9 %.
+// 64 rows a wave spill (650 TFLOP/s); 48 rows were 20 % faster per row where such tiles fill the chip, but they rarely do.  64 rows a
+// workgroup: tiles of 32 keys, registers and LDS for 4 workgroups a CU; 40 heads of 128 tokens over 1024, 12 sequences 64 us, with the loop
+// of the 128 rows 76.
 constexpr int CT_WAVES = 4, CT_ALIGN = 64;
+enum { VECTOR = 0x402, MATRIX = 0x008, LDS_READ = 0x100 };            // kinds of instructions, for the scheduler
 template <typename T, int DH, int QB> constexpr int ct_keys() { return QB == 1 && DH * (int)sizeof(T) > 128 ? 32 : 64; }
 template <typename T, int DH, int QB> constexpr int ct_lds() { return 4 * ct_keys<T, DH, QB>() * DH * (int)sizeof(T); }
 template <typename T, int DH, int QB> constexpr int ct_per_cu()
@@ -567,12 +587,16 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
         }
     };
 
-    f32x4 o[QB][DT];
-    float m[QB], l[QB];                                                // l: this lane's share
+    // sum: of float rows this lane's share, in [0]; of bf16 the whole, in each element
+    f32x4 o[QB][DT], sum[QB];
+    float m[QB];
+    bf16x8 ones;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ones[i] = (bf16_t)1.f;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         m[qb] = -INFINITY;
-        l[qb] = 0.f;
+        sum[qb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[qb][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -641,7 +665,7 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
                 float to = fmaxf(m[qb], rows_max(mx[qb])), ref = to == -INFINITY ? 0.f : to, alpha = fast_exp2(m[qb] - ref);
-                l[qb] *= alpha;
+                sum[qb] *= alpha;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) o[qb][dt] *= alpha;
                 m[qb] = to;
@@ -657,7 +681,7 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     s[qb][kb][r] = fast_exp2(fmaf(s[qb][kb][r], mul, -ref));
-                    l[qb] += s[qb][kb][r];
+                    if (sizeof(T) == 4) sum[qb][0] += s[qb][kb][r];
                 }
         }
     };
@@ -692,6 +716,8 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
 #pragma unroll
                     for (int e = 0; e < 8; ++e) pf[qb][e] = (bf16_t)s[qb][2 * ks + (e >> 2)][e & 3];
 #pragma unroll
+                for (int qb = 0; qb < QB; ++qb) sum[qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[qb], sum[qb], 0, 0, 0);
+#pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
                     const int at = ((2 * dt + (v_q >> 1)) ^ pf_swz<RB>(v_row)) << 4;
                     uint2 lo = pf_read_tr(sV + ks * 32 * RB + at), hi = pf_read_tr(sV + (ks * 32 + 16) * RB + at);
@@ -703,11 +729,62 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
         }
     };
 
-    if (n_tiles > 0) {
-        // Tile kt's values are loaded an iteration before its second product, its keys an iteration before that.
+    en = lookup(0);
+    float mx[QB];
+    if constexpr (QB == 2) if (n_tiles > 0) {
+        // Both of tile kt's a tile ahead.  8 LDS reads go before the MFMAs and one (of values two) between QB of them: left to itself the
+        // compiler reads each fragment right before its use, and the MFMAs wait.
+        Scores s;
+        auto both = [&](int kt) {
+            rv = from.rows(first_of(kt), en);
+            load_k(kt, rv);
+            load_v(kt, rv);
+            en = lookup(kt + 1);
+        };
+        both(0);
+        auto arrive = [&](int kt) {
+            wait_loads<0>();
+            __syncthreads();
+            if (kt + 1 < n_tiles) both(kt + 1);
+        };
+        auto iteration = [&](int kt) {
+            arrive(kt);
+            __builtin_amdgcn_s_setprio(1);                             // MFMAs go before another wave's softmax
+            scores(kt, s);
+            __builtin_amdgcn_sched_group_barrier(LDS_READ, 8, 0);
+#pragma unroll
+            for (int i = 0; i < KB * DS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(MATRIX, QB, 0);
+                __builtin_amdgcn_sched_group_barrier(LDS_READ, 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
+            largest(s, mx);
+            look(kt, s, mx);
+            exponentials(s);
+            __builtin_amdgcn_s_setprio(1);
+            values(kt, s);
+            __builtin_amdgcn_sched_group_barrier(LDS_READ, 8, 0);
+            __builtin_amdgcn_sched_group_barrier(VECTOR, 20 * QB * KB, 0);
+#pragma unroll
+            for (int i = 0; i < KB / 2 * DT; ++i) {
+                __builtin_amdgcn_sched_group_barrier(MATRIX, QB, 0);
+                __builtin_amdgcn_sched_group_barrier(LDS_READ, 2, 0);
+            }
+            __builtin_amdgcn_s_setprio(0);
+        };
+        int kt = 0;
+        for (; kt + 1 < n_mine; kt += 2) {
+            iteration(kt);
+            iteration(kt + 1);
+        }
+        if (kt < n_mine) iteration(kt++);
+        for (; kt < n_tiles; ++kt) arrive(kt);
+    }
+    if constexpr (QB == 1) if (n_tiles > 0) {
+        // Tile kt's values are loaded an iteration before its second product, its keys an iteration before that: scores of tile kt + 1 come
+        // before the second product of tile kt, so that their masks and maximum wait for no MFMA.
         Scores s[2];
-        float mx[QB];
-        en = lookup(0);
         bring(-1);
         wait_loads<0>();
         __syncthreads();
@@ -725,7 +802,7 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
         auto iteration = [&](int kt, Scores& now, Scores& next) {
             arrive(kt);
             exponentials(now);
-            __builtin_amdgcn_s_setprio(1);                             // MFMAs go before another wave's softmax
+            __builtin_amdgcn_s_setprio(1);
             scores(kt + 1, next);
             values(kt, now);
             __builtin_amdgcn_s_setprio(0);
@@ -760,17 +837,17 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
     for (int qb = 0; qb < QB; ++qb) {
         const int row = w0 + qb * 16 + qi, t = t0 + row / G, h = kvh * G + row % G;
         const bool write = row < rows && t >= 0 && t < a.tokens;
-        const float sum = rows_sum(l[qb]);
+        const float total = sizeof(T) == 4 ? rows_sum(sum[qb][0]) : sum[qb][0];
         if (parts > 1) {
             if (!write) continue;
             const int64_t at = part * a.tile.rows + a.row(t, h);
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) *(f32x4*)(a.tile.acc + at * DH + dt * 16 + 4 * g) = o[qb][dt];
-            if (g == 0) *(float2*)(a.tile.ml + at * 2) = float2{m[qb], sum};
+            if (g == 0) *(float2*)(a.tile.ml + at * 2) = float2{m[qb], total};
             continue;
         }
         const bool any = sees[qb].last > sees[qb].first;
-        const float inv = 1.f / sum;
+        const float inv = 1.f / total;
         float most = 0.f;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -915,17 +992,42 @@ struct ChunkPlan {
 };
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+static ChunkKernelArgs::Cut cut_to(int64_t parts, int64_t max_len, int align)
+{
+    if (parts <= 1) return {1, 0x7fffffff, 0, nullptr, nullptr};
+    int64_t keys = ceil_div(ceil_div(max_len, parts), align) * align;
+    return {(int)ceil_div(max_len, keys), (int)keys, 0, nullptr, nullptr};
+}
 // Parts for `wgs` workgroups that each would take up to max_len keys, so that `want` come of them, no part shorter than `least` keys.
 static ChunkKernelArgs::Cut cut_keys(int64_t wgs, int64_t max_len, int64_t want, int least, int align)
 {
     int64_t parts = want / wgs, most = ceil_div(max_len, least);
     parts = parts < most ? parts : most;
     parts = parts < MAX_PARTS ? parts : MAX_PARTS;
-    if (parts <= 1) return {1, 0x7fffffff, 0, nullptr, nullptr};
-    int64_t keys = ceil_div(ceil_div(max_len, parts), align) * align;
-    return {(int)ceil_div(max_len, keys), (int)keys, 0, nullptr, nullptr};
+    return cut_to(parts, max_len, align);
 }
 
+// Parts for the tile kernel, of `rows` packed rows with `seen` keys each: those with which the chip is done first.  Time is counted in keys of
+// a full CU: its `per_cu` workgroups take 2 of 10 shares together and 8 each by its own, and each part another 64 for its sums.  Joining
+// takes as long as 256 keys (7 us), of float ones 64.  2 x 512 tokens, 32 heads over 8 x 128, of 4096 keys are 256 workgroups: in 2 parts
+// 81 us, whole 98, in 3 parts, which a second round of workgroups has to take, 100; 1 x 512 behind 32000, 128 workgroups: 4 parts 258,
+// 5 parts 342.
+static ChunkKernelArgs::Cut cut_tiles(int64_t rows, int tile_rows, int per_cu, int64_t seen, int least, int each, int join)
+{
+    const int64_t round = 256 * per_cu;
+    int64_t parts = 1, best = 0;
+    for (int64_t p = 1; p <= MAX_PARTS && (p == 1 || p <= ceil_div(seen, least)); ++p) {
+        const int64_t wgs = ceil_div(rows * p, tile_rows), left = ceil_div(wgs % round, 256);
+        if (p > 1 && wgs > 4 * round) break;
+        const int64_t shares = wgs / round * 10 * per_cu + (left ? 2 * per_cu + 8 * left : 0);
+        const int64_t time = shares * (ceil_div(seen, p) + (p > 1 ? each : 0)) + (p > 1 ? 10 * per_cu * join : 0);
+        if (p == 1 || time < best) {
+            best = time;
+            parts = p;
+        }
+    }
+    return cut_to(parts, seen, CT_ALIGN);
+}
 static ChunkPlan chunk_plan(const ChunkAttnArgs& a)
 {
     ChunkPlan p{};
@@ -955,15 +1057,15 @@ static ChunkPlan chunk_plan(const ChunkAttnArgs& a)
         }
     }
     if (p.tile) {
-        auto wgs = [&](int qb) { return (ceil_div(T * G, 64 * qb) + (a.n_seqs - 1)) * a.Hkv; };
+        const int64_t wgs = (ceil_div(T * G, 128) + a.n_seqs - 1) * a.Hkv;
         // 128 rows a workgroup where several of its tiles share their keys, with 64 features only where the chip is full of them: bf16, us of
-        // 64 / 128 rows: x 128, 40 heads of 128 tokens over 1024, 12 sequences 67 / 93, 50 261 / 268; 32 heads over 8, 512 tokens over 4096, 1
-        // sequence 79 / 72, 16 668 / 568; the same x 64, 8 sequences 177 / 197, 16 345 / 322.  Float: registers leave room for 64.
-        p.qb = !f32 && rows >= 512 && wgs(2) >= (a.dh == 64 ? 2048 : 128) ? 2 : 1;
+        // 64 / 128 rows: x 128, 40 heads of 128 tokens over 1024, 12 sequences 64 / 78, 50 251 / 241; 32 heads over 8, 512 tokens over 4096, 1
+        // sequence 73 / 64, 16 629 / 492; the same x 64, 4 sequences 92 / 94, 8 170 / 166, 16 334 / 292.  Float: registers leave room for 64.
+        p.qb = !f32 && rows >= 512 && (a.dh == 128 || wgs >= 1024) ? 2 : 1;
         p.slots = T * G / (64 * p.qb) + a.n_seqs;
-        // Parts as for short calls above; float MFMAs are slow enough to pay for them from 128 keys on (8 heads of 100 tokens over 1000: 23 us,
-        // parts of 256 keys 34).
-        p.tile_cut = seen <= (f32 ? 128 : 640) ? whole : cut_keys(wgs(p.qb), seen, 640, f32 ? 128 : 256, CT_ALIGN);
+        const int per_cu = f32 ? a.dh == 128 ? ct_per_cu<float, 128, 1>() : ct_per_cu<float, 64, 1>()
+                         : p.qb == 1 ? ct_per_cu<bf16_t, 128, 1>() : a.dh == 128 ? ct_per_cu<bf16_t, 128, 2>() : ct_per_cu<bf16_t, 64, 2>();
+        p.tile_cut = cut_tiles(T * G * a.Hkv, 64 * p.qb, per_cu, seen, f32 ? 128 : 256, f32 ? 32 : 64, f32 ? 64 : 256);
     }
     // rows of the parts: those of the packed tokens, or see stream_row
     p.tile_cut.rows = T * a.H;
