@@ -466,14 +466,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_stream_kernel(ChunkKernel
 //    product, by one more MFMA with ones (64 features 3 % faster than additions); float ones leave the sum spread over four lanes.
 //  * Table entries are read a tile before their rows' addresses are made, and stay scalar; 4 (64-wide heads 2) loads follow one base.
 //  * A wave stops at the last key that its rows see and then moves only its share.
-//  * LDS reads of a product go before its MFMAs, 8 fragments ahead, by scheduling groups (128 rows): placed by the compiler, each right
-//    before its use, the MFMAs waited for them: 975 us at the size below.  12 ahead are no better.
-// 2048 tokens behind 30720, 32 heads over 8 x 128: 905 us, 1170 TFLOP/s (a matrix product of 8192^3 reaches 1400 here); 4
-// prompts of 2048 x 40 heads 213 us, 810 TFLOP/s, where prefill_mfma_kernel takes 236.  What is left are MFMAs and softmax that take turns: two waves a
-// SIMD overlap by chance, MFMAs at a raised priority gave 3 %, exponentials of one half tile between the MFMAs of the other -2 to -9 %.
-// 64 rows a wave spill (650 TFLOP/s); 48 rows were 20 % faster per row where such tiles fill the chip, but they rarely do.  64 rows a
-// workgroup: tiles of 32 keys, registers and LDS for 4 workgroups a CU; 40 heads of 128 tokens over 1024, 12 sequences 64 us, with the loop
-// of the 128 rows 76.
+//  * LDS reads of a product go before its MFMAs, 6 to 8 fragments ahead, by scheduling groups: placed by the compiler, each right before its
+//    use, the MFMAs waited for them: 975 us at the size below.  12 ahead are no better.
+// 2048 tokens behind 30720, 32 heads over 8 x 128: 902 us, 1180 TFLOP/s (a matrix product of 8192^3 reaches 1400 here); 4 prompts of 2048 x
+// 40 heads 213 us, 810 TFLOP/s, where prefill_mfma_kernel takes 236.  What is left are MFMAs and softmax that take turns: two waves a SIMD
+// overlap by chance, MFMAs at a raised priority gave 3 %, exponentials of one half tile between the MFMAs of the other -2 to -9 %, scores of
+// the next tile before the second product 0 to -5 %.  64 rows a wave spill (650 TFLOP/s); 48 rows were 20 % faster per row where such tiles
+// fill the chip, but they rarely do.  64 rows a workgroup: tiles of 32 keys, registers and LDS for 4 workgroups a CU.  40 heads of 97 to 256
+// tokens over 400 to 1280, 8 sequences: 51 us, 3.1 TB/s of keys and values.  Neither HBM nor L2 (9 TB/s), LDS (30 %), MFMAs (20 %) or vector
+// ALU bound it, but a wave's own chain of reads, MFMAs and softmax, 0.6 us a tile when a CU has it alone and 1.6 us beside three others;
+// loads two tiles ahead (3 workgroups a CU) 74 us, the keys in two parts 78.
 constexpr int CT_WAVES = 4, CT_ALIGN = 64;
 enum { VECTOR = 0x402, MATRIX = 0x008, LDS_READ = 0x100 };            // kinds of instructions, for the scheduler
 template <typename T, int DH, int QB> constexpr int ct_keys() { return QB == 1 && DH * (int)sizeof(T) > 128 ? 32 : 64; }
@@ -567,24 +569,12 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
     auto lookup = [&](int kt) { return from.lookup(first_of(kt)); };
     auto load_k = [&](int kt, const Rows& r) { from.keys(first_of(kt), r, dst + (kt & 1) * TILE); };
     auto load_v = [&](int kt, const Rows& r) { from.values(first_of(kt), r, dst + (2 + (kt & 1)) * TILE); };
-    // brings values of tile kt and keys of kt + 1
     Entries en;
-    Rows rv;                                                           // tiles of 64: the next values' rows, those that the keys came from
     auto bring = [&](int kt) {
-        if constexpr (KT == 64) {
-            if (kt >= 0) load_v(kt, rv);
-            if (kt + 1 < n_tiles) {
-                rv = from.rows(first_of(kt + 1), en);
-                load_k(kt + 1, rv);
-            }
-            en = lookup(kt + 2);
-        } else if (wave < 2) {
-            if (kt + 1 < n_tiles) load_k(kt + 1, from.rows(first_of(kt + 1), en));
-            en = lookup(kt + 2);
-        } else if (kt >= 0) {
-            load_v(kt, from.rows(first_of(kt), en));
-            en = lookup(kt + 1);
-        }
+        const Rows r = from.rows(first_of(kt), en);
+        if (KT == 64 || wave < 2) load_k(kt, r);
+        if (KT == 64 || wave >= 2) load_v(kt, r);
+        en = lookup(kt + 1);
     };
 
     // sum: of float rows this lane's share, in [0]; of bf16 the whole, in each element
@@ -729,29 +719,24 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
         }
     };
 
-    en = lookup(0);
-    float mx[QB];
-    if constexpr (QB == 2) if (n_tiles > 0) {
-        // Both of tile kt's a tile ahead.  8 LDS reads go before the MFMAs and one (of values two) between QB of them: left to itself the
-        // compiler reads each fragment right before its use, and the MFMAs wait.
+    if (n_tiles > 0) {
+        // Some LDS reads go before the MFMAs and the others between them, the values' after the exponentials: left to itself the compiler reads
+        // each fragment right before its use, and the MFMAs wait.
+        constexpr int AHEAD = QB == 1 ? 6 : 8;
         Scores s;
-        auto both = [&](int kt) {
-            rv = from.rows(first_of(kt), en);
-            load_k(kt, rv);
-            load_v(kt, rv);
-            en = lookup(kt + 1);
-        };
-        both(0);
+        float mx[QB];
+        en = lookup(0);
+        bring(0);
         auto arrive = [&](int kt) {
             wait_loads<0>();
             __syncthreads();
-            if (kt + 1 < n_tiles) both(kt + 1);
+            if (kt + 1 < n_tiles) bring(kt + 1);
         };
         auto iteration = [&](int kt) {
             arrive(kt);
             __builtin_amdgcn_s_setprio(1);                             // MFMAs go before another wave's softmax
             scores(kt, s);
-            __builtin_amdgcn_sched_group_barrier(LDS_READ, 8, 0);
+            __builtin_amdgcn_sched_group_barrier(LDS_READ, AHEAD, 0);
 #pragma unroll
             for (int i = 0; i < KB * DS; ++i) {
                 __builtin_amdgcn_sched_group_barrier(MATRIX, QB, 0);
@@ -764,7 +749,7 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
             exponentials(s);
             __builtin_amdgcn_s_setprio(1);
             values(kt, s);
-            __builtin_amdgcn_sched_group_barrier(LDS_READ, 8, 0);
+            __builtin_amdgcn_sched_group_barrier(LDS_READ, AHEAD, 0);
             __builtin_amdgcn_sched_group_barrier(VECTOR, 20 * QB * KB, 0);
 #pragma unroll
             for (int i = 0; i < KB / 2 * DT; ++i) {
@@ -779,55 +764,6 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
             iteration(kt + 1);
         }
         if (kt < n_mine) iteration(kt++);
-        for (; kt < n_tiles; ++kt) arrive(kt);
-    }
-    if constexpr (QB == 1) if (n_tiles > 0) {
-        // Tile kt's values are loaded an iteration before its second product, its keys an iteration before that: scores of tile kt + 1 come
-        // before the second product of tile kt, so that their masks and maximum wait for no MFMA.
-        Scores s[2];
-        bring(-1);
-        wait_loads<0>();
-        __syncthreads();
-        bring(0);
-        if (n_mine > 0) {
-            scores(0, s[0]);
-            largest(s[0], mx);
-            look(0, s[0], mx);
-        }
-        auto arrive = [&](int kt) {
-            wait_loads<0>();                                           // values of tile kt, keys of kt + 1
-            __syncthreads();
-            if (kt + 1 < n_tiles) bring(kt + 1);
-        };
-        auto iteration = [&](int kt, Scores& now, Scores& next) {
-            arrive(kt);
-            exponentials(now);
-            __builtin_amdgcn_s_setprio(1);
-            scores(kt + 1, next);
-            values(kt, now);
-            __builtin_amdgcn_s_setprio(0);
-            largest(next, mx);
-            look(kt + 1, next, mx);
-        };
-        int kt = 0;
-        for (; kt + 2 < n_mine; kt += 2) {
-            iteration(kt, s[0], s[1]);
-            iteration(kt + 1, s[1], s[0]);
-        }
-        if (kt + 1 < n_mine) {
-            iteration(kt, s[0], s[1]);
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb)
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb) s[0][qb][kb] = s[1][qb][kb];
-            ++kt;
-        }
-        if (kt < n_mine) {
-            arrive(kt);
-            exponentials(s[0]);
-            values(kt, s[0]);
-            ++kt;
-        }
         for (; kt < n_tiles; ++kt) arrive(kt);
     }
     if (!active) return;
