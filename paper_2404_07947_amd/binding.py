@@ -242,19 +242,22 @@ def _rows(t, dev: int, dtype: int, rows: int, width: int, stride: int) -> Option
     assert t.get_device() == dev, "expected a tensor on the current device"
     assert t.dtype is (_torch.bfloat16 if dtype else _torch.float32), f"expected the type {dtype}, got {t.dtype}"
     need = (rows - 1) * stride + width if rows > 0 else 0
-    assert need <= t.numel() or need <= t.untyped_storage().nbytes() // t.element_size() - t.storage_offset(), f"expected {need} elements"
+    assert (need <= t.numel() and t.is_contiguous()) or need <= t.untyped_storage().nbytes() // t.element_size() - t.storage_offset(), f"expected {need} elements"
     return t.data_ptr()
 
 
 def _where(stream):
-    """(current device, stream's address); without a GPU or with addresses only, torch is not asked."""
-    if stream is None or _torch is not None:
-        dev, current = _current()
-        return dev, current if stream is None else _stream_ptr(stream)
+    """(current device, stream's address); without a GPU there is no device, and addresses do."""
     try:
-        return _current()[0], _stream_ptr(stream)
+        dev, current = _current()
     except (RuntimeError, AssertionError):
+        if stream is None:
+            raise
         return None, _stream_ptr(stream)
+    if stream is None:
+        return dev, current
+    assert getattr(stream, "device_index", dev) == dev, "expected a stream of the current device"
+    return dev, _stream_ptr(stream)
 
 
 def _stream_ptr(stream) -> Optional[int]:
@@ -561,7 +564,10 @@ def exe_op_chunk_attention_paged_workspace(dtype, n_seqs, T, max_new, max_len, H
 def exe_op_chunk_attention_paged(dtype, n_seqs, cu_seqlens, T, max_new, q, q_stride, kv_blocks, n_blocks, block_table, max_blocks, block_size,
                                  length, max_len, H, Hkv, dh, scale, window, out, out_stride, workspace=None, stream=None):
     dev, s = _where(stream)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    ws_bytes = 0
+    if workspace is not None:
+        assert workspace.get_device() == dev, "expected a workspace on the current device"
+        ws_bytes = workspace.numel() * workspace.element_size()
     block = 2 * Hkv * block_size * dh
     _check(lib().exe_op_chunk_attention_paged(s, dtype, n_seqs, _array(cu_seqlens, dev, "int32", n_seqs + 1), T, max_new,
                                               _rows(q, dev, dtype, T, H * dh, q_stride), q_stride,

@@ -2425,7 +2425,7 @@ extern "C" int exe_op_chunk_attention_paged(void* hip_stream, int32_t dtype, int
     if (n_seqs < 0 || T < 0 || !cu_seqlens || !q || !kv_blocks || !block_table || !len || !out) return fail(EXE_ERR_ARG, "bad chunk attention arguments");
     if (max_new < 1 || max_len < 1 || window < 0) return fail(EXE_ERR_ARG, "max_new %d, max_len %d, window %d", max_new, max_len, window);
     if (H < Hkv || H % Hkv) return fail(EXE_ERR_SHAPE, "%d query heads over %d key/value heads", H, Hkv);
-    if ((int64_t)T * H > 0x7fffffff) return fail(EXE_ERR_SHAPE, "%d rows of %d heads", T, H);
+    if ((int64_t)T * H > 0x7fffffff || (int64_t)H * dh > 0x7fffffff) return fail(EXE_ERR_SHAPE, "%d rows of %d heads", T, H);
     const int esz = esz_of_dtype(dtype);
     if (q_stride < (int64_t)H * dh || out_stride < (int64_t)H * dh) return fail(EXE_ERR_SHAPE, "rows of %d heads overlap", H);
     if (q_stride * esz % 16 || out_stride * esz % 16) return fail(EXE_ERR_SHAPE, "rows must begin on 16 bytes");
@@ -2433,6 +2433,7 @@ extern "C" int exe_op_chunk_attention_paged(void* hip_stream, int32_t dtype, int
     for (const void* p : ptrs)
         if ((uintptr_t)p & 15) return fail(EXE_ERR_ARG, "operands must be 16-byte aligned");
     if (n_seqs == 0 || T == 0) return EXE_OK;
+    if (q == out) return fail(EXE_ERR_ARG, "rows of q are read after others of out are written: they cannot be the same");
     ChunkAttnArgs a = chunk_args(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window);
     uint64_t need = chunk_attn_workspace(a);
     if (need > (workspace ? workspace_bytes : 0)) return fail(EXE_ERR_ARG, "workspace too small (%llu bytes needed)", (unsigned long long)need);

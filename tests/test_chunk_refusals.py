@@ -126,3 +126,45 @@ def test_tensors_of_the_host_are_refused():
         exe.exe_op_kv_copy_blocks(*{**COPY, "pool": x}.values(), stream=1)
     with pytest.raises(AssertionError):
         exe.exe_op_chunk_attention_paged(*{**ATTEND, "table": pos}.values(), stream=1)
+
+
+def test_results_over_the_queries_are_refused():
+    with pytest.raises(exe.ExeError, match="cannot be the same"):
+        exe.exe_op_chunk_attention_paged(*ATTEND.values(), stream=1)
+
+
+def test_rows_whose_elements_no_int_counts_are_refused():
+    refused(exe.exe_op_chunk_attention_paged, {**ATTEND, "out": 2 * P}, -2, T=1, H=1 << 26, q_stride=1 << 40, out_stride=1 << 40)
+
+
+def test_tensors_that_hold_less_than_they_show_are_refused(monkeypatch):
+    torch = pytest.importorskip("torch")
+    from paper_2404_07947_amd import binding
+    monkeypatch.setattr(binding, "_torch", torch)
+    host = -1                                       # a host tensor's device number
+    one = torch.zeros(1, 64)
+    assert binding._rows(one.repeat(8, 1), host, 0, 8, 64, 64)
+    assert binding._rows(torch.zeros(8, 128)[:, 64:], host, 0, 8, 64, 128)
+    with pytest.raises(AssertionError):             # 8 rows to look at, memory of one
+        binding._rows(one.expand(8, 64), host, 0, 8, 64, 64)
+    with pytest.raises(AssertionError):             # the last row ends behind the memory
+        binding._rows(torch.zeros(8, 128)[:, 64:], host, 0, 8, 65, 128)
+
+
+def test_streams_and_workspaces_of_another_device_are_refused(monkeypatch):
+    torch = pytest.importorskip("torch")
+    from paper_2404_07947_amd import binding
+    monkeypatch.setattr(binding, "_torch", torch)
+    monkeypatch.setattr(binding, "_current", lambda: (0, None))
+
+    class Other:
+        device_index, cuda_stream = 1, 7
+
+    class Own:
+        device_index, cuda_stream = 0, 7
+
+    assert binding._where(Own()) == (0, 7)
+    with pytest.raises(AssertionError):
+        binding._where(Other())
+    with pytest.raises(AssertionError):
+        exe.exe_op_chunk_attention_paged(*{**ATTEND, "out": 2 * P}.values(), workspace=torch.zeros(16), stream=1)
