@@ -2,7 +2,8 @@
 //
 // The query rows of one sequence that share a key/value head are its new tokens times the G = H / Hkv heads of the group, row r = token
 // r / G, head r % G: they read the same keys, so they are packed into one tile.
-//  * chunk_stream_kernel: up to 16 rows a sequence (single tokens, a few drafted ones).  Bound by reading the cache once.
+//  * chunk_stream_kernel: up to 16 rows a sequence (single tokens, a few drafted ones), and calls of few rows in tiles of 16.  Bound by
+//    reading the cache.
 //  * chunk_tile_kernel: 64 or 128 rows a workgroup.  Bound by MFMAs and softmax, which overlap in part; with few rows to a sequence and
 //    many heads by the cache, again.
 //  * chunk_join_stream_kernel, chunk_join_tile_kernel: where the keys of a tile were cut into parts for several workgroups, add them up.
@@ -231,6 +232,42 @@ template <typename T, int DH, bool NT> struct RowLoader {
     __device__ __forceinline__ void values(int j, const Rows& r, unsigned dst) const { move(j, r.r0.key + r.r0.value, r.r1.key + r.r1.value, dst); }
 };
 
+// Workgroup -> (slot, head), see prefill_mfma_kernel: the tiles of one sequence and head run side by side on one XCD.  Last rows (most
+// keys) first.  Slot -> tile: those of sequence b begin at slot floor(cu[b] * G / rows of a tile) + b, which leaves room for every sequence's
+// last, partly filled tile whatever the lengths are.  b = -1: no tile, or a sequence of up to `least` rows, which is another kernel's.
+struct ChunkTile { int b, kvh, t0, rows, p0, r0; };
+__device__ __forceinline__ ChunkTile find_tile(const ChunkKernelArgs& a, unsigned wg, int slots, int tile_shift, int least, int lane)
+{
+    int slot, kvh;
+    if ((a.Hkv & 7) == 0) {
+        int hpx = a.Hkv >> 3, j = wg >> 3;
+        slot = j / hpx;
+        kvh = (wg & 7) + 8 * (j - slot * hpx);
+    } else {
+        slot = wg / a.Hkv;
+        kvh = wg - slot * a.Hkv;
+    }
+    slot = slots - 1 - slot;
+    auto first_slot = [&](int64_t t, int b) { return (int)(t * a.G >> tile_shift) + b; };
+    int b, t0, end, len;
+    if (a.n_seqs < WAVE) {                                             // all of it in one trip to memory
+        const int c = a.cu[lane < a.n_seqs ? lane : a.n_seqs], l = a.len[lane < a.n_seqs ? lane : a.n_seqs - 1];
+        b = __popcll(__builtin_amdgcn_ballot_w64(lane < a.n_seqs && first_slot(c, lane) <= slot)) - 1;
+        if (b < 0) return ChunkTile{-1};
+        t0 = __builtin_amdgcn_readlane(c, b);
+        end = __builtin_amdgcn_readlane(c, b + 1);
+        len = __builtin_amdgcn_readlane(l, b);
+    } else {
+        b = __builtin_amdgcn_readfirstlane(wave_search(0, a.n_seqs, lane, [&](int i) { return first_slot(a.cu[i], i) <= slot; }));
+        if (b < 0) return ChunkTile{-1};
+        t0 = a.cu[b];
+        end = a.cu[b + 1];
+        len = a.len[b];
+    }
+    const int n = end - t0 < a.tokens ? end - t0 : a.tokens, rows = n * a.G, r0 = (slot - first_slot(t0, b)) << tile_shift;
+    return ChunkTile{n <= 0 || r0 >= rows || rows <= least ? -1 : b, kvh, t0, rows, len - n, r0};
+}
+
 // A row's query fragments (B operand of the first product): lane (row qi, group g) holds 16-byte chunks 4 * ds + g.  The sign of the
 // scale goes to the query, since the softmax takes the maximum of the raw scores; scale 0 makes it 0, and all scores that are numbers.
 template <typename T, int DS> __device__ __forceinline__ void load_query(const T* q, int g, float scale, u32x4 (&f)[DS])
@@ -263,22 +300,30 @@ template <typename T, int DH, int WAVES> struct Stream {
     static constexpr int LDS = WAVES * STAGES * STAGE > MERGE ? WAVES * STAGES * STAGE : MERGE;
 };
 
-template <typename T, int DH, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 2) void chunk_stream_kernel(ChunkKernelArgs a)
+// TILES: the workgroup's 16 rows are a tile of a longer chunk, else all of a sequence's (16 at a time).
+template <typename T, int DH, int WAVES, bool TILES>
+__global__ __launch_bounds__(WAVES * 64, 2) void chunk_stream_kernel(ChunkKernelArgs a, int slots)
 {
     typedef Stream<T, DH, WAVES> S;
     constexpr int RB = S::RB, DS = RB / 64, DT = DH / 16;
     extern __shared__ __align__(16) unsigned char st_smem[];
     __shared__ float s_ml[WAVES][16][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), qi = lane & 15, g = lane >> 4;
-    const int b = blockIdx.x / a.Hkv, kvh = blockIdx.x - b * a.Hkv, part = blockIdx.y, G = a.G;
-    const int t0 = a.cu[b], end = a.cu[b + 1], n = end - t0 < a.tokens ? end - t0 : a.tokens, rows = n * G, p0 = a.len[b] - n, limit = table_limit(a.table);
-    if (n <= 0 || rows > a.stream_rows) return;
+    const int part = blockIdx.y, G = a.G, limit = table_limit(a.table);
+    ChunkTile tile;
+    if constexpr (TILES) {
+        tile = find_tile(a, blockIdx.x, slots, 4, 0, lane);
+    } else {
+        const int b = blockIdx.x / a.Hkv, t0 = a.cu[b], end = a.cu[b + 1], n = end - t0 < a.tokens ? end - t0 : a.tokens;
+        tile = ChunkTile{n <= 0 || n * G > a.stream_rows ? -1 : b, (int)blockIdx.x - b * a.Hkv, t0, n * G, a.len[b] - n, 0};
+    }
+    if (tile.b < 0) return;
+    const int b = tile.b, kvh = tile.kvh, t0 = tile.t0, rows = tile.rows, p0 = tile.p0;
     const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)st_smem + wave * (S::STAGES * S::STAGE);
     const unsigned char* mine = st_smem + wave * (S::STAGES * S::STAGE);
     const float mul = exponent_scale(a.scale);
 
-    for (int r0 = 0; r0 < rows; r0 += 16) {
+    for (int r0 = tile.r0; r0 < (TILES ? tile.r0 + 1 : rows); r0 += 16) {
         const int r1 = r0 + 16 < rows ? r0 + 16 : rows;
         const KeyRange all = tile_keys(p0, G, r0, r1, a.window, limit, ST_STEP);
         const int parts = parts_of(all, a.stream);
@@ -468,14 +513,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_stream_kernel(ChunkKernel
 //  * A wave stops at the last key that its rows see and then moves only its share.
 //  * LDS reads of a product go before its MFMAs, 6 to 8 fragments ahead, by scheduling groups: placed by the compiler, each right before its
 //    use, the MFMAs waited for them: 975 us at the size below.  12 ahead are no better.
-// 2048 tokens behind 30720, 32 heads over 8 x 128: 902 us, 1180 TFLOP/s (a matrix product of 8192^3 reaches 1400 here); 4 prompts of 2048 x
-// 40 heads 213 us, 810 TFLOP/s, where prefill_mfma_kernel takes 236.  What is left are MFMAs and softmax that take turns: two waves a SIMD
-// overlap by chance, MFMAs at a raised priority gave 3 %, exponentials of one half tile between the MFMAs of the other -2 to -9 %, scores of
-// the next tile before the second product 0 to -5 %.  64 rows a wave spill (650 TFLOP/s); 48 rows were 20 % faster per row where such tiles
-// fill the chip, but they rarely do.  64 rows a workgroup: tiles of 32 keys, registers and LDS for 4 workgroups a CU.  40 heads of 97 to 256
-// tokens over 400 to 1280, 8 sequences: 51 us, 3.1 TB/s of keys and values.  Neither HBM nor L2 (9 TB/s), LDS (30 %), MFMAs (20 %) or vector
-// ALU bound it, but a wave's own chain of reads, MFMAs and softmax, 0.6 us a tile when a CU has it alone and 1.6 us beside three others;
-// loads two tiles ahead (3 workgroups a CU) 74 us, the keys in two parts 78.
+// 2048 tokens, the last of 32768, 32 heads over 8 x 128: 900 us, 1180 TFLOP/s (a matrix product of 8192^3 reaches 1400 here); 4 prompts of
+// 2048 x 40 heads 213 us, 810 TFLOP/s, where prefill_mfma_kernel takes 236.  What is left are MFMAs and softmax that take turns: two waves a
+// SIMD overlap by chance, MFMAs at a raised priority gave 3 %, exponentials of one half tile between the MFMAs of the other -2 to -9 %,
+// scores of the next tile before the second product 0 to -5 %; 64 rows as two waves of 32: 128 features 0 to +4 %, 64 -3 to -40 %.  64 rows a
+// wave spill (650 TFLOP/s); 48 rows were 20 % faster per row where such tiles fill the chip, but they rarely do.  64 rows a workgroup: tiles
+// of 32 keys, registers and LDS for 4 workgroups a CU.  40 heads of 97 to 256 tokens over 400 to 1280, 8 sequences: 51 us, 3.1 TB/s of keys
+// and values.  Neither HBM nor L2 (9 TB/s), LDS (30 %), MFMAs (20 %) or vector ALU bound it, but a wave's own chain of reads, MFMAs and
+// softmax, 0.6 us a tile when a CU has it alone and 1.6 us beside three others; loads two tiles ahead (3 workgroups a CU) 74 us, the keys in
+// two parts 78.
 constexpr int CT_WAVES = 4, CT_ALIGN = 64;
 enum { VECTOR = 0x402, MATRIX = 0x008, LDS_READ = 0x100 };            // kinds of instructions, for the scheduler
 template <typename T, int DH, int QB> constexpr int ct_keys() { return QB == 1 && DH * (int)sizeof(T) > 128 ? 32 : 64; }
@@ -486,42 +532,6 @@ template <typename T, int DH, int QB> constexpr int ct_per_cu()
     return QB == 2 ? DH == 128 ? 2 : 3 : 4;
 }
 
-// Workgroup -> (slot, head), see prefill_mfma_kernel: the tiles of one sequence and head run side by side on one XCD.  Last rows (most
-// keys) first.  Slot -> tile: those of sequence b begin at slot floor(cu[b] * G / rows of a tile) + b, which leaves room for every sequence's
-// last, partly filled tile whatever the lengths are.  b = -1: no tile, or a sequence of the streaming kernel's.
-struct ChunkTile { int b, kvh, t0, rows, p0, r0; };
-__device__ __forceinline__ ChunkTile find_tile(const ChunkKernelArgs& a, unsigned wg, int slots, int tile_shift, int lane)
-{
-    int slot, kvh;
-    if ((a.Hkv & 7) == 0) {
-        int hpx = a.Hkv >> 3, j = wg >> 3;
-        slot = j / hpx;
-        kvh = (wg & 7) + 8 * (j - slot * hpx);
-    } else {
-        slot = wg / a.Hkv;
-        kvh = wg - slot * a.Hkv;
-    }
-    slot = slots - 1 - slot;
-    auto first_slot = [&](int64_t t, int b) { return (int)(t * a.G >> tile_shift) + b; };
-    int b, t0, end, len;
-    if (a.n_seqs < WAVE) {                                             // all of it in one trip to memory
-        const int c = a.cu[lane < a.n_seqs ? lane : a.n_seqs], l = a.len[lane < a.n_seqs ? lane : a.n_seqs - 1];
-        b = __popcll(__builtin_amdgcn_ballot_w64(lane < a.n_seqs && first_slot(c, lane) <= slot)) - 1;
-        if (b < 0) return ChunkTile{-1};
-        t0 = __builtin_amdgcn_readlane(c, b);
-        end = __builtin_amdgcn_readlane(c, b + 1);
-        len = __builtin_amdgcn_readlane(l, b);
-    } else {
-        b = __builtin_amdgcn_readfirstlane(wave_search(0, a.n_seqs, lane, [&](int i) { return first_slot(a.cu[i], i) <= slot; }));
-        if (b < 0) return ChunkTile{-1};
-        t0 = a.cu[b];
-        end = a.cu[b + 1];
-        len = a.len[b];
-    }
-    const int n = end - t0 < a.tokens ? end - t0 : a.tokens, rows = n * a.G, r0 = (slot - first_slot(t0, b)) << tile_shift;
-    return ChunkTile{n <= 0 || r0 >= rows || rows <= a.stream_rows ? -1 : b, kvh, t0, rows, len - n, r0};
-}
-
 template <typename T, int DH, int QB>
 __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk_tile_kernel(ChunkKernelArgs a, int slots)
 {
@@ -530,7 +540,7 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
     extern __shared__ __align__(16) unsigned char ct_smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), qi = lane & 15, g = lane >> 4;
     const int G = a.G, part = blockIdx.y;
-    const ChunkTile tile = find_tile(a, blockIdx.x, slots, QB == 2 ? 7 : 6, lane);
+    const ChunkTile tile = find_tile(a, blockIdx.x, slots, QB == 2 ? 7 : 6, a.stream_rows, lane);
     if (tile.b < 0) return;
     const int b = tile.b, kvh = tile.kvh, t0 = tile.t0, rows = tile.rows, p0 = tile.p0, r0 = tile.r0, limit = table_limit(a.table);
     const KeyRange all = tile_keys(p0, G, r0, r0 + ROWS < rows ? r0 + ROWS : rows, a.window, limit, CT_ALIGN);
@@ -858,7 +868,7 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_
 {
     constexpr int PER = DH / 4;
     const int tid = threadIdx.x, lane = tid & 63, G = a.G;
-    const ChunkTile tile = find_tile(a, blockIdx.x, slots, a.tile_rows == 128 ? 7 : 6, lane);
+    const ChunkTile tile = find_tile(a, blockIdx.x, slots, a.tile_rows == 128 ? 7 : 6, a.stream_rows, lane);
     if (tile.b < 0) return;
     const int limit = table_limit(a.table), r1 = tile.r0 + a.tile_rows < tile.rows ? tile.r0 + a.tile_rows : tile.rows;
     const int parts = parts_of(tile_keys(tile.p0, G, tile.r0, r1, a.window, limit, CT_ALIGN), a.tile);
@@ -921,6 +931,7 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_
 // ---------------------------------------------------------------- launches
 struct ChunkPlan {
     bool stream, tile;               // which kernels run
+    bool small;                      // the streaming kernel, in tiles
     int waves;                       // of the streaming kernel's workgroups
     int qb;                          // row blocks per wave of the tile kernel
     int64_t slots;
@@ -972,12 +983,21 @@ static ChunkPlan chunk_plan(const ChunkAttnArgs& a)
     const bool f32 = a.dtype == DT_F32;
     const ChunkKernelArgs::Cut whole{1, 0x7fffffff, 0, nullptr, nullptr};
     p.stream_cut = p.tile_cut = whole;
-    p.tile = rows > STREAM_ROWS;
+    // A call of few rows by tiles of 16, whose keys go to 8 waves: shorter chains than the tile kernel's, and no second launch where that one
+    // cuts them.  Up to 1024 keys and 512 workgroups; of 64 features, whose tiles are cheaper, 320 and no more than 1024 keys a CU; float x 128
+    // has 4 waves and gains nothing.  us, tile kernel first: bf16 x 128, 32 heads over 8, 32 to 64 tokens over 512 16.1, 10.0, 128 to 256 16.9,
+    // 15.2; 40 heads, 4 x 12 to 24 over 600 30.8, 13.1; 16 heads over 4, 4 x 64 over 2000 22.1, 21.7; x 64, 40 heads, 4 x 12 to 24 over 600 19.7, 10.0;
+    // 32 over 8, 128 to 256 over 512 10.9, 12.7; float x 64, 16 over 4, 64 over 512 14.9, 12.0.
+    const int64_t small = (ceil_div(T * G, STREAM_ROWS) + a.n_seqs - 1) * a.Hkv;
+    p.small = rows > STREAM_ROWS && seen <= 1024 && (a.dh == 64 ? small <= 320 && small * seen <= 256 * 1024 : !f32 && small <= 512);
+    p.tile = rows > STREAM_ROWS && !p.small;
     // Beside longer sequences one of up to 16 rows goes to the streaming kernel, not where there can be none (one sequence, or all bring
     // max_new tokens), and not where they are few and none is long: the tile kernel then takes it along, in the time that its other
-    // sequences take, and a launch or two are saved (8 chunks of 97 to 256 tokens, 40 heads: 59 us, of them 9).
+    // sequences take, and a launch or two are saved (8 chunks of 97 to 256 tokens, 40 heads: 50 us).
     p.stream = !p.tile || (a.n_seqs > 1 && T <= (int64_t)(a.n_seqs - 1) * a.max_new + STREAM_ROWS / G && (T * G < (int64_t)64 * a.n_seqs || seen > 4096));
-    if (p.stream) {
+    if (p.small) {
+        p.slots = T * G / STREAM_ROWS + a.n_seqs;
+    } else if (p.stream) {
         const int64_t wgs = (int64_t)a.n_seqs * a.Hkv;
         // At most one workgroup a CU: of 8 waves (float x 128 fills a CU's LDS with 4), as many parts as CUs are left.  Short ones whole: a
         // second launch takes longer than the keys (1 x 40 heads of 512 keys: 10.3 us, in 4 parts 10.0 and a launch; of 1024: 15.4, 11.4).
@@ -1029,17 +1049,17 @@ template <typename T, int DH, int QB> static hipError_t launch_tile(const ChunkK
     return hipGetLastError();
 }
 
-template <typename T, int DH, int WAVES> static hipError_t launch_stream(const ChunkKernelArgs& k, const ChunkPlan& p, hipStream_t s)
+template <typename T, int DH, int WAVES, bool TILES> static hipError_t launch_stream(const ChunkKernelArgs& k, const ChunkPlan& p, hipStream_t s)
 {
     typedef Stream<T, DH, WAVES> S;
     static LdsLimit limit[MAX_DEVICES];
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) dev = 0;
-    hipError_t e = limit[dev].raise((const void*)chunk_stream_kernel<T, DH, WAVES>, S::LDS);
+    hipError_t e = limit[dev].raise((const void*)chunk_stream_kernel<T, DH, WAVES, TILES>, S::LDS);
     if (e != hipSuccess) return e;
-    const int64_t wgs = (int64_t)k.n_seqs * k.Hkv;
+    const int64_t wgs = (TILES ? p.slots : k.n_seqs) * k.Hkv;
     if (wgs * WAVES * 64 * p.stream_cut.parts > MAX_LAUNCH_THREADS) return hipErrorInvalidValue;
-    chunk_stream_kernel<T, DH, WAVES><<<dim3((unsigned)wgs, p.stream_cut.parts), WAVES * 64, S::LDS, s>>>(k);
+    chunk_stream_kernel<T, DH, WAVES, TILES><<<dim3((unsigned)wgs, p.stream_cut.parts), WAVES * 64, S::LDS, s>>>(k, (int)p.slots);
     return hipGetLastError();
 }
 
@@ -1059,8 +1079,9 @@ template <typename T, int DH> static hipError_t launch_chunk(const ChunkAttnArgs
     k.stream_rows = !p.tile ? 0x7fffffff : p.stream ? STREAM_ROWS : 0;
     hipError_t e;
     if (p.stream) {
-        if constexpr (sizeof(T) == 2 || DH == 64) e = p.waves == 8 ? launch_stream<T, DH, 8>(k, p, s) : launch_stream<T, DH, ST_WAVES>(k, p, s);
-        else e = launch_stream<T, DH, ST_WAVES>(k, p, s);
+        if constexpr (sizeof(T) == 2 || DH == 64)
+            e = p.small ? launch_stream<T, DH, 8, true>(k, p, s) : p.waves == 8 ? launch_stream<T, DH, 8, false>(k, p, s) : launch_stream<T, DH, ST_WAVES, false>(k, p, s);
+        else e = launch_stream<T, DH, ST_WAVES, false>(k, p, s);
         if (e != hipSuccess) return e;
     }
     if (p.tile) {

@@ -10,6 +10,9 @@ U = 2.0 ** -24                                   # half a step of float
 HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}    # half a step of the storage type
 
 
+BOUND = 1          # of the lengths, at least: sizes the launch, so a larger one brings small cases to the kernels of larger ones
+
+
 class Batch:
     """Sequences of `seqs` = [(new tokens, positions with them)] over blocks in random order; what no sequence holds is NaN, the
     table's unused entries are far out of the pool."""
@@ -57,7 +60,7 @@ class Batch:
     def attend(self, window=0, max_new=None, max_len=None, out=None, stream=None, workspace=None, scale=None):
         """The library's result (rows behind the last sequence hold 7)."""
         n = max([s[0] for s in self.seqs] + [1]) if max_new is None else max_new
-        L = max([s[1] for s in self.seqs] + [1]) if max_len is None else max_len
+        L = max([s[1] for s in self.seqs] + [BOUND]) if max_len is None else max_len
         w = self.H * self.dh
         if out is None:
             out = torch.full((self.rows, w), 7.0, dtype=self.t, device=DEV)

@@ -4,9 +4,17 @@ import numpy as np
 import pytest
 import torch
 
+import chunk_util
 from chunk_util import DEV, HALF, U, Batch, check
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, params=[1, 1100], ids=["own", "tiles"])
+def bound(request, monkeypatch):
+    """Calls of few rows and up to 1024 keys go to the streaming kernel: with a larger bound of the lengths, to the tile kernel."""
+    monkeypatch.setattr(chunk_util, "BOUND", request.param)
+
 
 HEADS = [(4, 4), (8, 2), (6, 2), (5, 1), (16, 1), (3, 3), (40, 8)]
 # (new tokens, positions with them)
