@@ -206,7 +206,7 @@ hipError_t launch_rotary_append(const RotaryAppendArgs& a, hipStream_t s)
 // Positions 0 .. rows - 1 of every head's keys and values, of every layer.  The list travels in the kernel's arguments: nothing is
 // allocated or staged, and a captured launch keeps its own.  A workgroup moves COPY_PIECE bytes of one (copy, layer), in which the runs
 // of the heads (rows * row_bytes each; one run where whole blocks are copied) follow each other.  Stores are nontemporal, loads are not: a
-// fork reads one source for every copy.  90 blocks of 1.3 MB in 8 layers, 1.9 GB moved: 362 us (5.2 TB/s; torch's copy of 2 GiB 4.9), with
+// fork reads one source for every copy.  90 blocks of 1.3 MB in 8 layers, 1.9 GB moved: 362 us (5.2 TB/s; a plain copy of 2 GiB 4.9), with
 // ordinary stores 369; 37 of 64 positions of a block to 8 others, 40 layers, 273 MB: 57 and 79 us.
 constexpr int COPY_MAX = 256, COPY_THREADS = 256, COPY_U = 16, COPY_PIECE = COPY_THREADS * COPY_U * 16;
 struct CopyList { BlockCopy c[COPY_MAX]; };
