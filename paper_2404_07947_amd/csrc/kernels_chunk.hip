@@ -7,7 +7,7 @@
 //  * chunk_tile_kernel: 64 or 128 rows a workgroup.  Bound by MFMAs and softmax, which overlap in part; with few rows to a sequence and
 //    many heads by the cache, again.
 //  * chunk_join_stream_kernel, chunk_join_tile_kernel: where the keys of a tile were cut into parts for several workgroups, add them up.
-//  * chunk_row: a wave per row, for rows that a hidden infinity or NaN has spoilt.
+//  * chunk_row: a wave per row, for rows that a hidden infinity or NaN has spoilt, or whose sums passed a float's end.
 // All hold scores and softmax in float, with the running maximum and sum of one pass over the keys.  Which run is chunk_plan's choice,
 // from what the host knows (bounds of the lengths); which sequence is whose, and how many parts a tile has, each kernel finds from the
 // lengths on the device, so that a captured launch follows them.
@@ -36,6 +36,8 @@ __device__ __forceinline__ int table_limit(const PagedTable& t)
 
 // One query row by one wave over keys first .. last - 1, 64 at a time: a lane takes a key for the scores, and features lane, lane + 64
 // of the result.  kv: this head's keys of block 0; rows of a block's values lie v_off elements behind its keys; sc: the scale for exp2.
+// acc is the mean over the keys so far, not their sum: it stays within the values' range, where the sum of some hundred values near a float's
+// end does not.  A factor a step more, and 3 half steps of rounding for each 64 keys.
 template <typename T, int DH>
 __device__ __forceinline__ void chunk_row(const T* q, const T* kv, int64_t block_elems, int64_t v_off, const PagedTable& tbl, int b, KeyRange r, float sc,
                                           int lane, T* out)
@@ -54,10 +56,12 @@ __device__ __forceinline__ void chunk_row(const T* q, const T* kv, int64_t block
         for (int e = 0; e < DH; ++e) s = fmaf(to_f32(q[e]), to_f32(k[e]), s);
         s = j < r.last ? s * sc : -INFINITY;
         float mx = wave_max(fmaxf(m, s)), mref = mx == -INFINITY ? 0.f : mx;
-        float alpha = fast_exp2(m - mref), p = fast_exp2(s - mref);
-        l = l * alpha + wave_sum(p);
+        float old = l * fast_exp2(m - mref), p = fast_exp2(s - mref);
+        l = old + wave_sum(p);
+        const float inv = l > 0.f ? 1.f / l : 0.f, keep = old * inv;
+        p *= inv;
 #pragma unroll
-        for (int f = 0; f < DH / 64; ++f) acc[f] *= alpha;
+        for (int f = 0; f < DH / 64; ++f) acc[f] *= keep;
         for (int t = 0; t < cnt; ++t) {
             float pt = __shfl(p, t, WAVE);
             const T* v = kv + __shfl(at, t, WAVE) + v_off + lane;
@@ -68,7 +72,7 @@ __device__ __forceinline__ void chunk_row(const T* q, const T* kv, int64_t block
     }
     if (__builtin_amdgcn_ballot_w64(bad)) l = NAN;
 #pragma unroll
-    for (int f = 0; f < DH / 64; ++f) out[lane + f * 64] = from_f32<T>(r.last > r.first ? acc[f] / l : 0.f);
+    for (int f = 0; f < DH / 64; ++f) out[lane + f * 64] = from_f32<T>(r.last <= r.first ? 0.f : l > 0.f ? acc[f] : NAN);
 }
 
 // ---------------------------------------------------------------- what the kernels share
@@ -95,6 +99,10 @@ struct ChunkKernelArgs {
     }
 };
 
+// Rows whose results are not finite are computed again from their own keys: 0 times the infinite or NaN value of a key that the mask hides is
+// NaN, and sums, of probabilities up to 2^8 here, pass a float's end where their mean does not.  most: the largest magnitude, or NaN.
+__device__ __forceinline__ float magnitude(float most, float v) { return __builtin_elementwise_maximum(most, fabsf(v)); }
+__device__ __forceinline__ bool not_finite(float most) { return !(most < INFINITY); }
 // Row (t, h) of sequence b, by one wave (see chunk_row)
 template <typename T, int DH> __device__ __forceinline__ void row_again(const ChunkKernelArgs& a, int b, int t, int h, KeyRange r, int lane)
 {
@@ -479,10 +487,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void chunk_stream_kernel(ChunkKernel
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     v[f][e] = ks.last > ks.first ? v[f][e] * inv : 0.f;
-                    most = __builtin_elementwise_maximum(most, v[f][e]);
+                    most = magnitude(most, v[f][e]);
                 }
-            // 0 times the infinite or NaN value of a key that the mask hides is NaN: such a row is computed again from its own keys
-            unsigned long long again = __builtin_amdgcn_ballot_w64(write && most != most);
+            const unsigned long long again = __builtin_amdgcn_ballot_w64(write && not_finite(most));
             if (write && !(again >> (lane & 48) & 0xffff)) {
 #pragma unroll
                 for (int f = 0; f < DH / 64; ++f) {
@@ -800,10 +807,9 @@ __global__ __launch_bounds__(CT_WAVES * 64, (ct_per_cu<T, DH, QB>())) void chunk
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 o[qb][dt][e] = any ? o[qb][dt][e] * inv : 0.f;
-                most = __builtin_elementwise_maximum(most, o[qb][dt][e]);
+                most = magnitude(most, o[qb][dt][e]);
             }
-        // 0 times the infinite or NaN value of a key that the mask hides is NaN: such a row is computed again from its own keys
-        unsigned long long lanes = __builtin_amdgcn_ballot_w64(write && most != most);
+        const unsigned long long lanes = __builtin_amdgcn_ballot_w64(write && not_finite(most));
         unsigned again = (unsigned)(lanes | lanes >> 32);
         again = (again | again >> 16) & 0xffff;                        // bit qi: row w0 + 16 * qb + qi
         if (write && !(again >> qi & 1)) {
@@ -860,9 +866,9 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             v[e] = ks.last > ks.first ? v[e] / L : 0.f;
-            most = __builtin_elementwise_maximum(most, v[e]);
+            most = magnitude(most, v[e]);
         }
-        if (__builtin_amdgcn_ballot_w64(most != most)) {               // as in the kernels above
+        if (__builtin_amdgcn_ballot_w64(not_finite(most))) {
             row_again<T, DH>(a, b, t, h, ks, lane);
         } else if (sub == 0) {
             typename Vec4<T>::type y;
@@ -919,10 +925,10 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void chunk_join_
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         v[e] = ks.last > ks.first ? v[e] / L : 0.f;
-        most = __builtin_elementwise_maximum(most, v[e]);
+        most = magnitude(most, v[e]);
     }
-    // as in the kernels above; the rows of a wave are whole ones
-    const unsigned long long again = __builtin_amdgcn_ballot_w64(live && most != most);
+    // the rows of a wave are whole ones
+    const unsigned long long again = __builtin_amdgcn_ballot_w64(live && not_finite(most));
     const unsigned long long mine = PER == 32 ? 0xffffffffull << (lane & 32) : 0xffffull << (lane & 48);
     if (live && !(again & mine)) {
         typename Vec4<T>::type x;
