@@ -131,12 +131,13 @@ __device__ __forceinline__ KeyRange part_of(KeyRange k, const ChunkKernelArgs::C
     return KeyRange{first, part + 1 < parts ? first + cut.keys : k.last};
 }
 
-// What the loads of a position without a block read in its place, 16 rows: NaN keys make the scores of the rows that see it NaN.
-struct NanRows {
-    uint32_t v[16 * 512 / 4];
-    constexpr NanRows() : v() { for (uint32_t& x : v) x = 0xffffffffu; }
+// What the loads of a position without a block read in its place, 16 rows each: NaN keys make the scores of the rows that see it NaN,
+// values of 0 leave the others as they are.  (Tiles reach up to 63 positions in front of a window, where pages may have been given back.)
+struct NoBlock {
+    uint32_t keys[16 * 512 / 4], values[16 * 512 / 4];
+    constexpr NoBlock() : keys(), values() { for (uint32_t& x : keys) x = 0xffffffffu; }
 };
-static __device__ const __align__(16) NanRows no_block;
+static __device__ const __align__(16) NoBlock no_block;
 
 template <int N> __device__ __forceinline__ void wait_loads()        // all but the last N
 {
@@ -172,13 +173,13 @@ template <typename T, int DH, bool NT> struct RowLoader {
         const int j0 = j < last ? j : last - 1, j1 = j + 8 < last ? j + 8 : last - 1, i0 = j0 >> shift, i1 = j1 >> shift;
         return Entries{entry[i0 < max_blocks ? i0 : max_blocks - 1], entry[i1 < max_blocks ? i1 : max_blocks - 1]};
     }
-    // Where the keys of a position lie, and its value behind them (0 for NaN rows).
+    // Where the key of a position lies, and how far behind it its value.
     struct Row { const char* key; int64_t value; };
     __device__ __forceinline__ Row row(int e, int pos) const
     {
         const bool ok = (unsigned)e < (unsigned)n_blocks && pos < limit;
         const uint64_t at = (uint64_t)(unsigned)e * block_bytes + (unsigned)((pos & ((1 << shift) - 1)) * RB);
-        return Row{ok ? kv + at : (const char*)no_block.v, ok ? v_off : 0};
+        return Row{ok ? kv + at : (const char*)no_block.keys, ok ? v_off : (int64_t)sizeof(no_block.keys)};
     }
     struct Rows { Row r0, r1; };          // of positions j .. j + 7 and j + 8 .. j + 15; of the last one where those are beyond it
     __device__ __forceinline__ Rows rows(int j, Entries en) const
