@@ -424,7 +424,8 @@ int exe_probe_ingest(void* hip_stream, int32_t mode, uint64_t region_bytes, int3
  * Hkv = H.  The new tokens of n_seqs sequences lie packed: those of sequence b are rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1
  * (cu_seqlens [n_seqs + 1], DEVICE, from 0, not falling; a sequence may have none), and len[b] (device) counts b's positions
  * with them, so row cu_seqlens[b] + i has position p = len[b] - n + i of n.  block_table [n_seqs, max_blocks] device; T: rows of the
- * packed arrays, no less than cu_seqlens[n_seqs].  Rows behind the last sequence are neither read nor written.
+ * packed arrays, no less than cu_seqlens[n_seqs].  Rows behind the last sequence are neither read nor written.  Without rows or
+ * sequences a call does nothing, and its pointers may be NULL.
  * Lengths and tables stay on the device, so that a captured graph can be replayed with others.  What they name is checked there: a
  * table entry outside of [0, n_blocks) and a position without an entry are never followed.  The calls allocate nothing and hold
  * nothing back; q, out, the cache and workspaces are 16-byte aligned; no block may be written twice by one call.

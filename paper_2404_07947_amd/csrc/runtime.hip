@@ -2362,12 +2362,14 @@ extern "C" int exe_op_rotary(void* hip_stream, int32_t dtype, int32_t T, const v
                              int64_t out_stride)
 {
     if (dtype != DT_F32 && dtype != DT_BF16) return fail(EXE_ERR_ARG, "bad dtype");
-    if (T < 0 || heads < 1 || !x || !out || !pos || (rot > 0 && !inv_freq)) return fail(EXE_ERR_ARG, "bad rotary arguments");
+    if (T < 0 || heads < 1) return fail(EXE_ERR_ARG, "bad rotary arguments");
     if (dh != 64 && dh != 128) return fail(EXE_ERR_SHAPE, "head_dim must be 64 or 128");
     if (rot < 0 || rot > dh || rot % 2) return fail(EXE_ERR_SHAPE, "cannot turn %d of %d elements", rot, dh);
     if (interleaved != 0 && interleaved != 1) return fail(EXE_ERR_ARG, "interleaved must be 0 or 1");
     if ((int64_t)heads * dh > 0x7fffffff) return fail(EXE_ERR_SHAPE, "%d heads in a row", heads);
     if (x_stride < (int64_t)heads * dh || out_stride < (int64_t)heads * dh) return fail(EXE_ERR_SHAPE, "rows of %d heads overlap", heads);
+    if (T == 0) return EXE_OK;             // empty arrays have no address
+    if (!x || !out || !pos || (rot > 0 && !inv_freq)) return fail(EXE_ERR_ARG, "bad rotary arguments");
     if (x == out && x_stride != out_stride) return fail(EXE_ERR_ARG, "in place, both strides must be the same");
     if ((uintptr_t)x % esz_of_dtype(dtype) || (uintptr_t)out % esz_of_dtype(dtype)) return fail(EXE_ERR_ARG, "operands must be aligned to their type");
     RotaryArgs a{dtype, T, heads, dh, rot, interleaved, x, x_stride, pos, inv_freq, amplitude, out, out_stride};
@@ -2383,12 +2385,13 @@ extern "C" int exe_op_rotary_append_paged(void* hip_stream, int32_t dtype, int32
 {
     int r = check_paged(dtype, dh, Hkv, n_blocks, max_blocks, block_size);
     if (r) return r;
-    if (n_seqs < 0 || T < 0 || H < 0 || !cu_seqlens || !qkv || !kv_blocks || !block_table || !len || (rot > 0 && !inv_freq))
-        return fail(EXE_ERR_ARG, "bad rotary append arguments");
+    if (n_seqs < 0 || T < 0 || H < 0) return fail(EXE_ERR_ARG, "bad rotary append arguments");
     if (rot < 0 || rot > dh || rot % 2) return fail(EXE_ERR_SHAPE, "cannot turn %d of %d elements", rot, dh);
     if (interleaved != 0 && interleaved != 1) return fail(EXE_ERR_ARG, "interleaved must be 0 or 1");
     if (((int64_t)H + 2 * (int64_t)Hkv) * dh > 0x7fffffff) return fail(EXE_ERR_SHAPE, "%d and %d heads in a row", H, Hkv);
     if (row_stride < ((int64_t)H + 2 * (int64_t)Hkv) * dh || (q_out && q_out_stride < (int64_t)H * dh)) return fail(EXE_ERR_SHAPE, "rows overlap");
+    if (n_seqs == 0 || T == 0) return EXE_OK;
+    if (!cu_seqlens || !qkv || !kv_blocks || !block_table || !len || (rot > 0 && !inv_freq)) return fail(EXE_ERR_ARG, "bad rotary append arguments");
     if (q_out == qkv && q_out_stride != row_stride) return fail(EXE_ERR_ARG, "in place, both strides must be the same");
     if ((uintptr_t)kv_blocks & 15) return fail(EXE_ERR_ARG, "the cache must be 16-byte aligned");
     if ((uintptr_t)qkv % esz_of_dtype(dtype) || (uintptr_t)q_out % esz_of_dtype(dtype)) return fail(EXE_ERR_ARG, "operands must be aligned to their type");
@@ -2422,17 +2425,19 @@ extern "C" int exe_op_chunk_attention_paged(void* hip_stream, int32_t dtype, int
 {
     int r = check_paged(dtype, dh, Hkv, n_blocks, max_blocks, block_size);
     if (r) return r;
-    if (n_seqs < 0 || T < 0 || !cu_seqlens || !q || !kv_blocks || !block_table || !len || !out) return fail(EXE_ERR_ARG, "bad chunk attention arguments");
-    if (max_new < 1 || max_len < 1 || window < 0) return fail(EXE_ERR_ARG, "max_new %d, max_len %d, window %d", max_new, max_len, window);
+    if (n_seqs < 0 || T < 0) return fail(EXE_ERR_ARG, "bad chunk attention arguments");
+    const int least = n_seqs > 0 && T > 0;                               // the longest of no chunks is 0
+    if (max_new < least || max_len < least || window < 0) return fail(EXE_ERR_ARG, "max_new %d, max_len %d, window %d", max_new, max_len, window);
     if (H < Hkv || H % Hkv) return fail(EXE_ERR_SHAPE, "%d query heads over %d key/value heads", H, Hkv);
     if ((int64_t)T * H > 0x7fffffff || (int64_t)H * dh > 0x7fffffff) return fail(EXE_ERR_SHAPE, "%d rows of %d heads", T, H);
     const int esz = esz_of_dtype(dtype);
     if (q_stride < (int64_t)H * dh || out_stride < (int64_t)H * dh) return fail(EXE_ERR_SHAPE, "rows of %d heads overlap", H);
     if (q_stride * esz % 16 || out_stride * esz % 16) return fail(EXE_ERR_SHAPE, "rows must begin on 16 bytes");
+    if (!least) return EXE_OK;
+    if (!cu_seqlens || !q || !kv_blocks || !block_table || !len || !out) return fail(EXE_ERR_ARG, "bad chunk attention arguments");
     const void* ptrs[] = {q, kv_blocks, out, workspace};
     for (const void* p : ptrs)
         if ((uintptr_t)p & 15) return fail(EXE_ERR_ARG, "operands must be 16-byte aligned");
-    if (n_seqs == 0 || T == 0) return EXE_OK;
     if (q == out) return fail(EXE_ERR_ARG, "rows of q are read after others of out are written: they cannot be the same");
     ChunkAttnArgs a = chunk_args(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window);
     uint64_t need = chunk_attn_workspace(a);
