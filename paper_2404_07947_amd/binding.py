@@ -562,12 +562,18 @@ def exe_op_chunk_attention_paged_workspace(dtype, n_seqs, T, max_new, max_len, H
 
 
 def exe_op_chunk_attention_paged(dtype, n_seqs, cu_seqlens, T, max_new, q, q_stride, kv_blocks, n_blocks, block_table, max_blocks, block_size,
-                                 length, max_len, H, Hkv, dh, scale, window, out, out_stride, workspace=None, stream=None):
+                                 length, max_len, H, Hkv, dh, scale, window, out, out_stride, workspace=None, stream=None, ws_bytes=None):
+    """workspace: a device tensor, or an address and ws_bytes."""
     dev, s = _where(stream)
-    ws_bytes = 0
-    if workspace is not None:
+    if workspace is None:
+        ws_bytes = 0
+    elif isinstance(workspace, int):
+        assert ws_bytes is not None and ws_bytes >= 0, "an address needs its size, ws_bytes"
+    else:
         assert workspace.get_device() == dev, "expected a workspace on the current device"
-        ws_bytes = workspace.numel() * workspace.element_size()
+        have = workspace.numel() * workspace.element_size()
+        assert ws_bytes is None or 0 <= ws_bytes <= have, f"a workspace of {have} bytes"
+        ws_bytes = have if ws_bytes is None else ws_bytes
     block = 2 * Hkv * block_size * dh
     _check(lib().exe_op_chunk_attention_paged(s, dtype, n_seqs, _array(cu_seqlens, dev, "int32", n_seqs + 1), T, max_new,
                                               _rows(q, dev, dtype, T, H * dh, q_stride), q_stride,
