@@ -972,17 +972,21 @@ static ChunkKernelArgs::Cut cut_keys(int64_t wgs, int64_t max_len, int64_t want,
     return cut_to(parts, max_len, align);
 }
 
-// Parts for the tile kernel, of `rows` packed rows with `seen` keys each: those with which the chip is done first.  Time is counted in keys of
+// Parts for the tile kernel, of `tiles` workgroups with `seen` keys each: those with which the chip is done first.  Time is counted in keys of
 // a full CU: its `per_cu` workgroups take 2 of 10 shares together and 8 each by its own, and each part another 64 for its sums.  Joining
 // takes as long as 256 keys (7 us), of float ones 64.  2 x 512 tokens, 32 heads over 8 x 128, of 4096 keys are 256 workgroups: in 2 parts
 // 81 us, whole 98, in 3 parts, which a second round of workgroups has to take, 100; 1 x 512 behind 32000, 128 workgroups: 4 parts 258,
-// 5 parts 342.
-static ChunkKernelArgs::Cut cut_tiles(int64_t rows, int tile_rows, int per_cu, int64_t seen, int least, int each, int join)
+// 5 parts 342.  `tiles` are those of sequences of the mean length, the last one of each partly filled: as many as run where all bring the same,
+// about as many where they do not.  (Counted as if packed without gaps, us of then / now: 32 x 20 tokens of 40 heads over 2000 keys 306 / 251, 32 x 5
+// of 32 heads over 8, 4000 keys 115 / 103, 8 x 24 of 40 heads, 4000 keys 148 / 134; 10 x 20 to 90 of 16 heads over 4, 400 to 3000 keys 33.5 / 34.7.)
+// Beside the streaming kernel, which takes an unknown number of the sequences, they are counted packed: 23 single tokens and 3 x 8 to 26 of 16 heads
+// over 8 x 64, window 1000, 25.9, by the mean length of all 29.6.
+static ChunkKernelArgs::Cut cut_tiles(int64_t tiles, int per_cu, int64_t seen, int least, int each, int join)
 {
     const int64_t round = 256 * per_cu;
     int64_t parts = 1, best = 0;
     for (int64_t p = 1; p <= MAX_PARTS && (p == 1 || p <= ceil_div(seen, least)); ++p) {
-        const int64_t wgs = ceil_div(rows * p, tile_rows), left = ceil_div(wgs % round, 256);
+        const int64_t wgs = tiles * p, left = ceil_div(wgs % round, 256);
         if (p > 1 && wgs > 4 * round) break;
         const int64_t shares = wgs / round * 10 * per_cu + (left ? 2 * per_cu + 8 * left : 0);
         const int64_t time = shares * (ceil_div(seen, p) + (p > 1 ? each : 0)) + (p > 1 ? 10 * per_cu * join : 0);
@@ -1039,7 +1043,8 @@ static ChunkPlan chunk_plan(const ChunkAttnArgs& a)
         p.slots = T * G / (64 * p.qb) + a.n_seqs;
         const int per_cu = f32 ? a.dh == 128 ? ct_per_cu<float, 128, 1>() : ct_per_cu<float, 64, 1>()
                          : p.qb == 1 ? ct_per_cu<bf16_t, 128, 1>() : a.dh == 128 ? ct_per_cu<bf16_t, 128, 2>() : ct_per_cu<bf16_t, 64, 2>();
-        p.tile_cut = cut_tiles(T * G * a.Hkv, 64 * p.qb, per_cu, seen, f32 ? 128 : 256, f32 ? 32 : 64, f32 ? 64 : 256);
+        const int64_t seqs = p.stream ? 1 : a.n_seqs, tiles = seqs * ceil_div(ceil_div(T * G, seqs), 64 * p.qb) * a.Hkv;
+        p.tile_cut = cut_tiles(tiles, per_cu, seen, f32 ? 128 : 256, f32 ? 32 : 64, f32 ? 64 : 256);
     }
     // rows of the parts: those of the packed tokens, or see stream_row
     p.tile_cut.rows = T * a.H;
