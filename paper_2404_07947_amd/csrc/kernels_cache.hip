@@ -11,8 +11,9 @@ namespace exe {
 // Every head of a token is turned by the same rot / 2 <= 64 angles, so a wave takes one token (or a part of its heads), makes an angle a
 // lane, and goes over its heads with the sines and cosines in LDS: per 32 bytes moved a lane then spends its time on memory alone.
 // Angles are made in turns, in 64 bits with the products' rounding errors carried along (a position of 2^31 keeps its angle to 1e-15), cut
-// to an eighth of a turn either side of a quarter, and only then rounded to float: the sine's error is 3e-8 at most wherever the
-// position is.  (A float angle is 0.06 off at position 10^6.)
+// to an eighth of a turn either side of a quarter, and only then rounded to float: wherever the position is, that moves the angle by
+// 2 pi 2^-28 = 2.3e-8 at most, to which the sine and cosine add their own rounding (2^-25 and more; together 6.7e-8 at most over 2^22 angles).
+// (A float angle is 0.06 off at position 10^6.)
 __device__ __forceinline__ float2 rotary_cs(int pos, double freq, float amplitude)
 {
     constexpr double INV = 0.15915494309189535, INV_LO = -9.839338337591474e-18;       // 1 / 2 pi
