@@ -435,7 +435,9 @@ int exe_probe_ingest(void* hip_stream, int32_t mode, uint64_t region_bytes, int3
  *   EXE_ROPE_LINEAR: every frequency / factor;   EXE_ROPE_BASE: base * factor^(rot / (rot - 2)), which leaves the fastest pair and
  *   divides the slowest by factor;   EXE_ROPE_RAMP: a pair that makes turns_fast turns or more over original_positions is left, one
  *   of turns_slow or fewer divided by factor, linear in its turns between.
- * *amplitude: 0.1 ln(factor) + 1 for EXE_ROPE_RAMP with factor > 1, else 1.  Arguments that a scaling does not name are not read. */
+ * *amplitude: 0.1 ln(factor) + 1 for EXE_ROPE_RAMP with factor > 1, else 1.  Arguments that a scaling does not name are not read.
+ * Weights that were trained with another rule (a ramp linear in the pair's index, corners rounded to whole pairs, no amplitude) want a
+ * table of their own: the calls below take any. */
 int exe_rotary_frequencies(int32_t rot, double base, int32_t scaling, double factor, int32_t original_positions, double turns_slow,
                            double turns_fast, double* inv_freq, float* amplitude);
 /* Turns heads of rows x [T, heads * dh] (dtype, rows x_stride elements apart): of the first rot elements of a head (even, 0 .. dh)
@@ -454,11 +456,18 @@ int exe_op_rotary_append_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, 
                                int32_t max_blocks, int32_t block_size, const int32_t* len, void* q_out, int64_t q_out_stride);
 /* Attention of the new tokens over the cache, which holds them already: row t of q [T, H * dh] (rows q_stride elements apart,
  * multiples of 16 bytes) at position p sees keys 0 .. p, of these the last `window` if window > 0.  out [T, H * dh], rows out_stride
- * apart, not q.  A row that sees no key (p < 0) is 0; one that would read a position without a block is NaN.  Scores and softmax in
- * float; the probabilities are rounded to the storage type for the product with the values, the result once more.
+ * apart, not q.  A row that sees no key (p < 0) is 0; one that would read a position without a block is NaN.  Positions in front of the
+ * window need no block.  Scores and softmax in float; the result is rounded to the storage type.
  * max_new (tokens of the longest chunk) and max_len (the largest len) size the launch and the workspace; where they are wrong, it is
- * slower, not wrong.  workspace: exe_op_chunk_attention_paged_workspace bytes (0 for bad arguments), NULL if that is 0; nothing in it
- * needs clearing; calls that may overlap need one each. */
+ * slower, not wrong.  With n_seqs, T and the heads they choose the kernel, and so the order of sums and, in bf16, the bits with which a
+ * probability enters the product with the values: 8 (one rounding to bf16, as the result has) in the kernel of many rows, 16 in that of
+ * small calls and of sequences with up to 16 rows to a key/value head.  Equal arguments give equal bits.
+ * A row whose result is not finite although its scores are (infinite or NaN values among the keys that it sees or that a tile reads
+ * beside them, sums beyond a float's end) is computed once more, key by key, which takes 30 to 170 times as long where all rows are such.
+ * One new token a sequence and Hkv == H: exe_op_decode_attention_paged does the same without a workspace, and is the faster call but for
+ * few, long sequences (us, that one first: bf16 x 128, 40 heads, 1 x 576 keys 9.0 and 10.4, 256 x 60 to 300 140 and 159, 1 x 4000 42 and 20).
+ * workspace: exe_op_chunk_attention_paged_workspace bytes (0 for bad arguments), NULL if that is 0; nothing in it needs clearing; calls
+ * that may overlap need one each. */
 int exe_op_chunk_attention_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, const int32_t* cu_seqlens, int32_t T, int32_t max_new,
                                  const void* q, int64_t q_stride, const void* kv_blocks, int32_t n_blocks, const int32_t* block_table,
                                  int32_t max_blocks, int32_t block_size, const int32_t* len, int32_t max_len, int32_t H, int32_t Hkv,

@@ -300,8 +300,11 @@ __device__ __forceinline__ float exponent_scale(float scale) { return scale == 0
 // the rest is computed on.  (4 waves a CU with 32 KB each took 230 us where 8 take 182: a step is 400 instructions, most of them not
 // the matrix's.)  Per step and wave: S^T = K . Q^T and O^T += V^T . P^T by MFMAs with the 16 rows as columns (see prefill_mfma_kernel);
 // idle columns cost nothing that the loads do not hide.  Probabilities enter the second product as two bf16 parts, 2^-17 relative.
-// Bound by memory.  Nontemporal loads: 200 -> 182 us for 64 sequences of 500 to 8100 keys, 8 heads x 128 (1.1 GB, 6.1 TB/s); of 4096 keys
-// each 161 us (6.66 TB/s, where a plain read reaches 7.1): the difference is the cut into parts, which lengths that differ want.
+// Bound by memory where contexts are long.  Nontemporal loads: 200 -> 182 us for 64 sequences of 500 to 8100 keys, 8 heads x 128 (1.1 GB, 6.1 TB/s); of
+// 4096 keys each 169 us (6.34 TB/s; whole 161, 6.66, where a plain read reaches 7.1): the cut into parts, which lengths that differ want, costs
+// 5 %.  Shorter ones pay the start of a workgroup (5.4 us with 16 keys) in each of up to four rounds, and the join: 200 to 2000 keys
+// 56 us, 5.1 TB/s, 100 to 1024 38 us, 4.0 TB/s; 64-wide heads of 500 to 4000 69 us, 4.7 TB/s.  Float, 500 to 4000 keys: x 64 116 us, 5.6 TB/s, x 128
+// (4 waves a CU) 293 us, 4.4 TB/s.
 constexpr int ST_WAVES = 4, ST_STEP = 16;
 template <typename T, int DH, int WAVES> struct Stream {
     static constexpr int RB = DH * (int)sizeof(T), TILE = ST_STEP * RB, STAGE = 2 * TILE;
