@@ -454,6 +454,21 @@ int exe_op_rotary_append_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, 
                                int64_t row_stride, int32_t H, int32_t Hkv, int32_t dh, int32_t rot, int32_t interleaved, const int32_t* pos,
                                const double* inv_freq, float amplitude, void* kv_blocks, int32_t n_blocks, const int32_t* block_table,
                                int32_t max_blocks, int32_t block_size, const int32_t* len, void* q_out, int64_t q_out_stride);
+/* Norms of heads and exe_op_rotary in one pass: every head x of a row becomes gain * (x - mean) / sqrt(mean((x - mean)^2) + eps)
+ * (LayerNorm without a shift), or with rms 1 the same without the means (RMSNorm), and is then turned as by exe_op_rotary (rot 0: not at
+ * all; pos and inv_freq may be NULL).  gain: dtype, [dh] for all heads or, with gain_per_head 1, [heads, dh] (so that queries and keys, side
+ * by side in a row, go in one call); NULL: 1.  eps >= 0, added to the mean of squares: a head of zeros with eps 0 is NaN.  A head with a NaN is NaN, and so is,
+ * without the mean, the infinite element of a head, whose other elements are 0.  In float, rounded once; in place as exe_op_rotary. */
+int exe_op_head_norm_rotary(void* hip_stream, int32_t dtype, int32_t T, const void* x, int64_t x_stride, int32_t heads, int32_t dh, int32_t rms,
+                            const void* gain, int32_t gain_per_head, float eps, int32_t rot, int32_t interleaved, const int32_t* pos,
+                            const double* inv_freq, float amplitude, void* out, int64_t out_stride);
+/* exe_op_rotary_append_paged with the norms of queries (q_gain [dh] or [H, dh]) and keys (k_gain [dh] or [Hkv, dh]) in front of the turn;
+ * values are stored as they are. */
+int exe_op_head_norm_rotary_append_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, const int32_t* cu_seqlens, int32_t T, const void* qkv,
+                                         int64_t row_stride, int32_t H, int32_t Hkv, int32_t dh, int32_t rms, const void* q_gain, const void* k_gain,
+                                         int32_t gain_per_head, float eps, int32_t rot, int32_t interleaved, const int32_t* pos,
+                                         const double* inv_freq, float amplitude, void* kv_blocks, int32_t n_blocks, const int32_t* block_table,
+                                         int32_t max_blocks, int32_t block_size, const int32_t* len, void* q_out, int64_t q_out_stride);
 /* Attention of the new tokens over the cache, which holds them already: row t of q [T, H * dh] (rows q_stride elements apart,
  * multiples of 16 bytes) at position p sees keys 0 .. p, of these the last `window` if window > 0.  out [T, H * dh], rows out_stride
  * apart, not q.  A row that sees no key (p < 0) is 0; one that would read a position without a block is NaN.  Positions in front of the
@@ -482,6 +497,21 @@ int exe_op_kv_copy_blocks(void* hip_stream, int32_t dtype, void* kv_blocks, int3
                           int32_t dh, int32_t n_copies, const int32_t* copies);
 /* argmax over each row of float logits [rows, n] -> int32 out [rows]; lowest index on ties */
 int exe_op_argmax(void* hip_stream, const float* logits, int32_t rows, int32_t n, int32_t* out);
+/* Log probabilities, p = softmax(scale * logits) row by row: rows of n logits (dtype, row_stride elements apart, aligned to their type),
+ * scale > 0 (one over a temperature).
+ *  logprobs [rows, n_tokens] float: ln p of tokens [rows, n_tokens] (int32, device); a token outside of 0 .. n - 1 is never looked up, and NaN.
+ *  entropy [rows] float, nullable: -sum p ln p.
+ *  top_ids [rows, top_k] int32, top_logprobs [rows, top_k] float: the top_k (0 .. 64, at most n) largest logits, largest first, the lowest
+ *  index on ties, and their ln p.  Logits of minus infinity are ruled out: their p is 0, they are no alternatives, and where fewer than
+ *  top_k are left the rest is -1 and minus infinity.  A NaN is never an alternative either.
+ * Log probabilities and entropy of a row with a NaN or plus infinity, or without any number above minus infinity, are NaN; those of alternatives
+ * that are there too.  Sums in float; each row's results depend on that row alone.  What is not asked for (n_tokens 0, top_k 0) may be NULL.
+ * workspace: exe_op_logprobs_workspace bytes (0 for bad arguments; it covers any alignment), 16-byte aligned, NULL if that is 0; nothing in it needs clearing; calls that may
+ * overlap need one each. */
+int exe_op_logprobs(void* hip_stream, int32_t dtype, const void* logits, int64_t row_stride, int32_t rows, int32_t n, float scale,
+                    const int32_t* tokens, int32_t n_tokens, float* logprobs, float* entropy, int32_t top_k, int32_t* top_ids, float* top_logprobs,
+                    void* workspace, uint64_t workspace_bytes);
+uint64_t exe_op_logprobs_workspace(int32_t dtype, int32_t rows, int32_t n, int32_t top_k);
 /* T5 bucket of rel = key - query as this library computes it (host function, exact integer arithmetic) */
 int exe_rel_bucket(int32_t rel, int32_t bidirectional, int32_t n_buckets, int32_t max_dist);
 

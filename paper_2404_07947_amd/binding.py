@@ -16,7 +16,7 @@ DECLARED_SYMBOLS = [
     "exe_expected_weights", "exe_model_load", "exe_model_free", "exe_encode", "exe_decode_step",
     "exe_seq_release", "exe_seq_length", "exe_kv_stats", "exe_seq_export_bytes", "exe_seq_export", "exe_seq_import", "exe_seq_reserve", "exe_seq_fork", "exe_kv_compact", "exe_profile", "exe_run_rra", "exe_kernel_timing",
     "exe_kernel_times", "exe_op_gemm", "exe_op_gemm_workspace", "exe_op_gemm_plan", "exe_op_gemm_model_plan", "exe_op_gemm_kv_plan", "exe_op_kv_store_index", "exe_op_gemm_stream", "exe_op_gemm_model", "exe_op_gemm_ld", "exe_op_gemm_noalloc", "exe_op_gemm_noalloc_max_workspace", "exe_op_paged_index_check", "exe_op_norm", "exe_op_resid_norm", "exe_op_prefill_attention", "exe_op_prefill_tiles",
-    "exe_op_decode_attention", "exe_op_decode_attention_paged", "exe_probe_peaks", "exe_probe_ingest", "exe_rotary_frequencies", "exe_op_rotary", "exe_op_rotary_append_paged", "exe_op_chunk_attention_paged", "exe_op_chunk_attention_paged_workspace", "exe_op_kv_copy_blocks", "exe_op_argmax", "exe_rel_bucket", "exe_last_error", "exe_version",
+    "exe_op_decode_attention", "exe_op_decode_attention_paged", "exe_probe_peaks", "exe_probe_ingest", "exe_rotary_frequencies", "exe_op_rotary", "exe_op_rotary_append_paged", "exe_op_chunk_attention_paged", "exe_op_chunk_attention_paged_workspace", "exe_op_kv_copy_blocks", "exe_op_head_norm_rotary", "exe_op_head_norm_rotary_append_paged", "exe_op_logprobs", "exe_op_logprobs_workspace", "exe_op_argmax", "exe_rel_bucket", "exe_last_error", "exe_version",
     # exe_sched.h (host only)
     "exe_sim_completion", "exe_sim_step_ms", "exe_sim_rra", "exe_sim_waa", "exe_sched_search", "exe_sched_rra",
 ]
@@ -169,6 +169,12 @@ def lib():
     L.exe_op_chunk_attention_paged_workspace.argtypes = [i32] * 9
     L.exe_op_chunk_attention_paged_workspace.restype = C.c_uint64
     L.exe_op_kv_copy_blocks.argtypes = [vp, i32, vp, i32, i32, i32, i32, i32, i32, ip]
+    L.exe_op_head_norm_rotary.argtypes = [vp, i32, i32, vp, i64, i32, i32, i32, vp, i32, C.c_float, i32, i32, vp, vp, C.c_float, vp, i64]
+    L.exe_op_head_norm_rotary_append_paged.argtypes = [vp, i32, i32, vp, i32, vp, i64, i32, i32, i32, i32, vp, vp, i32, C.c_float, i32, i32, vp, vp,
+                                                       C.c_float, vp, i32, vp, i32, i32, vp, vp, i64]
+    L.exe_op_logprobs.argtypes = [vp, i32, vp, i64, i32, i32, C.c_float, vp, i32, vp, vp, i32, vp, vp, vp, C.c_uint64]
+    L.exe_op_logprobs_workspace.argtypes = [i32] * 4
+    L.exe_op_logprobs_workspace.restype = C.c_uint64
     L.exe_op_argmax.argtypes = [vp, vp, i32, i32, vp]
     L.exe_rel_bucket.argtypes = [i32, i32, i32, i32]
     L.exe_last_error.restype = C.c_char_p
@@ -557,6 +563,48 @@ def exe_op_rotary_append_paged(dtype, n_seqs, cu_seqlens, T, qkv, row_stride, H,
                                             _array(length, dev, "int32", n_seqs), _rows(q_out, dev, dtype, T, H * dh, q_out_stride), q_out_stride))
 
 
+def _kind(dtype: int) -> str:
+    return "bfloat16" if dtype else "float32"
+
+
+def exe_op_head_norm_rotary(dtype, T, x, x_stride, heads, dh, rms, gain, gain_per_head, eps, rot, interleaved, pos, inv_freq, amplitude, out,
+                            out_stride, stream=None):
+    """x and out: as exe_op_rotary takes them; gain: [dh] or [heads, dh] of the storage type, or None."""
+    dev, s = _where(stream)
+    _check(lib().exe_op_head_norm_rotary(s, dtype, T, _rows(x, dev, dtype, T, heads * dh, x_stride), x_stride, heads, dh, rms,
+                                         _array(gain, dev, _kind(dtype), heads * dh if gain_per_head else dh), gain_per_head, eps, rot, interleaved,
+                                         _array(pos, dev, "int32", T), _array(inv_freq, dev, "float64", rot // 2), amplitude,
+                                         _rows(out, dev, dtype, T, heads * dh, out_stride), out_stride))
+
+
+def exe_op_head_norm_rotary_append_paged(dtype, n_seqs, cu_seqlens, T, qkv, row_stride, H, Hkv, dh, rms, q_gain, k_gain, gain_per_head, eps, rot,
+                                         interleaved, pos, inv_freq, amplitude, kv_blocks, n_blocks, block_table, max_blocks, block_size, length,
+                                         q_out, q_out_stride, stream=None):
+    dev, s = _where(stream)
+    block = 2 * Hkv * block_size * dh
+    _check(lib().exe_op_head_norm_rotary_append_paged(s, dtype, n_seqs, _array(cu_seqlens, dev, "int32", n_seqs + 1), T,
+                                                      _rows(qkv, dev, dtype, T, (H + 2 * Hkv) * dh, row_stride), row_stride, H, Hkv, dh, rms,
+                                                      _array(q_gain, dev, _kind(dtype), H * dh if gain_per_head else dh),
+                                                      _array(k_gain, dev, _kind(dtype), Hkv * dh if gain_per_head else dh), gain_per_head, eps, rot,
+                                                      interleaved, _array(pos, dev, "int32", T), _array(inv_freq, dev, "float64", rot // 2), amplitude,
+                                                      _rows(kv_blocks, dev, dtype, n_blocks, block, block), n_blocks,
+                                                      _array(block_table, dev, "int32", n_seqs * max_blocks), max_blocks, block_size,
+                                                      _array(length, dev, "int32", n_seqs), _rows(q_out, dev, dtype, T, H * dh, q_out_stride), q_out_stride))
+
+
+def _workspace(workspace, dev, ws_bytes):
+    """(address, bytes) of a device tensor, or of an address and its size."""
+    if workspace is None:
+        return None, 0
+    if isinstance(workspace, int):
+        assert ws_bytes is not None and ws_bytes >= 0, "an address needs its size, ws_bytes"
+        return workspace, ws_bytes
+    assert workspace.get_device() == dev, "expected a workspace on the current device"
+    have = workspace.numel() * workspace.element_size()
+    assert ws_bytes is None or 0 <= ws_bytes <= have, f"a workspace of {have} bytes"
+    return _dev(workspace), have if ws_bytes is None else ws_bytes
+
+
 def exe_op_chunk_attention_paged_workspace(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window=0) -> int:
     return int(lib().exe_op_chunk_attention_paged_workspace(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window))
 
@@ -610,6 +658,21 @@ def exe_probe_ingest(mode: int, region_bytes: int, passes: int, waves: int, load
     r = C.c_double()
     _check(L.exe_probe_ingest(_stream_ptr(stream), mode, region_bytes, passes, waves, loads_per_batch, row_bytes, C.byref(r)))
     return r.value
+
+
+def exe_op_logprobs_workspace(dtype, rows, n, top_k) -> int:
+    return int(lib().exe_op_logprobs_workspace(dtype, rows, n, top_k))
+
+
+def exe_op_logprobs(dtype, logits, row_stride, rows, n, scale, tokens, n_tokens, logprobs, entropy, top_k, top_ids, top_logprobs, workspace=None,
+                    stream=None, ws_bytes=None):
+    """logits: a device tensor (or address) whose rows are row_stride elements apart; workspace: a device tensor, or an address and ws_bytes."""
+    dev, s = _where(stream)
+    ws, ws_bytes = _workspace(workspace, dev, ws_bytes)
+    _check(lib().exe_op_logprobs(s, dtype, _rows(logits, dev, dtype, rows, n, row_stride), row_stride, rows, n, scale,
+                                 _array(tokens, dev, "int32", rows * n_tokens), n_tokens, _array(logprobs, dev, "float32", rows * n_tokens),
+                                 _array(entropy, dev, "float32", rows), top_k, _array(top_ids, dev, "int32", rows * top_k),
+                                 _array(top_logprobs, dev, "float32", rows * top_k), ws, ws_bytes))
 
 
 def exe_op_argmax(logits, rows, n, out, stream=None):

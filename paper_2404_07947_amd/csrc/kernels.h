@@ -171,6 +171,20 @@ hipError_t launch_kv_append_paged(int dtype, const void* src, int ld, int k_off,
 hipError_t launch_kv_rows(const int32_t* tok_b, const int32_t* tok_pos, const int64_t* base, const int32_t* cap, int T, int dh,
                           int64_t* row, int32_t* row_cap, hipStream_t s);
 hipError_t launch_argmax(const float* logits, int rows, int n, int32_t* out, hipStream_t s);
+// ---- log probabilities, entropy, largest probabilities of rows of logits (kernels_logprobs.hip)
+constexpr int LOGPROB_MAX_TOP = 64;
+struct LogprobArgs {
+    int dtype, rows, n;
+    const void* logits; int64_t row_stride;
+    float scale;
+    const int32_t* tokens; int n_tokens;   // [rows, n_tokens]
+    float *logprobs, *entropy;             // [rows, n_tokens]; [rows], nullable
+    int k;                                 // 0 .. LOGPROB_MAX_TOP
+    int32_t* top_ids; float* top_logprobs; // [rows, k]
+    void* workspace;                       // logprobs_workspace bytes
+};
+size_t logprobs_workspace(const LogprobArgs& a);      // of dtype, rows, n, k
+hipError_t launch_logprobs(const LogprobArgs& a, hipStream_t s);
 
 struct AttnCacheArgs {       // one query row per batch entry against that sequence's cached K/V
     int dtype, B, H, dh;
@@ -229,6 +243,24 @@ struct RotaryAppendArgs {    // rows [tokens, (H + 2 * Hkv) * dh]: queries, keys
     void* q_out; int64_t q_out_stride;     // nullable
 };
 hipError_t launch_rotary_append(const RotaryAppendArgs& a, hipStream_t s);
+struct HeadNormArgs {        // rows [tokens, H * dh] (H heads, gains of H), or with kv_blocks as those of RotaryAppendArgs
+    int dtype, tokens, H, Hkv, dh, rms;
+    const void *q_gain, *k_gain;           // [dh], or [heads, dh]; nullable: 1
+    int gain_per_head;
+    float eps;
+    int rot, interleaved;
+    const void* x; int64_t x_stride;
+    const int32_t* pos;
+    const double* inv_freq;
+    float amplitude;
+    void* out; int64_t out_stride;         // may be x; nullable with kv_blocks
+    int n_seqs;                            // from here on: with kv_blocks only
+    const int32_t* cu;
+    void* kv_blocks;
+    PagedTable table;
+    const int32_t* len;
+};
+hipError_t launch_head_norm(const HeadNormArgs& a, hipStream_t s);
 struct BlockCopy { int32_t src, dst, rows; };
 struct BlockCopyArgs {       // pool [layers][n_blocks][runs][block_rows] rows of row_bytes (a multiple of 16); a block less than 32 GB
     void* pool;

@@ -2401,6 +2401,66 @@ extern "C" int exe_op_rotary_append_paged(void* hip_stream, int32_t dtype, int32
     return EXE_OK;
 }
 
+// what both calls of head norms take
+static int check_head_norm(int rms, int gain_per_head, float eps, int dh, int rot, int interleaved)
+{
+    if (rms != 0 && rms != 1) return fail(EXE_ERR_ARG, "rms must be 0 or 1");
+    if (gain_per_head != 0 && gain_per_head != 1) return fail(EXE_ERR_ARG, "gain_per_head must be 0 or 1");
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(EXE_ERR_ARG, "an eps of %g", (double)eps);
+    if (rot < 0 || rot > dh || rot % 2) return fail(EXE_ERR_SHAPE, "cannot turn %d of %d elements", rot, dh);
+    if (interleaved != 0 && interleaved != 1) return fail(EXE_ERR_ARG, "interleaved must be 0 or 1");
+    return EXE_OK;
+}
+
+extern "C" int exe_op_head_norm_rotary(void* hip_stream, int32_t dtype, int32_t T, const void* x, int64_t x_stride, int32_t heads, int32_t dh,
+                                       int32_t rms, const void* gain, int32_t gain_per_head, float eps, int32_t rot, int32_t interleaved,
+                                       const int32_t* pos, const double* inv_freq, float amplitude, void* out, int64_t out_stride)
+{
+    if (dtype != DT_F32 && dtype != DT_BF16) return fail(EXE_ERR_ARG, "bad dtype");
+    if (T < 0 || heads < 1) return fail(EXE_ERR_ARG, "bad head norm arguments");
+    if (dh != 64 && dh != 128) return fail(EXE_ERR_SHAPE, "head_dim must be 64 or 128");
+    int r = check_head_norm(rms, gain_per_head, eps, dh, rot, interleaved);
+    if (r) return r;
+    if ((int64_t)heads * dh > 0x7fffffff) return fail(EXE_ERR_SHAPE, "%d heads in a row", heads);
+    if (x_stride < (int64_t)heads * dh || out_stride < (int64_t)heads * dh) return fail(EXE_ERR_SHAPE, "rows of %d heads overlap", heads);
+    if (T == 0) return EXE_OK;
+    if (!x || !out || (rot > 0 && (!pos || !inv_freq))) return fail(EXE_ERR_ARG, "bad head norm arguments");
+    if (x == out && x_stride != out_stride) return fail(EXE_ERR_ARG, "in place, both strides must be the same");
+    const void* ptrs[] = {x, out, gain};
+    for (const void* p : ptrs)
+        if ((uintptr_t)p % esz_of_dtype(dtype)) return fail(EXE_ERR_ARG, "operands must be aligned to their type");
+    HeadNormArgs a{dtype, T, heads, 0, dh, rms, gain, nullptr, gain_per_head, eps, rot, interleaved, x, x_stride, pos, inv_freq, amplitude, out, out_stride,
+                   0, nullptr, nullptr, PagedTable{}, nullptr};
+    HIP_TRY(launch_head_norm(a, (hipStream_t)hip_stream));
+    return EXE_OK;
+}
+
+extern "C" int exe_op_head_norm_rotary_append_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, const int32_t* cu_seqlens, int32_t T,
+                                                    const void* qkv, int64_t row_stride, int32_t H, int32_t Hkv, int32_t dh, int32_t rms,
+                                                    const void* q_gain, const void* k_gain, int32_t gain_per_head, float eps, int32_t rot,
+                                                    int32_t interleaved, const int32_t* pos, const double* inv_freq, float amplitude,
+                                                    void* kv_blocks, int32_t n_blocks, const int32_t* block_table, int32_t max_blocks,
+                                                    int32_t block_size, const int32_t* len, void* q_out, int64_t q_out_stride)
+{
+    int r = check_paged(dtype, dh, Hkv, n_blocks, max_blocks, block_size);
+    if (r) return r;
+    if (n_seqs < 0 || T < 0 || H < 0) return fail(EXE_ERR_ARG, "bad head norm arguments");
+    if ((r = check_head_norm(rms, gain_per_head, eps, dh, rot, interleaved))) return r;
+    if (((int64_t)H + 2 * (int64_t)Hkv) * dh > 0x7fffffff) return fail(EXE_ERR_SHAPE, "%d and %d heads in a row", H, Hkv);
+    if (row_stride < ((int64_t)H + 2 * (int64_t)Hkv) * dh || (q_out && q_out_stride < (int64_t)H * dh)) return fail(EXE_ERR_SHAPE, "rows overlap");
+    if (n_seqs == 0 || T == 0) return EXE_OK;
+    if (!cu_seqlens || !qkv || !kv_blocks || !block_table || !len || (rot > 0 && !inv_freq)) return fail(EXE_ERR_ARG, "bad head norm arguments");
+    if (q_out == qkv && q_out_stride != row_stride) return fail(EXE_ERR_ARG, "in place, both strides must be the same");
+    if ((uintptr_t)kv_blocks & 15) return fail(EXE_ERR_ARG, "the cache must be 16-byte aligned");
+    const void* ptrs[] = {qkv, q_out, q_gain, k_gain};
+    for (const void* p : ptrs)
+        if ((uintptr_t)p % esz_of_dtype(dtype)) return fail(EXE_ERR_ARG, "operands must be aligned to their type");
+    HeadNormArgs a{dtype, T, H, Hkv, dh, rms, q_gain, k_gain, gain_per_head, eps, rot, interleaved, qkv, row_stride, pos, inv_freq, amplitude, q_out,
+                   q_out_stride, n_seqs, cu_seqlens, kv_blocks, PagedTable{block_table, max_blocks, block_shift_of(block_size), n_blocks}, len};
+    HIP_TRY(launch_head_norm(a, (hipStream_t)hip_stream));
+    return EXE_OK;
+}
+
 static ChunkAttnArgs chunk_args(int dtype, int n_seqs, int T, int max_new, int max_len, int H, int Hkv, int dh, int window)
 {
     ChunkAttnArgs a{};
@@ -2494,5 +2554,33 @@ extern "C" int exe_op_argmax(void* hip_stream, const float* logits, int32_t rows
 {
     if (!logits || !out || rows < 0 || n < 1) return fail(EXE_ERR_ARG, "bad argmax arguments");
     HIP_TRY(launch_argmax(logits, rows, n, out, (hipStream_t)hip_stream));
+    return EXE_OK;
+}
+
+extern "C" uint64_t exe_op_logprobs_workspace(int32_t dtype, int32_t rows, int32_t n, int32_t top_k)
+{
+    if ((dtype != DT_F32 && dtype != DT_BF16) || rows < 1 || n < 1 || top_k < 0 || top_k > LOGPROB_MAX_TOP || top_k > n) return 0;
+    LogprobArgs a{};
+    a.dtype = dtype; a.rows = rows; a.n = n; a.k = top_k;
+    return logprobs_workspace(a);
+}
+
+extern "C" int exe_op_logprobs(void* hip_stream, int32_t dtype, const void* logits, int64_t row_stride, int32_t rows, int32_t n, float scale,
+                               const int32_t* tokens, int32_t n_tokens, float* logprobs, float* entropy, int32_t top_k, int32_t* top_ids,
+                               float* top_logprobs, void* workspace, uint64_t workspace_bytes)
+{
+    if (dtype != DT_F32 && dtype != DT_BF16) return fail(EXE_ERR_ARG, "bad dtype");
+    if (rows < 0 || n < 1 || n_tokens < 0) return fail(EXE_ERR_ARG, "bad log probability arguments");
+    if (top_k < 0 || top_k > LOGPROB_MAX_TOP || top_k > n) return fail(EXE_ERR_SHAPE, "%d alternatives of %d tokens", top_k, n);
+    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(EXE_ERR_ARG, "a scale of %g", (double)scale);
+    if (row_stride < n) return fail(EXE_ERR_SHAPE, "rows of %d logits overlap", n);
+    if (rows == 0) return EXE_OK;
+    if (!logits || (n_tokens > 0 && (!tokens || !logprobs)) || (top_k > 0 && (!top_ids || !top_logprobs))) return fail(EXE_ERR_ARG, "bad log probability arguments");
+    if ((uintptr_t)logits % esz_of_dtype(dtype)) return fail(EXE_ERR_ARG, "logits must be aligned to their type");
+    if ((uintptr_t)workspace & 15) return fail(EXE_ERR_ARG, "the workspace must be 16-byte aligned");
+    LogprobArgs a{dtype, rows, n, logits, row_stride, scale, tokens, n_tokens, logprobs, entropy, top_k, top_ids, top_logprobs, workspace};
+    const uint64_t need = logprobs_workspace(a);
+    if (need > (workspace ? workspace_bytes : 0)) return fail(EXE_ERR_ARG, "workspace too small (%llu bytes needed)", (unsigned long long)need);
+    HIP_TRY(launch_logprobs(a, (hipStream_t)hip_stream));
     return EXE_OK;
 }

@@ -1,0 +1,281 @@
+"""Norms of heads with rotary positions, alone and with the append of a chunk's keys and values, against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2404_07947_amd as exe
+from chunk_util import DEV, HALF, TYPES, U, Batch, turned
+
+pytestmark = pytest.mark.gpu
+
+
+def normed(x, gain, rms, eps):
+    """x [tokens, heads, dh] in 64 bits, and the bound.  The sum of 128 squares in float, 16 in a row at most and then by a tree: 16 + 7 half
+    steps, of which the root halves the share; the root's own 2 (one ulp), a product each for it and the gain: 16 together.  A mean adds the
+    rounding of x - mean twice and what the second mean is off by, 23 half steps of the mean magnitude of the deviations, which is 1 at most in
+    units of their root mean square; the same again goes through the sum of squares."""
+    x = x.double()
+    d = x if rms else x - x.mean(-1, keepdim=True)
+    y = d / torch.sqrt((d * d).mean(-1, keepdim=True) + eps) * gain
+    return y, U * (18 * y.abs() if rms else 48 * (y.abs() + gain.abs()))
+
+
+def normed_turned(x, gain, rms, eps, pos, f, amplitude, rot, interleaved):
+    y, e = normed(x, gain, rms, eps)
+    z, ez = turned(y, pos, f, amplitude, rot, interleaved)
+    # a turn takes the bound of a pair's elements along
+    a, b = (e[..., 0:rot:2], e[..., 1:rot:2]) if interleaved else (e[..., :rot // 2], e[..., rot // 2:rot])
+    both = (a + b) * abs(float(amplitude))
+    if interleaved:
+        e[..., 0:rot:2], e[..., 1:rot:2] = both, both
+    else:
+        e[..., :rot // 2], e[..., rot // 2:rot] = both, both
+    return z, e + ez
+
+
+def close(got, want, err, dtype):
+    got = got.cpu().double()
+    assert got.shape == want.shape and torch.equal(got.isnan(), want.isnan())          # a head without deviations, eps 0: 0 / 0
+    got, want, err = (torch.nan_to_num(v, nan=0.0) for v in (got, want, err))
+    over = (got - want).abs() - err - HALF[dtype] * (want.abs() + err) * (1 + 1e-6) - 1e-37
+    assert bool((over <= 0).all()), float(over.max())
+
+
+def freq(rot):
+    return torch.as_tensor(exe.exe_rotary_frequencies(rot)[0]) if rot else torch.zeros(0, dtype=torch.float64)
+
+
+def call(x, heads, dh, rms, gain, per_head, eps, rot, il, pos, f, amplitude, out=None):
+    out = torch.full_like(x, 7.0) if out is None else out
+    exe.exe_op_head_norm_rotary(0 if x.dtype == torch.float32 else 1, x.shape[0], x, x.stride(0), heads, dh, rms, gain, per_head, eps, rot, il, pos,
+                                f, amplitude, out, out.stride(0))
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("interleaved", [0, 1])
+@pytest.mark.parametrize("rms", [0, 1])
+@pytest.mark.parametrize("dh,rot", [(64, 64), (64, 32), (64, 0), (64, 2), (128, 128), (128, 64), (128, 70), (128, 126), (64, 24)])
+def test_rows(dtype, interleaved, rms, dh, rot):
+    for i, (T, heads) in enumerate(((1, 1), (3, 5), (130, 2), (777, 41))):
+        g = torch.Generator().manual_seed(T)
+        x = (torch.randn((T, heads * dh), generator=g) * 3 + (0 if rms else 2)).to(TYPES[dtype][1])
+        per_head = i & 1
+        gain = None if i == 2 else (1 + 0.3 * torch.randn((heads if per_head else 1, dh), generator=g)).to(TYPES[dtype][1])
+        pos = torch.randint(-5, 1 << 20, (T,), generator=g, dtype=torch.int32)
+        f, d = freq(rot), x.to(DEV)
+        args = (heads, dh, rms, None if gain is None else gain.to(DEV), per_head, 1e-5, rot, interleaved, pos.to(DEV) if rot else None, f.to(DEV) if rot else None, 1.2)
+        got = call(d, *args)
+        w = torch.ones((1, dh), dtype=torch.float64) if gain is None else gain.double()
+        y, e = normed_turned(x.view(T, heads, dh), w, rms, float(np.float32(1e-5)), pos, f, np.float32(1.2), rot, interleaved)
+        close(got, y.flatten(1), e.flatten(1), dtype)
+        assert torch.equal(call(d, *args, out=d), got)          # in place
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rms", [0, 1])
+def test_strides_and_alignments(dtype, rms):
+    """Rows and gains that begin anywhere; what lies between them is left alone."""
+    t = TYPES[dtype][1]
+    T, heads, dh, rot = 5, 3, 64, 64
+    w = heads * dh
+    f = freq(rot)
+    pos = torch.arange(T, dtype=torch.int32) * 77
+    for start, extra, gstart in ((0, 0, 1), (1, 0, 0), (3, 1, 2), (8, 8, 8), (0, 5, 3)):
+        g = torch.Generator().manual_seed(start)
+        buf, gb = torch.randn(T * (w + extra) + start, generator=g).to(t), (1 + 0.3 * torch.randn(w + gstart, generator=g)).to(t)
+        d, gd = buf.to(DEV), gb.to(DEV)
+        dx = torch.as_strided(d, (T, w), (w + extra, 1), start)
+        x = torch.as_strided(buf, (T, w), (w + extra, 1), start).reshape(T, heads, dh)
+        for il in (0, 1):
+            o = torch.full((T * (w + 5) + 2,), 7.0, dtype=t, device=DEV)
+            exe.exe_op_head_norm_rotary(TYPES[dtype][0], T, dx, w + extra, heads, dh, rms, gd[gstart:], 1, 1e-6, rot, il, pos.to(DEV), f.to(DEV), 1.0, o[1:], w + 5)
+            y, e = normed_turned(x, gb[gstart:].view(heads, dh).double(), rms, float(np.float32(1e-6)), pos, f, 1.0, rot, il)
+            close(torch.as_strided(o, (T, w), (w + 5, 1), 1), y.flatten(1), e.flatten(1), dtype)
+            torch.as_strided(o, (T, w), (w + 5, 1), 1).fill_(7.0)
+            assert bool((o == 7).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rms", [0, 1])
+@pytest.mark.parametrize("dh,start", [(64, 0), (128, 0), (64, 1), (128, 1)])
+def test_magnitudes(dtype, rms, dh, start):
+    """Heads whose squares pass a float's ends, beside ordinary ones; a mean that is large beside the deviations."""
+    t = TYPES[dtype][1]
+    g = torch.Generator().manual_seed(dh)
+    sizes = [1.0, 1e30, 1e-30, 2e38, 1e-37, 1.0, 1e19, 1e-19]
+    for eps in (0.0, 1e-6, 1e-34):
+        rows = torch.rand((2, len(sizes), dh), generator=g) * 2 - 1
+        x = (rows * torch.tensor(sizes)[None, :, None]).to(t)
+        buf = torch.zeros(x.numel() + start, dtype=t, device=DEV)
+        buf[start:] = x.flatten().to(DEV)
+        dx = buf[start:].view(2, -1)
+        got = call(dx, len(sizes), dh, rms, None, 0, eps, 0, 0, None, None, 1.0)
+        y, e = normed(x, torch.ones(1, dtype=torch.float64), rms, float(np.float32(eps)))
+        # subnormal floats of a head of 1e-37 are whole steps of 2^-149: 1e-8 of it, for each element and the mean
+        close(got, y.flatten(1), e.flatten(1) + (1e-7 if eps < 1e-6 else 0), dtype)
+    if not rms:
+        x = (1000.0 + torch.randn((3, 2 * dh), generator=g)).to(t)
+        y, e = normed(x.view(3, 2, dh), torch.ones(1, dtype=torch.float64), 0, 0.0)
+        # the first mean, 23 half steps of 1000 off, times the roundings of the differences: below a half step of 1
+        close(call(x.to(DEV), 2, dh, 0, None, 0, 0.0, 0, 0, None, None, 1.0), y.flatten(1), e.flatten(1) * 2, dtype)
+
+
+def test_zeros_infinities_and_nan_stay_in_their_heads():
+    for dtype in ("f32", "bf16"):
+        for dh in (64, 128):
+            x = torch.randn((1, 5 * dh), generator=torch.Generator().manual_seed(1)).to(TYPES[dtype][1])
+            clean = call(x.to(DEV), 5, dh, 1, None, 0, 1e-6, 0, 0, None, None, 1.0).cpu().view(5, dh)
+            v = x.view(5, dh)
+            v[0], v[2, 7], v[3, 9] = 0, float("inf"), float("nan")
+            for rms in (1, 0):
+                got = call(x.to(DEV), 5, dh, rms, None, 0, 1e-6, 0, 0, None, None, 1.0).cpu().view(5, dh)
+                assert bool((got[0] == 0).all()) and bool(got[3].isnan().all()) and not bool(got[1].isnan().any()) and not bool(got[4].isnan().any())
+                if rms:
+                    assert torch.equal(got[1], clean[1]) and torch.equal(got[4], clean[4])
+                    assert bool(got[2, 7].isnan()) and bool((got[2, :7] == 0).all()) and bool((got[2, 8:] == 0).all())
+                else:
+                    assert bool(got[2].isnan().all())
+            assert bool(call(torch.zeros((1, dh), device=DEV), 1, dh, 1, None, 0, 0.0, 0, 0, None, None, 1.0).isnan().all())
+
+
+def append(b, qkv, rms, q_gain, k_gain, per_head, rot, interleaved, pos, f, amplitude, q_out, stride=None, q_stride=None, stream=None):
+    exe.exe_op_head_norm_rotary_append_paged(b.code, len(b.seqs), b.d_cu, b.rows, qkv, stride or qkv.shape[1], b.H, b.Hkv, b.dh, rms, q_gain, k_gain, per_head,
+                                             1e-6, rot, interleaved, pos, f, amplitude, b.d_pool, b.n_blocks, b.d_table, b.max_blocks, b.block, b.d_len,
+                                             q_out, q_stride or b.H * b.dh, stream=stream)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("interleaved", [0, 1])
+@pytest.mark.parametrize("H,Hkv,dh,rot,block", [(4, 4, 64, 64, 8), (8, 2, 128, 128, 16), (5, 1, 128, 64, 4096), (3, 3, 64, 0, 16), (6, 2, 128, 90, 64)])
+def test_append(dtype, interleaved, H, Hkv, dh, rot, block):
+    for i, seqs in enumerate(([(1, 1)], [(1, 9), (0, 4), (1, 64), (40, 65), (0, 0), (3, 3)], [(1, 17 * i + 1) for i in range(70)] + [(300, 333)])):
+        b = Batch(seqs, H, Hkv, dh, block, dtype, extra_rows=2).fill().device()
+        g = torch.Generator().manual_seed(5)
+        qkv = (torch.randn((b.rows, (H + 2 * Hkv) * dh), generator=g) * 3).to(b.t)
+        f = freq(rot)
+        per_head, rms = i & 1, int(interleaved == 0)
+        gq, gk = ((1 + 0.3 * torch.randn((n if per_head else 1, dh), generator=g)).to(b.t) for n in (H, Hkv))
+        before = b.d_pool.clone()
+        for pos in (None, torch.randint(0, 100000, (b.rows,), generator=g, dtype=torch.int32)):
+            q_out = torch.full((b.rows, H * dh), 7.0, dtype=b.t, device=DEV)
+            b.d_pool.copy_(before)
+            append(b, qkv.to(DEV), rms, gq.to(DEV), None if i == 2 else gk.to(DEV), per_head, rot, interleaved, None if pos is None else pos.to(DEV), f.to(DEV) if rot else None, 1.1, q_out)
+            at = torch.cat([torch.arange(L - n, L) for n, L in seqs]) if pos is None else pos[:b.T]
+            x = qkv[:b.T].view(b.T, H + 2 * Hkv, dh)
+            gain = torch.cat([gq.double().expand(H, dh), (torch.ones_like(gk) if i == 2 else gk).double().expand(Hkv, dh)])
+            y, e = normed_turned(x[:, :H + Hkv], gain, rms, float(np.float32(1e-6)), at, f, np.float32(1.1), rot, interleaved)
+            close(q_out[:b.T], y[:, :H].flatten(1), e[:, :H].flatten(1), dtype)
+            assert bool((q_out[b.T:] == 7).all())
+            after, want = b.d_pool.cpu(), before.cpu()
+            t = 0
+            for s, (n, L) in enumerate(seqs):
+                for p in range(L - n, L):
+                    blk, row = int(b.table[s, p // block]), p % block
+                    close(after[blk, 0, :, row], y[t, H:], e[t, H:], dtype)
+                    assert torch.equal(after[blk, 1, :, row], x[t, H + Hkv:])
+                    want[blk, :, :, row] = after[blk, :, :, row]
+                    t += 1
+            assert torch.equal(torch.nan_to_num(after, nan=99.0), torch.nan_to_num(want, nan=99.0))      # nothing else moved
+
+
+def test_append_in_place_without_queries_and_unaligned():
+    b = Batch([(3, 20), (1, 5)], 4, 2, 64, 16, "bf16").fill().device()
+    f = freq(64).to(DEV)
+    qkv = torch.randn((4, 8 * 64), generator=torch.Generator().manual_seed(1)).bfloat16().to(DEV)
+    gain = (1 + 0.1 * torch.randn(64, generator=torch.Generator().manual_seed(2))).bfloat16().to(DEV)
+    q_out = torch.empty((4, 256), dtype=torch.bfloat16, device=DEV)
+    append(b, qkv, 1, gain, gain, 0, 64, 0, None, f, 1.0, q_out)
+    pool = b.d_pool.clone()
+    b.d_pool.fill_(3.0)
+    append(b, qkv, 1, gain, gain, 0, 64, 0, None, f, 1.0, None)            # keys and values only
+    rows = [(0, p) for p in (17, 18, 19)] + [(1, 4)]
+    at = lambda t: torch.stack([t[int(b.table[s, p // 16]), :, :, p % 16] for s, p in rows])
+    assert torch.equal(at(b.d_pool), at(pool)) and int((b.d_pool != 3).any(-1).sum()) == 4 * 4
+    wide = torch.zeros((4, 8 * 64 + 3), dtype=torch.bfloat16, device=DEV)
+    wide[:, 1:8 * 64 + 1] = qkv
+    b.d_pool.fill_(3.0)
+    append(b, wide[:, 1:], 1, gain, gain, 0, 64, 0, None, f, 1.0, wide[:, 1:], stride=8 * 64 + 3, q_stride=8 * 64 + 3)      # in place, odd rows
+    # other lanes add up the squares: the last bit of a bf16 may differ
+    off = lambda x, y: float(((x.double() - y.double()).abs() / y.double().abs().clamp_min(1e-3)).max())
+    assert off(at(b.d_pool), at(pool)) <= 2.0 ** -7 and off(wide[:, 1:257], q_out) <= 2.0 ** -7 and torch.equal(wide[:, 257:513], qkv[:, 256:])
+
+
+@pytest.mark.parametrize("entry", [-1, 1 << 30, -(1 << 31), None])
+def test_positions_without_a_block_are_not_stored(entry):
+    b = Batch([(40, 60), (1, 10)], 4, 2, 64, 16, "bf16").fill()
+    if entry is None:
+        b.table, b.max_blocks = b.table[:, :2].copy(), 2
+        lost = range(32, 60)
+    else:
+        b.table[0, 2] = entry
+        lost = range(32, 48)
+    b.device()
+    b.d_len[1] = -3                                                         # and a token before position 0
+    before = b.d_pool.clone()
+    qkv = torch.randn((41, 8 * 64), generator=torch.Generator().manual_seed(1)).bfloat16().to(DEV)
+    q_out = torch.full((41, 256), 7.0, dtype=torch.bfloat16, device=DEV)
+    append(b, qkv, 1, None, None, 0, 0, 0, None, None, 1.0, q_out)
+    assert torch.equal(q_out, call(qkv[:, :256].contiguous(), 4, 64, 1, None, 0, 1e-6, 0, 0, None, None, 1.0))
+    changed = torch.zeros((b.n_blocks, 16), dtype=torch.bool)
+    for p in range(20, 60):
+        if p not in lost:
+            changed[int(b.table[0, p // 16]), p % 16] = True
+    same = ((b.d_pool == before) | (b.d_pool.isnan() & before.isnan())).all(-1).all(1).all(1).cpu()
+    assert torch.equal(~same, changed)
+
+
+def test_append_replayed_with_other_lengths_and_on_another_stream():
+    """One graph, lengths and tables changed between its replays, against eager calls."""
+    b = Batch([(1, 20 + i) for i in range(5)], 8, 2, 128, 16, "bf16", table_pad=1).fill().device()
+    b.d_table.copy_(torch.arange(b.d_table.numel(), device=DEV).view(b.d_table.shape) % b.n_blocks)
+    f = freq(128).to(DEV)
+    gain = torch.ones(128, dtype=torch.bfloat16, device=DEV) * 1.5
+    qkv = torch.randn((5, 12 * 128), generator=torch.Generator().manual_seed(1)).bfloat16().to(DEV)
+    q_out = torch.zeros((5, 8 * 128), dtype=torch.bfloat16, device=DEV)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        append(b, qkv, 1, gain, gain, 0, 128, 0, None, f, 1.0, q_out)
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        append(b, qkv, 1, gain, gain, 0, 128, 0, None, f, 1.0, q_out)
+    for step in range(1, 5):
+        b.d_len.add_(1)
+        qkv.copy_(torch.randn((5, 12 * 128), generator=torch.Generator().manual_seed(step)).bfloat16())
+        b.d_pool.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, q = b.d_pool.clone(), q_out.clone()
+        b.d_pool.zero_()
+        append(b, qkv, 1, gain, gain, 0, 128, 0, None, f, 1.0, q_out)
+        assert torch.equal(got, b.d_pool) and torch.equal(q, q_out) and int((got != 0).any(-1).sum()) > 0
+
+
+def test_many_heads_and_rows_of_more_than_2_31_bytes():
+    """A row of 40000 heads; rows more than 2^31 elements from the first one."""
+    x = torch.randn((2, 40000 * 64), generator=torch.Generator().manual_seed(3)).bfloat16()
+    y, e = normed(x.view(2, 40000, 64), torch.ones(1, dtype=torch.float64), 1, 1e-6)
+    close(call(x.to(DEV), 40000, 64, 1, None, 0, 1e-6, 0, 0, None, None, 1.0), y.flatten(1), e.flatten(1), "bf16")
+    stride = (1 << 31) // 3 + 8
+    buf = torch.zeros(3 * stride + 128, dtype=torch.bfloat16, device=DEV)
+    v = torch.as_strided(buf, (4, 128), (stride, 1))
+    rows = torch.randn((4, 128), generator=torch.Generator().manual_seed(4)).bfloat16()
+    v.copy_(rows.to(DEV))
+    exe.exe_op_head_norm_rotary(1, 4, buf, stride, 2, 64, 1, None, 0, 1e-6, 0, 0, None, None, 1.0, buf, stride)
+    y, e = normed(rows.view(4, 2, 64), torch.ones(1, dtype=torch.float64), 1, 1e-6)
+    close(v, y.flatten(1), e.flatten(1), "bf16")
+
+
+def test_tensors_that_would_be_misread_are_refused():
+    x = torch.zeros((4, 256), dtype=torch.bfloat16, device=DEV)
+    pos, f = torch.zeros(4, dtype=torch.int32, device=DEV), torch.zeros(32, dtype=torch.float64, device=DEV)
+    gain = torch.ones(64, dtype=torch.bfloat16, device=DEV)
+    good = dict(dtype=1, T=4, x=x, x_stride=256, heads=4, dh=64, rms=1, gain=gain, gain_per_head=0, eps=1e-6, rot=64, interleaved=0, pos=pos, inv_freq=f, amplitude=1.0, out=x,
+                out_stride=256)
+    exe.exe_op_head_norm_rotary(**good)
+    for change in (dict(x=x.float(), out=x.float()), dict(dtype=0), dict(gain=gain.float()), dict(gain=gain[:63]), dict(gain_per_head=1), dict(pos=pos.long()), dict(inv_freq=f[:31]),
+                   dict(gain=gain.cpu()), dict(x=x[:, 1:])):
+        with pytest.raises(AssertionError):
+            exe.exe_op_head_norm_rotary(**{**good, **change})
