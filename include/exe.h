@@ -490,6 +490,26 @@ int exe_op_chunk_attention_paged(void* hip_stream, int32_t dtype, int32_t n_seqs
                                  uint64_t workspace_bytes);
 uint64_t exe_op_chunk_attention_paged_workspace(int32_t dtype, int32_t n_seqs, int32_t T, int32_t max_new, int32_t max_len, int32_t H,
                                                 int32_t Hkv, int32_t dh, int32_t window);
+/* The same attention, without a window, for a batch whose sequences share their first positions in groups: several continuations of one prompt
+ * (exe_seq_fork), many questions on one document, a system prompt in front of all.  Each group's prefix is read once, for all of its rows.
+ * Group g are sequences cu_groups[g] .. cu_groups[g + 1] - 1 (cu_groups [n_groups + 1], device, from 0, not falling, up to n_seqs; a group may be empty
+ * or of one, sequences behind the last group share nothing), whose first prefix[g] (device) positions hold the same keys and values.  Of these the ones in front of
+ * every new token of the group are read through the block table of the group's first sequence, so the other sequences' entries for blocks that lie
+ * in the prefix are not looked at; the positions behind are each sequence's own, as is all that prefix[g] names beyond the shortest context of its group, or
+ * below 0.  A prefix may end inside a block: the sequences then have blocks of their own there, as forks have.
+ * max_new (new tokens of a sequence), max_group (new tokens of a group), max_prefix and max_own (a sequence's positions behind its prefix, the new ones
+ * among them) size the launch and the workspace; where they are wrong, it is slower, not wrong.  Probabilities have 16 bits in the product with bf16
+ * values, and 8 in that with a prefix that more than 32 query rows share per key/value head (new tokens of the group times H / Hkv; bf16: max_group chooses).
+ * Made for single and drafted tokens: chunks of many tokens run in tiles of 16 rows a sequence here.
+ * Everything else as exe_op_chunk_attention_paged has it: rows without keys are 0, with a missing block NaN, spoilt ones computed once more; workspace:
+ * exe_op_prefix_attention_paged_workspace bytes, always some (0 for bad arguments). */
+int exe_op_prefix_attention_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, const int32_t* cu_seqlens, int32_t T, int32_t max_new,
+                                  int32_t n_groups, const int32_t* cu_groups, const int32_t* prefix, int32_t max_group, int32_t max_prefix,
+                                  const void* q, int64_t q_stride, const void* kv_blocks, int32_t n_blocks, const int32_t* block_table,
+                                  int32_t max_blocks, int32_t block_size, const int32_t* len, int32_t max_own, int32_t H, int32_t Hkv, int32_t dh,
+                                  float scale, void* out, int64_t out_stride, void* workspace, uint64_t workspace_bytes);
+uint64_t exe_op_prefix_attention_paged_workspace(int32_t dtype, int32_t n_seqs, int32_t T, int32_t max_new, int32_t n_groups, int32_t max_group,
+                                                 int32_t max_prefix, int32_t max_own, int32_t H, int32_t Hkv, int32_t dh);
 /* Copies positions between blocks of a pool [n_layers][n_blocks][K|V][Hkv][block_size][dh] (forks, compaction), in every layer: copies
  * [n_copies][3] HOST, each (source, destination, leading positions copied, 0 .. block_size).  A source may serve several copies; a
  * destination that is written twice or is another copy's source (or its own) is EXE_ERR_ARG.  The list travels with the launch. */

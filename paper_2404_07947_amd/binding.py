@@ -16,7 +16,7 @@ DECLARED_SYMBOLS = [
     "exe_expected_weights", "exe_model_load", "exe_model_free", "exe_encode", "exe_decode_step",
     "exe_seq_release", "exe_seq_length", "exe_kv_stats", "exe_seq_export_bytes", "exe_seq_export", "exe_seq_import", "exe_seq_reserve", "exe_seq_fork", "exe_kv_compact", "exe_profile", "exe_run_rra", "exe_kernel_timing",
     "exe_kernel_times", "exe_op_gemm", "exe_op_gemm_workspace", "exe_op_gemm_plan", "exe_op_gemm_model_plan", "exe_op_gemm_kv_plan", "exe_op_kv_store_index", "exe_op_gemm_stream", "exe_op_gemm_model", "exe_op_gemm_ld", "exe_op_gemm_noalloc", "exe_op_gemm_noalloc_max_workspace", "exe_op_paged_index_check", "exe_op_norm", "exe_op_resid_norm", "exe_op_prefill_attention", "exe_op_prefill_tiles",
-    "exe_op_decode_attention", "exe_op_decode_attention_paged", "exe_probe_peaks", "exe_probe_ingest", "exe_rotary_frequencies", "exe_op_rotary", "exe_op_rotary_append_paged", "exe_op_chunk_attention_paged", "exe_op_chunk_attention_paged_workspace", "exe_op_kv_copy_blocks", "exe_op_head_norm_rotary", "exe_op_head_norm_rotary_append_paged", "exe_op_logprobs", "exe_op_logprobs_workspace", "exe_op_argmax", "exe_rel_bucket", "exe_last_error", "exe_version",
+    "exe_op_decode_attention", "exe_op_decode_attention_paged", "exe_probe_peaks", "exe_probe_ingest", "exe_rotary_frequencies", "exe_op_rotary", "exe_op_rotary_append_paged", "exe_op_chunk_attention_paged", "exe_op_chunk_attention_paged_workspace", "exe_op_kv_copy_blocks", "exe_op_head_norm_rotary", "exe_op_head_norm_rotary_append_paged", "exe_op_prefix_attention_paged", "exe_op_prefix_attention_paged_workspace", "exe_op_logprobs", "exe_op_logprobs_workspace", "exe_op_argmax", "exe_rel_bucket", "exe_last_error", "exe_version",
     # exe_sched.h (host only)
     "exe_sim_completion", "exe_sim_step_ms", "exe_sim_rra", "exe_sim_waa", "exe_sched_search", "exe_sched_rra",
 ]
@@ -172,6 +172,10 @@ def lib():
     L.exe_op_head_norm_rotary.argtypes = [vp, i32, i32, vp, i64, i32, i32, i32, vp, i32, C.c_float, i32, i32, vp, vp, C.c_float, vp, i64]
     L.exe_op_head_norm_rotary_append_paged.argtypes = [vp, i32, i32, vp, i32, vp, i64, i32, i32, i32, i32, vp, vp, i32, C.c_float, i32, i32, vp, vp,
                                                        C.c_float, vp, i32, vp, i32, i32, vp, vp, i64]
+    L.exe_op_prefix_attention_paged.argtypes = [vp, i32, i32, vp, i32, i32, i32, vp, vp, i32, i32, vp, i64, vp, i32, vp, i32, i32, vp, i32, i32, i32, i32,
+                                                C.c_float, vp, i64, vp, C.c_uint64]
+    L.exe_op_prefix_attention_paged_workspace.argtypes = [i32] * 11
+    L.exe_op_prefix_attention_paged_workspace.restype = C.c_uint64
     L.exe_op_logprobs.argtypes = [vp, i32, vp, i64, i32, i32, C.c_float, vp, i32, vp, vp, i32, vp, vp, vp, C.c_uint64]
     L.exe_op_logprobs_workspace.argtypes = [i32] * 4
     L.exe_op_logprobs_workspace.restype = C.c_uint64
@@ -629,6 +633,26 @@ def exe_op_chunk_attention_paged(dtype, n_seqs, cu_seqlens, T, max_new, q, q_str
                                               _array(block_table, dev, "int32", n_seqs * max_blocks), max_blocks, block_size,
                                               _array(length, dev, "int32", n_seqs), max_len, H, Hkv, dh, scale, window,
                                               _rows(out, dev, dtype, T, H * dh, out_stride), out_stride, _dev(workspace), ws_bytes))
+
+
+def exe_op_prefix_attention_paged_workspace(dtype, n_seqs, T, max_new, n_groups, max_group, max_prefix, max_own, H, Hkv, dh) -> int:
+    return int(lib().exe_op_prefix_attention_paged_workspace(dtype, n_seqs, T, max_new, n_groups, max_group, max_prefix, max_own, H, Hkv, dh))
+
+
+def exe_op_prefix_attention_paged(dtype, n_seqs, cu_seqlens, T, max_new, n_groups, cu_groups, prefix, max_group, max_prefix, q, q_stride, kv_blocks,
+                                  n_blocks, block_table, max_blocks, block_size, length, max_own, H, Hkv, dh, scale, out, out_stride, workspace=None,
+                                  stream=None, ws_bytes=None):
+    """workspace: a device tensor, or an address and ws_bytes."""
+    dev, s = _where(stream)
+    ws, ws_bytes = _workspace(workspace, dev, ws_bytes)
+    block = 2 * Hkv * block_size * dh
+    _check(lib().exe_op_prefix_attention_paged(s, dtype, n_seqs, _array(cu_seqlens, dev, "int32", n_seqs + 1), T, max_new, n_groups,
+                                               _array(cu_groups, dev, "int32", n_groups + 1), _array(prefix, dev, "int32", n_groups), max_group,
+                                               max_prefix, _rows(q, dev, dtype, T, H * dh, q_stride), q_stride,
+                                               _rows(kv_blocks, dev, dtype, n_blocks, block, block), n_blocks,
+                                               _array(block_table, dev, "int32", n_seqs * max_blocks), max_blocks, block_size,
+                                               _array(length, dev, "int32", n_seqs), max_own, H, Hkv, dh, scale,
+                                               _rows(out, dev, dtype, T, H * dh, out_stride), out_stride, ws, ws_bytes))
 
 
 def exe_op_kv_copy_blocks(dtype, kv_blocks, n_layers, n_blocks, block_size, Hkv, dh, copies, stream=None):

@@ -283,6 +283,20 @@ struct ChunkAttnArgs {
 };
 size_t chunk_attn_workspace(const ChunkAttnArgs& a);
 hipError_t launch_chunk_attn(const ChunkAttnArgs& a, hipStream_t s);
+struct PrefixAttnArgs {      // as ChunkAttnArgs, of sequences in groups that share their first positions
+    int dtype, n_seqs, tokens, H, Hkv, dh, n_groups;
+    int max_new, max_group, max_prefix, max_own;       // size the launch; of a sequence, new tokens of a group, ..
+    const int32_t *cu, *cu_groups, *prefix;
+    const void* q; int64_t q_stride;
+    const void* kv_blocks;
+    PagedTable table;
+    const int32_t* len;
+    float scale;
+    void* out; int64_t out_stride;
+    float* workspace;                      // prefix_attn_workspace bytes
+};
+size_t prefix_attn_workspace(const PrefixAttnArgs& a);
+hipError_t launch_prefix_attn(const PrefixAttnArgs& a, hipStream_t s);
 
 constexpr int PREFILL_TILE_Q = 128, PREFILL_TILE_K = 64;
 struct PrefillWork {         // of one head over a batch

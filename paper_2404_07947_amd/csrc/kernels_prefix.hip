@@ -1,0 +1,480 @@
+// Attention of new tokens over a paged cache in which the sequences of a group share their first positions.
+//
+// The prefix of a group is read once for all of its sequences: the query rows of the group that share a key/value head, its new tokens times the
+// G = H / Hkv heads, are packed into tiles of 16 * QB rows, which all see the whole prefix and need no mask there.  The positions behind
+// it are each sequence's own, in tiles of 16 rows.  One launch takes both kinds, cut into parts of their keys; what a part makes of a row (the
+// sum of values by 2^(score - maximum), the maximum and the sum of probabilities, in float) is joined by a second one.
+// Which sequences are whose, and how many parts there are, the kernels find from what lies on the device, so that a captured launch follows
+// it; the host's bounds only size the launch.
+#include <algorithm>
+
+#include "chunk.h"
+
+namespace exe {
+
+constexpr int PX_WAVES = 4, PX_STEP = 16, PX_THREADS = PX_WAVES * WAVE, PX_PARTS = WAVE;
+constexpr float NO_PART = -2.f, NO_KEYS = -1.f;       // in place of a sum of probabilities: a part that is not there, a row without keys
+
+struct PrefixKernelArgs {
+    const int32_t *cu, *len, *cu_groups, *prefix;
+    int n_seqs, tokens, n_groups;
+    const void* q; int64_t q_stride;
+    const void* kv_blocks;
+    PagedTable table;
+    int H, Hkv, G;
+    float scale;
+    void* out; int64_t out_stride;
+    // Keys go to workgroups in parts of `keys`, at most `parts` (the last takes what is left).  Part i of row r: acc[i * rows + r][DH], ml[i * rows +
+    // r][maximum, sum], the prefix's parts in front of the own ones'.
+    struct Cut { int parts, keys; } shared, own;
+    float *acc, *ml;
+    int slots, own_tiles;             // of prefix tiles; tiles of a sequence's rows side by side
+    unsigned shared_units, own_units; // workgroups of each kind
+};
+
+// A group: sequences b0 .. b1 - 1, new tokens t0 .. t1 - 1, and the positions that they share.  Those in front of every new token of the group
+// count: what a call passes beyond is a sequence's own.  Group n_groups is what lies behind the last one, without a prefix.
+struct PrefixGroup { int g, b0, b1, t0, t1, prefix; };
+__device__ __forceinline__ int lanes_min(int v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const int w = __shfl_xor(v, o, WAVE);
+        v = w < v ? w : v;
+    }
+    return v;
+}
+// The group of tile slot `at` (those of group g begin at floor(first token * G / rows of a tile) + g, see ChunkTile), or of sequence `at`.
+template <bool SLOT> __device__ __forceinline__ PrefixGroup find_group(const PrefixKernelArgs& a, int at, int tile_shift, int lane)
+{
+    auto before = [&](int first_seq, int first_token, int g) { return SLOT ? (int)((int64_t)first_token * a.G >> tile_shift) + g <= at : first_seq <= at; };
+    PrefixGroup r;
+    int least;
+    if (a.n_seqs < WAVE && a.n_groups < WAVE - 1) {                    // all of it in one trip to memory
+        const int c = a.cu[lane < a.n_seqs ? lane : a.n_seqs], l = a.len[lane < a.n_seqs ? lane : a.n_seqs - 1];
+        int first = a.n_seqs, shared = 0;
+        if (a.n_groups) {
+            if (lane <= a.n_groups) first = a.cu_groups[lane];
+            shared = a.prefix[lane < a.n_groups ? lane : a.n_groups - 1];
+        } else if (lane == 0) first = 0;
+        first = first < 0 ? 0 : first < a.n_seqs ? first : a.n_seqs;
+        const int token = __shfl(c, first, WAVE), n = __shfl(c, lane + 1, WAVE) - c;
+        r.g = __popcll(__builtin_amdgcn_ballot_w64(lane <= a.n_groups && before(first, token, lane))) - 1;
+        if (r.g < 0) return PrefixGroup{-1, 0, 0, 0, 0, 0};
+        r.b0 = __builtin_amdgcn_readlane(first, r.g);
+        r.b1 = __builtin_amdgcn_readlane(first, r.g + 1);
+        r.t0 = __builtin_amdgcn_readlane(token, r.g);
+        r.t1 = __builtin_amdgcn_readlane(token, r.g + 1);
+        least = __builtin_amdgcn_readlane(shared, r.g);
+        const int p0 = lanes_min(lane >= r.b0 && lane < r.b1 && n > 0 ? l - n : 0x7fffffff);
+        least = p0 < least ? p0 : least;
+    } else {
+        auto first_of = [&](int g) {
+            const int first = g > a.n_groups ? a.n_seqs : a.n_groups ? a.cu_groups[g] : 0;
+            return first < 0 ? 0 : first < a.n_seqs ? first : a.n_seqs;
+        };
+        r.g = wave_search(0, a.n_groups + 1, lane, [&](int g) {
+            const int first = first_of(g);
+            return before(first, SLOT ? a.cu[first] : 0, g);
+        });
+        r.g = __builtin_amdgcn_readfirstlane(r.g);
+        if (r.g < 0) return PrefixGroup{-1, 0, 0, 0, 0, 0};
+        r.b0 = first_of(r.g);
+        r.b1 = first_of(r.g + 1);
+        r.t0 = a.cu[r.b0];
+        r.t1 = a.cu[r.b1];
+        least = r.g < a.n_groups ? a.prefix[r.g] : 0;
+        int p0 = 0x7fffffff;
+        if (least > 0) {
+            for (int b = r.b0 + lane; b < r.b1; b += WAVE) {
+                const int n = a.cu[b + 1] - a.cu[b], p = a.len[b] - n;
+                if (n > 0 && p < p0) p0 = p;
+            }
+            p0 = lanes_min(p0);
+        }
+        least = p0 < least ? p0 : least;
+    }
+    auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    return PrefixGroup{scalar(r.g), scalar(r.b0), scalar(r.b1), scalar(r.t0), scalar(r.t1), scalar(r.g < a.n_groups && least > 0 ? least : 0)};
+}
+
+__device__ __forceinline__ int parts_of(KeyRange k, const PrefixKernelArgs::Cut& cut)
+{
+    if (k.last <= k.first) return 1;
+    const int n = (int)(((int64_t)k.last - k.first + cut.keys - 1) / cut.keys);
+    return n < cut.parts ? n : cut.parts;
+}
+__device__ __forceinline__ KeyRange part_of(KeyRange k, const PrefixKernelArgs::Cut& cut, int part, int parts)
+{
+    const int first = k.first + part * cut.keys;
+    return KeyRange{first, part + 1 < parts ? first + cut.keys : k.last};
+}
+
+template <typename T, int DH> struct PrefixStream {
+    static constexpr int RB = DH * (int)sizeof(T), TILE = PX_STEP * RB, STAGE = 2 * TILE;
+    static constexpr int FIT = 16384 / STAGE, STAGES = FIT < 2 ? 2 : FIT, LOADS = TILE / 1024;
+    static constexpr int MERGE = PX_WAVES * 16 * (DH + 4) * 4;            // bytes of the waves' results, over the stages
+    static constexpr int LDS = PX_WAVES * STAGES * STAGE > MERGE ? PX_WAVES * STAGES * STAGE : MERGE;
+};
+
+// Query rows r0 .. r1 - 1 of a run of packed tokens from t0 on (row r: token t0 + r / G, head kvh * G + r % G) against keys k of table row b; row
+// r sees keys lo .. hi(r) - 1 of them.  Every wave takes steps of 16 keys of its own through a ring of stages in LDS, as chunk_stream_kernel does,
+// with QB blocks of 16 rows: S^T = K . Q^T, O^T += V^T . P^T.  The result goes to part `part`.
+template <typename T, int DH, int QB, bool NT, typename F>
+__device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned char* smem, float (*s_ml)[16][2], int b, int kvh, int t0, int r0, int r1,
+                                            KeyRange k, int lo, F hi, int part)
+{
+    typedef PrefixStream<T, DH> S;
+    constexpr int RB = S::RB, DS = RB / 64, DT = DH / 16;
+    constexpr bool TWO = sizeof(T) == 2 && QB <= 2;                      // probabilities as two bf16 parts, 2^-17 relative, where loads hide it; else rounded once
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), qi = lane & 15, g = lane >> 4, G = a.G;
+    const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem + wave * (S::STAGES * S::STAGE);
+    const unsigned char* mine = smem + wave * (S::STAGES * S::STAGE);
+    const float mul = exponent_scale(a.scale);
+    const int limit = table_limit(a.table);
+
+    u32x4 qf[QB][DS];
+    int last[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int r = r0 + qb * 16 + qi, row = r < r1 ? r : r1 - 1, t = t0 + row / G;
+        last[qb] = hi(row);
+        load_query<T, DS>((const T*)a.q + (int64_t)(t >= 0 && t < a.tokens ? t : 0) * a.q_stride + (kvh * G + row % G) * DH, g, a.scale, qf[qb]);
+    }
+    const int least = hi(r0);                                            // the first row sees the fewest
+    const int steps = k.last > k.first ? (k.last - k.first + PX_STEP - 1) / PX_STEP : 0, own = steps > wave ? (steps - wave + PX_WAVES - 1) / PX_WAVES : 0;
+    typedef RowLoader<T, DH, NT> Loader;
+    const Loader from(a.table, a.kv_blocks, b, kvh, a.Hkv, limit, k.last, lane);
+    auto first_of = [&](int i) { return k.first + (wave + i * PX_WAVES) * PX_STEP; };
+    typename Loader::Entries en{-1, -1};
+    auto issue = [&](int i) {
+        const unsigned dst = lds + i % S::STAGES * S::STAGE;
+        const typename Loader::Rows r = from.rows(first_of(i), en);
+        from.keys(first_of(i), r, dst);
+        from.values(first_of(i), r, dst + S::TILE);
+    };
+
+    float m[QB], l[QB];                                                  // l: this lane's share of the sum
+    f32x4 o[QB][DT];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        m[qb] = -INFINITY;
+        l[qb] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[qb][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int ahead = S::STAGES - 1;
+    for (int i = 0; i < ahead && i < own; ++i) {
+        en = from.lookup(first_of(i));
+        issue(i);
+    }
+    if (ahead < own) en = from.lookup(first_of(ahead));
+    for (int i = 0; i < own; ++i) {
+        if (i + ahead < own) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // step i - 1 has left its stage
+            issue(i + ahead);
+            if (i + ahead + 1 < own) en = from.lookup(first_of(i + ahead + 1));
+            wait_loads<2 * S::LOADS * (S::STAGES - 1)>();
+        } else {
+            wait_loads<0>();
+        }
+        const unsigned char* sK = mine + i % S::STAGES * S::STAGE;
+        f32x4 s[QB][2];
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) s[qb][0] = s[qb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ds = 0; ds < DS; ++ds) {
+            const u32x4 fk = *(const u32x4*)(sK + qi * RB + (((ds * 4 + g) ^ pf_swz<RB>(qi)) << 4));
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) s[qb][QB < 4 ? ds & 1 : 0] = HalfUnit<T>::mma(fk, qf[qb][ds], s[qb][QB < 4 ? ds & 1 : 0]);
+        }
+        const unsigned char* sV = sK + S::TILE;
+        const int v_row = 4 * g + (qi >> 2), v_q = qi & 3;
+        uint2 fv[sizeof(T) == 2 ? DT : 1];                               // on their way while the softmax is made
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) fv[dt] = pf_read_tr(sV + v_row * RB + (((2 * dt + (v_q >> 1)) ^ pf_swz<RB>(v_row)) << 4) + (v_q & 1) * 8);
+        }
+        const int j = first_of(i);
+        float mx[QB];
+        bool grew = false;
+        if (j + PX_STEP > least || j < lo) {
+            int key0 = j + 4 * g;
+            asm volatile("" : "+v"(key0));                               // keeps the mask arithmetic inside this branch
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+                if (QB < 4) s[qb][0] += s[qb][1];
+                s[qb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[qb][0][r] = key0 + r >= lo && key0 + r < last[qb] ? s[qb][0][r] : -INFINITY;
+            }
+        } else if (QB < 4) {
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) s[qb][0] += s[qb][1];
+        }
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            mx[qb] = fmaxf(fmaxf(s[qb][0][0], s[qb][0][1]), fmaxf(s[qb][0][2], s[qb][0][3])) * mul;
+            grew |= mx[qb] > m[qb] + 8.f;                                // the maximum follows only where it grew by more than 2^8: sums stay far from a float's ends
+        }
+        if (__builtin_amdgcn_ballot_w64(grew)) {
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+                const float to = fmaxf(m[qb], rows_max(mx[qb])), ref = to == -INFINITY ? 0.f : to, alpha = fast_exp2(m[qb] - ref);
+                l[qb] *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[qb][dt] *= alpha;
+                m[qb] = to;
+            }
+        }
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const float ref = m[qb] == -INFINITY ? 0.f : m[qb];
+            f32x4& p = s[qb][0];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                p[r] = fast_exp2(fmaf(p[r], mul, -ref));
+                l[qb] += p[r];
+            }
+            if constexpr (sizeof(T) == 2) {
+                typedef __attribute__((ext_vector_type(4))) short v4s;
+                bf16x4 high, low;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    high[r] = (bf16_t)p[r];
+                    low[r] = (bf16_t)(p[r] - (float)high[r]);
+                }
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    if (TWO) o[qb][dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, fv[dt]), __builtin_bit_cast(v4s, low), o[qb][dt], 0, 0, 0);
+                    o[qb][dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, fv[dt]), __builtin_bit_cast(v4s, high), o[qb][dt], 0, 0, 0);
+                }
+            }
+        }
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+                f32x4 c[QB];                                             // a sum per step, so that no chain of additions is as long as the cache
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) c[qb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float v = *(const float*)(sV + (4 * g + r) * RB + (((4 * dt + (qi >> 2)) ^ pf_swz<RB>(4 * g + r)) << 4) + (qi & 3) * 4);
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb) c[qb] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[qb][0][r], c[qb], 0, 0, 0);
+                }
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) o[qb][dt] += c[qb];
+            }
+        }
+    }
+
+    // the waves' results, joined, 16 rows at a time; lane (qi, g) holds features 16 * dt + 4 * g .. +3 of its row
+    float* s_o = (float*)smem;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        if (r0 + qb * 16 >= r1) break;
+        __syncthreads();                                                 // no wave reads its stages, or the block before, any more
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) *(f32x4*)(s_o + (wave * 16 + qi) * (DH + 4) + dt * 16 + 4 * g) = o[qb][dt];
+        const float total = rows_sum(l[qb]);
+        if (g == 0) {
+            s_ml[wave][qi][0] = m[qb];
+            s_ml[wave][qi][1] = total;
+        }
+        __syncthreads();
+        const int r = tid >> 4, c = tid & 15, row = r0 + qb * 16 + r, t = t0 + row / G;        // 16 threads a row, features 4 * c .. +3 of every 64
+        float M = -INFINITY, L = 0.f, w[PX_WAVES];
+#pragma unroll
+        for (int i = 0; i < PX_WAVES; ++i) M = fmaxf(M, s_ml[i][r][0]);
+        const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int i = 0; i < PX_WAVES; ++i) {
+            w[i] = fast_exp2(s_ml[i][r][0] - ref);
+            L += s_ml[i][r][1] * w[i];
+        }
+        if (row < r1 && t >= 0 && t < a.tokens) {
+            const int64_t at = ((int64_t)part * a.tokens + t) * a.H + kvh * G + row % G;
+#pragma unroll
+            for (int f = 0; f < DH / 64; ++f) {
+                f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < PX_WAVES; ++i) v += *(const f32x4*)(s_o + (i * 16 + r) * (DH + 4) + f * 64 + 4 * c) * w[i];
+                *(f32x4*)(a.acc + at * DH + f * 64 + 4 * c) = v;
+            }
+            if (c == 0) *(float2*)(a.ml + at * 2) = float2{M, hi(row) > lo ? L : NO_KEYS};
+        }
+    }
+    __syncthreads();                                                     // before the next tile's loads overwrite the results
+}
+// The same rows where there is no such part.
+__device__ __forceinline__ void no_part(const PrefixKernelArgs& a, int kvh, int t0, int r0, int r1, int part)
+{
+    const int row = r0 + threadIdx.x, t = t0 + row / a.G;
+    if (row < r1 && t >= 0 && t < a.tokens)
+        *(float2*)(a.ml + (((int64_t)part * a.tokens + t) * a.H + kvh * a.G + row % a.G) * 2) = float2{-INFINITY, NO_PART};
+}
+
+// Bound by reading the cache where contexts are long.
+template <typename T, int DH, int QB> __global__ __launch_bounds__(PX_THREADS, 2) void prefix_stream_kernel(PrefixKernelArgs a)
+{
+    constexpr int SHIFT = QB == 1 ? 4 : QB == 2 ? 5 : 6, ROWS = 16 * QB;
+    extern __shared__ __align__(16) unsigned char px_smem[];
+    __shared__ float s_ml[PX_WAVES][16][2];
+    const int lane = threadIdx.x & 63, limit = table_limit(a.table), G = a.G;
+    unsigned wg = blockIdx.x;
+    if (wg < a.shared_units) {
+        // tiles that read the same keys one after the other on one XCD
+        const unsigned u = (wg & 7) + 8 * ((wg >> 3) / a.slots), slot = (wg >> 3) % a.slots;
+        if (u >= (unsigned)(a.Hkv * a.shared.parts)) return;
+        const int kvh = u % a.Hkv, part = u / a.Hkv;
+        const PrefixGroup gr = find_group<true>(a, slot, SHIFT, lane);
+        if (gr.g < 0) return;
+        const int n = gr.t1 - gr.t0 < a.tokens ? gr.t1 - gr.t0 : a.tokens, rows = n * G;
+        const int r0 = (int)(slot - (unsigned)((int)((int64_t)gr.t0 * G >> SHIFT) + gr.g)) << SHIFT;
+        if (n <= 0 || r0 >= rows) return;
+        const int r1 = r0 + ROWS < rows ? r0 + ROWS : rows, end = gr.prefix < limit ? gr.prefix : limit;
+        const KeyRange all{0, end};
+        const int parts = end > 0 ? parts_of(all, a.shared) : 0;
+        if (part >= parts) return no_part(a, kvh, gr.t0, r0, r1, part);
+        stream_rows<T, DH, QB, false>(a, px_smem, s_ml, gr.b0, kvh, gr.t0, r0, r1, part_of(all, a.shared, part, parts), 0, [&](int) { return end; }, part);
+        return;
+    }
+    wg -= a.shared_units;
+    const int part = wg % a.own.parts, tile = wg / a.own.parts % a.own_tiles, head = wg / a.own.parts / a.own_tiles, kvh = head % a.Hkv, b = head / a.Hkv;
+    const int t0 = a.cu[b], end = a.cu[b + 1], p_end = a.len[b], n = end - t0 < a.tokens ? end - t0 : a.tokens, p0 = p_end - n;
+    const PrefixGroup gr = find_group<false>(a, b, 0, lane);
+    if (n <= 0) return;
+    const int lo = gr.prefix < limit ? gr.prefix : limit;
+    auto hi = [&](int row) { return keys_of(p0 + row / G, 0, limit).last; };
+    for (int r0 = tile * 16; r0 < n * G; r0 += a.own_tiles * 16) {
+        const int r1 = r0 + 16 < n * G ? r0 + 16 : n * G;
+        const KeyRange all{lo & -PX_STEP, hi(r1 - 1)};
+        const int parts = parts_of(all, a.own);
+        if (part >= parts) no_part(a, kvh, t0, r0, r1, a.shared.parts + part);
+        else stream_rows<T, DH, 1, true>(a, px_smem, s_ml, b, kvh, t0, r0, r1, part_of(all, a.own, part, parts), lo, hi, a.shared.parts + part);
+    }
+}
+
+// The sum over a row's parts of 2^(m_i - M) times their sums, in their order: a wave per row, DH / 4 lanes a part, 2 or 4 parts at a time.
+template <typename T, int DH> __global__ __launch_bounds__(256) void prefix_join_kernel(PrefixKernelArgs a)
+{
+    constexpr int PER = DH / 4, SUBS = 64 / PER;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = (a.H + 3) / 4;
+    const int t = blockIdx.x / quarter, h = (blockIdx.x - t * quarter) * 4 + wave;
+    if (h >= a.H) return;
+    const int parts = a.shared.parts + a.own.parts, sub = lane / PER, f = lane % PER * 4;
+    const int64_t at = (int64_t)t * a.H + h, step = (int64_t)a.tokens * a.H;
+    const int packed = a.cu[a.n_seqs];
+    const float2 x = lane < parts ? *(const float2*)(a.ml + (at + lane * step) * 2) : float2{-INFINITY, NO_PART};
+    if (t >= packed) return;
+    const float M = wave_max(x.x), w = x.y == NO_PART ? -1.f : fast_exp2(x.x - (M == -INFINITY ? 0.f : M)), L = wave_sum(x.y < 0.f ? 0.f : x.y * w);
+    const bool none = __builtin_amdgcn_ballot_w64(x.y == NO_KEYS);
+    const float* acc = a.acc + at * DH + f;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < parts; i += SUBS) {
+        const int k = i + sub;
+        const float wk = __shfl(w, k < parts ? k : parts - 1, WAVE);
+        const f32x4 p = *(const f32x4*)(acc + (k < parts ? k : parts - 1) * step * DH);
+        if (k < parts && wk >= 0.f) v += p * wk;
+    }
+#pragma unroll
+    for (int d = PER; d < 64; d <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], d, WAVE);
+    float most = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        v[e] = none ? 0.f : v[e] / L;
+        most = magnitude(most, v[e]);
+    }
+    T* out = (T*)a.out + (int64_t)t * a.out_stride + h * DH;
+    if (!none && __builtin_amdgcn_ballot_w64(spoilt(most, L))) {
+        const ChunkSeq sq = seq_of_token(a.cu, a.n_seqs, t, lane);
+        if (sq.b < 0) return;
+        const PrefixGroup gr = find_group<false>(a, sq.b, 0, lane);
+        const int limit = table_limit(a.table);
+        const int64_t head = (int64_t)DH << a.table.shift;
+        chunk_row<T, DH>((const T*)a.q + (int64_t)t * a.q_stride + h * DH, (const T*)a.kv_blocks + h / a.G * head, 2 * a.Hkv * head, a.Hkv * head, a.table.shift,
+                         [&](int j) { return a.table.block(j < gr.prefix ? gr.b0 : sq.b, j); }, keys_of(a.len[sq.b] - sq.n + (t - sq.t0), 0, limit), a.scale * LOG2E, lane, out);
+    } else if (sub == 0) {
+        typename Vec4<T>::type y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = from_f32<T>(v[e]);
+        *(typename Vec4<T>::type*)(out + f) = y;
+    }
+}
+
+// ---------------------------------------------------------------- launches
+struct PrefixPlan {
+    int qb;
+    PrefixKernelArgs::Cut shared, own;
+    int own_tiles;
+    int64_t slots, shared_units, own_units;
+};
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+static PrefixKernelArgs::Cut cut_keys(int64_t keys, int64_t target, int most)
+{
+    int64_t parts = ceil_div(keys, target);
+    parts = parts < 1 ? 1 : parts < most ? parts : most;
+    if (parts == 1) return {1, 0x7fffffff};
+    const int64_t each = ceil_div(ceil_div(keys, parts), PX_STEP) * PX_STEP;
+    return {(int)ceil_div(keys, each), (int)each};
+}
+static PrefixPlan prefix_plan(const PrefixAttnArgs& a)
+{
+    PrefixPlan p{};
+    const int64_t G = a.H / a.Hkv, rows = (int64_t)a.max_group * G;
+    p.qb = a.n_groups == 0 || rows <= 16 ? 1 : rows <= 32 || a.dtype == DT_F32 ? 2 : 4;
+    p.slots = (int64_t)a.tokens * G / (16 * p.qb) + a.n_groups + 1;
+    const int64_t most = (int64_t)a.tokens * G / (16 * p.qb) + a.n_groups, each = a.n_groups * ceil_div(rows, 16 * p.qb), tiles = (each < most ? each : most) * a.Hkv;
+    const int64_t own = a.n_seqs * a.Hkv, own_rows = ceil_div(a.max_new * G, 16);
+    const int64_t wgs = a.dtype == DT_F32 && a.dh == 128 ? 256 : 512;
+    int64_t target = ceil_div(tiles * a.max_prefix + own * own_rows * a.max_own, wgs);
+    target = target < 128 ? 128 : target;
+    p.own = cut_keys(a.max_own, target, 16);
+    p.shared = a.n_groups ? cut_keys(a.max_prefix, target, PX_PARTS - p.own.parts) : PrefixKernelArgs::Cut{0, 0x7fffffff};
+    p.shared_units = ceil_div(a.Hkv * p.shared.parts, 8) * 8 * p.slots;
+    p.own_tiles = (int)std::max<int64_t>(1, std::min(own_rows, (1 << 20) / (own * p.own.parts)));      // a workgroup goes on with what is left
+    p.own_units = own * p.own_tiles * p.own.parts;
+    return p;
+}
+size_t prefix_attn_workspace(const PrefixAttnArgs& a)
+{
+    const PrefixPlan p = prefix_plan(a);
+    return (size_t)(p.shared.parts + p.own.parts) * a.tokens * a.H * (a.dh + 2) * sizeof(float);
+}
+
+template <typename T, int DH, int QB> static hipError_t launch_stream(const PrefixKernelArgs& k, int64_t wgs, hipStream_t s)
+{
+    static LdsLimit limit[MAX_DEVICES];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) dev = 0;
+    hipError_t e = limit[dev].raise((const void*)prefix_stream_kernel<T, DH, QB>, PrefixStream<T, DH>::LDS);
+    if (e != hipSuccess) return e;
+    prefix_stream_kernel<T, DH, QB><<<(unsigned)wgs, PX_THREADS, PrefixStream<T, DH>::LDS, s>>>(k);
+    return hipGetLastError();
+}
+template <typename T, int DH> static hipError_t launch_prefix(const PrefixAttnArgs& a, hipStream_t s)
+{
+    const PrefixPlan p = prefix_plan(a);
+    const int64_t wgs = p.shared_units + p.own_units, rows = (int64_t)a.tokens * a.H;
+    if (p.slots > 0x7fffffff || wgs * PX_THREADS > MAX_LAUNCH_THREADS || rows / 4 + a.tokens > MAX_LAUNCH_THREADS / PX_THREADS) return hipErrorInvalidValue;
+    PrefixKernelArgs k{a.cu, a.len, a.cu_groups, a.prefix, a.n_seqs, a.tokens, a.n_groups, a.q, a.q_stride, a.kv_blocks, a.table, a.H, a.Hkv, a.H / a.Hkv, a.scale, a.out,
+                       a.out_stride, p.shared, p.own, a.workspace, a.workspace + (size_t)(p.shared.parts + p.own.parts) * rows * DH, (int)p.slots, p.own_tiles,
+                       (unsigned)p.shared_units, (unsigned)p.own_units};
+    hipError_t e;
+    if (p.qb == 1) e = launch_stream<T, DH, 1>(k, wgs, s);
+    else if (sizeof(T) == 4 || p.qb == 2) e = launch_stream<T, DH, 2>(k, wgs, s);
+    else e = launch_stream<T, DH, sizeof(T) == 4 ? 2 : 4>(k, wgs, s);
+    if (e != hipSuccess) return e;
+    prefix_join_kernel<T, DH><<<(unsigned)(a.tokens * ceil_div(a.H, 4)), 256, 0, s>>>(k);
+    return hipGetLastError();
+}
+hipError_t launch_prefix_attn(const PrefixAttnArgs& a, hipStream_t s)
+{
+    if (a.dtype == DT_F32) return a.dh == 64 ? launch_prefix<float, 64>(a, s) : launch_prefix<float, 128>(a, s);
+    return a.dh == 64 ? launch_prefix<bf16_t, 64>(a, s) : launch_prefix<bf16_t, 128>(a, s);
+}
+
+}  // namespace exe

@@ -2516,6 +2516,65 @@ extern "C" int exe_op_chunk_attention_paged(void* hip_stream, int32_t dtype, int
     return EXE_OK;
 }
 
+static PrefixAttnArgs prefix_args(int dtype, int n_seqs, int T, int max_new, int n_groups, int max_group, int max_prefix, int max_own, int H, int Hkv, int dh)
+{
+    PrefixAttnArgs a{};
+    a.dtype = dtype; a.n_seqs = n_seqs; a.tokens = T; a.H = H; a.Hkv = Hkv; a.dh = dh; a.n_groups = n_groups;
+    a.max_new = std::min(max_new, T); a.max_group = std::min(max_group, T); a.max_prefix = max_prefix; a.max_own = max_own;
+    return a;
+}
+
+extern "C" uint64_t exe_op_prefix_attention_paged_workspace(int32_t dtype, int32_t n_seqs, int32_t T, int32_t max_new, int32_t n_groups, int32_t max_group,
+                                                            int32_t max_prefix, int32_t max_own, int32_t H, int32_t Hkv, int32_t dh)
+{
+    if ((dtype != DT_F32 && dtype != DT_BF16) || (dh != 64 && dh != 128)) return 0;
+    if (n_seqs < 1 || T < 1 || max_new < 1 || n_groups < 0 || max_group < (n_groups > 0) || max_prefix < 0 || max_own < 1 || Hkv < 1 || H < Hkv || H % Hkv ||
+        (int64_t)T * H > 0x7fffffff) return 0;
+    return prefix_attn_workspace(prefix_args(dtype, n_seqs, T, max_new, n_groups, max_group, max_prefix, max_own, H, Hkv, dh));
+}
+
+extern "C" int exe_op_prefix_attention_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, const int32_t* cu_seqlens, int32_t T, int32_t max_new,
+                                             int32_t n_groups, const int32_t* cu_groups, const int32_t* prefix, int32_t max_group, int32_t max_prefix,
+                                             const void* q, int64_t q_stride, const void* kv_blocks, int32_t n_blocks, const int32_t* block_table,
+                                             int32_t max_blocks, int32_t block_size, const int32_t* len, int32_t max_own, int32_t H, int32_t Hkv,
+                                             int32_t dh, float scale, void* out, int64_t out_stride, void* workspace, uint64_t workspace_bytes)
+{
+    int r = check_paged(dtype, dh, Hkv, n_blocks, max_blocks, block_size);
+    if (r) return r;
+    if (n_seqs < 0 || T < 0 || n_groups < 0) return fail(EXE_ERR_ARG, "bad prefix attention arguments");
+    const int least = n_seqs > 0 && T > 0;                               // the longest of no chunks is 0
+    if (max_new < least || max_own < least || max_group < (least && n_groups > 0) || max_prefix < 0)
+        return fail(EXE_ERR_ARG, "max_new %d, max_group %d, max_prefix %d, max_own %d", max_new, max_group, max_prefix, max_own);
+    if (H < Hkv || H % Hkv) return fail(EXE_ERR_SHAPE, "%d query heads over %d key/value heads", H, Hkv);
+    if ((int64_t)T * H > 0x7fffffff || (int64_t)H * dh > 0x7fffffff) return fail(EXE_ERR_SHAPE, "%d rows of %d heads", T, H);
+    const int esz = esz_of_dtype(dtype);
+    if (q_stride < (int64_t)H * dh || out_stride < (int64_t)H * dh) return fail(EXE_ERR_SHAPE, "rows of %d heads overlap", H);
+    if (q_stride * esz % 16 || out_stride * esz % 16) return fail(EXE_ERR_SHAPE, "rows must begin on 16 bytes");
+    if (!least) return EXE_OK;
+    if (!cu_seqlens || !q || !kv_blocks || !block_table || !len || !out || (n_groups > 0 && (!cu_groups || !prefix))) return fail(EXE_ERR_ARG, "bad prefix attention arguments");
+    const void* ptrs[] = {q, kv_blocks, out, workspace};
+    for (const void* p : ptrs)
+        if ((uintptr_t)p & 15) return fail(EXE_ERR_ARG, "operands must be 16-byte aligned");
+    if (q == out) return fail(EXE_ERR_ARG, "rows of q are read after others of out are written: they cannot be the same");
+    PrefixAttnArgs a = prefix_args(dtype, n_seqs, T, max_new, n_groups, max_group, max_prefix, max_own, H, Hkv, dh);
+    const uint64_t need = prefix_attn_workspace(a);
+    if (need > (workspace ? workspace_bytes : 0)) return fail(EXE_ERR_ARG, "workspace too small (%llu bytes needed)", (unsigned long long)need);
+    a.cu = cu_seqlens;
+    a.cu_groups = cu_groups;
+    a.prefix = prefix;
+    a.q = q;
+    a.q_stride = q_stride;
+    a.kv_blocks = kv_blocks;
+    a.table = PagedTable{block_table, max_blocks, block_shift_of(block_size), n_blocks};
+    a.len = len;
+    a.scale = scale;
+    a.out = out;
+    a.out_stride = out_stride;
+    a.workspace = (float*)workspace;
+    HIP_TRY(launch_prefix_attn(a, (hipStream_t)hip_stream));
+    return EXE_OK;
+}
+
 extern "C" int exe_op_kv_copy_blocks(void* hip_stream, int32_t dtype, void* kv_blocks, int32_t n_layers, int32_t n_blocks, int32_t block_size, int32_t Hkv,
                                      int32_t dh, int32_t n_copies, const int32_t* copies)
 {
