@@ -12,6 +12,7 @@ namespace exe {
 
 typedef unsigned long long u64;
 constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / WAVE, LP_CAP = LP_THREADS, LP_JOIN = 64;
+static_assert(LP_WAVES == 4 && LP_THREADS == 256, "four best ones a lane");
 constexpr float LN2 = 0.69314718055994530942f;
 
 struct LogprobKernelArgs {
@@ -22,7 +23,7 @@ struct LogprobKernelArgs {
     float *logprobs, *entropy;
     int k;
     int32_t* top_ids; float* top_logprobs;
-    unsigned parts;                        // of a row, that this launch writes
+    unsigned parts, span;                  // of a row, that this launch writes; logits of each
     float* sums; u64* lists;               // where they go: [rows * parts][M, S, Y, -], [rows * parts][k]; parts 1: the results themselves
     unsigned from_parts;                   // joining: of a row, that it reads
     const float* from_sums; const u64* from_lists;
@@ -35,11 +36,8 @@ __device__ __forceinline__ unsigned logit_order(float x)
     return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ u64 logit_key(unsigned order, unsigned i) { return (u64)order << 32 | ~i; }
-__device__ __forceinline__ float key_logit(u64 key)
-{
-    const unsigned o = (unsigned)(key >> 32);
-    return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xffffffffu));
-}
+__device__ __forceinline__ float order_logit(unsigned o) { return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xffffffffu)); }
+__device__ __forceinline__ float key_logit(u64 key) { return order_logit((unsigned)(key >> 32)); }
 
 // The largest over the wave, of numbers (a NaN is never taken)
 __device__ __forceinline__ float lanes_max(float v)
@@ -52,13 +50,14 @@ __device__ __forceinline__ float lanes_max(float v)
 }
 
 struct Sums { float M, S, Y; };
-// Of up to 64 parts, a lane each (the others hold M = -inf, S = Y = 0).  Where a part has no number but -inf its M is -inf, and its sums are 0, or NaN.
-__device__ __forceinline__ Sums join_sums(Sums p, float c)
+// A part's sums to the largest logit M of several.  Where a part has no number but -inf its M is -inf, and its sums are 0, or NaN.
+__device__ __forceinline__ void sums_to(Sums& p, float M, float c)
 {
-    const float M = lanes_max(p.M);
-    const bool none = p.M == -INFINITY;
+    if (p.M == -INFINITY) return;
     const float d = fmaxf((p.M - M) * c, -1e30f), w = fast_exp2(d);
-    return Sums{M, wave_sum(none ? p.S : p.S * w), wave_sum(none ? p.Y : w * fmaf(p.S, d, p.Y))};
+    p.Y = w * fmaf(p.S, d, p.Y);
+    p.S *= w;
+    p.M = M;
 }
 
 // The results of a row, by a workgroup: sums, and the k best keys in LDS (0: there are fewer).
@@ -92,35 +91,55 @@ template <typename T, int C> struct LogitPart {
     }
     // place of element i among the part's
     static __device__ __forceinline__ unsigned place(int i) { return (i / V * LP_THREADS + threadIdx.x) * V + i % V; }
-    // first: the logit with which the part begins, on 16 bytes; up to V - 1 before the row's first one.  What is not of the row is -inf.
-    __device__ __forceinline__ void load(const T* x, unsigned first, unsigned n)
+    // New values to the compiler, which would keep what it made of all of them in registers from one use to the next.
+    __device__ __forceinline__ void renew()
     {
-        if (first < n && n - first >= SPAN) {
 #pragma unroll
-            for (int c = 0; c < C; ++c) raw[c] = load_chunk<true>(x + first + place(c * V));
-            return;
+        for (int c = 0; c < C; ++c) asm volatile("" : "+v"(raw[c].x), "+v"(raw[c].y), "+v"(raw[c].z), "+v"(raw[c].w));
+    }
+    // Logits first .. end - 1 of the row, the first on 16 bytes: up to V - 1 before the row's first one.  What is not of them is -inf.  All loads go
+    // out before anything waits: those of chunks that are not there, or only in part, from the nearest whole one.
+    __device__ __forceinline__ void load(const T* x, unsigned first, unsigned end, unsigned n)
+    {
+        const int low = (int)(-(unsigned)((uintptr_t)x & 15) / sizeof(T) % V), high = (int)(n - low) < V ? -1 : low + ((int)n - low - V) / V * V;
+        if (high >= 0) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int i = (int)(first + place(c * V));
+                raw[c] = load_chunk<true>(x + (i < low ? low : i < high ? i : high));
+            }
         }
+        // the last thread's last chunk is there, and the first thread's first: all are
+        if (first < end && end - first >= SPAN) return;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const unsigned i = first + place(c * V);
-            if (i < n && n - i >= V) {
-                raw[c] = load_chunk<true>(x + i);
-            } else {
-                unsigned w[4];
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    if constexpr (sizeof(T) == 4) {
-                        w[d] = i + d < n ? __float_as_uint(x[i + d]) : 0xff800000u;
-                    } else {
-                        const unsigned lo = i + 2 * d < n ? ((const uint16_t*)x)[i + 2 * d] : 0xff80u, hi = i + 2 * d + 1 < n ? ((const uint16_t*)x)[i + 2 * d + 1] : 0xff80u;
-                        w[d] = lo | hi << 16;
-                    }
-                }
-                raw[c] = uint4{w[0], w[1], w[2], w[3]};
+            if (i < end && end - i >= V) continue;
+            if (i - first >= end - first) {                    // nothing of it
+                const unsigned none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+                raw[c] = uint4{none, none, none, none};
+                continue;
             }
+            unsigned w[4];
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                if constexpr (sizeof(T) == 4) {
+                    w[d] = i + d < end ? __float_as_uint(x[i + d]) : 0xff800000u;
+                } else {
+                    const unsigned lo = i + 2 * d < end ? ((const uint16_t*)x)[i + 2 * d] : 0xff80u, hi = i + 2 * d + 1 < end ? ((const uint16_t*)x)[i + 2 * d + 1] : 0xff80u;
+                    w[d] = lo | hi << 16;
+                }
+            }
+            raw[c] = uint4{w[0], w[1], w[2], w[3]};
         }
     }
 };
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 
 // The best keys among those of the part that `take` lets through, at most LP_CAP: sorted by counting, for each, those above it.
 __device__ __forceinline__ void sort_keys(const u64* keys, int count, u64* top, int k)
@@ -141,22 +160,38 @@ template <typename T, int C> __global__ __launch_bounds__(LP_THREADS) void logpr
     constexpr int N = Part::N;
     __shared__ u64 s_keys[LP_CAP], s_top[WAVE];
     __shared__ Sums s_sums[LP_WAVES];
-    __shared__ float s_least[LP_WAVES];
-    __shared__ int s_count, s_counts[48];
+    __shared__ __align__(16) float s_best[LP_THREADS];
+    __shared__ int s_count, s_digit, s_counts[256];
+    static_assert(LP_THREADS == 256 && Part::SPAN <= 1 << 16, "a count for each digit; 16 bits of a place");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row = blockIdx.x / a.parts;
     const unsigned part = blockIdx.x - (unsigned)row * a.parts;
     const T* x = (const T*)a.logits + row * a.row_stride;
-    const unsigned first = part * Part::SPAN - (unsigned)((uintptr_t)x & 15) / sizeof(T);
+    const unsigned first = part * a.span - (unsigned)((uintptr_t)x & 15) / sizeof(T), end = first + a.span < a.n ? first + a.span : a.n;
     Part p;
-    p.load(x, first, a.n);
+    p.load(x, first, end, a.n);
     if (tid == 0) s_count = 0;
-    if (tid < 48) s_counts[tid] = 0;
 
-    float best = p.at(0);
+    float tops[C], best = -INFINITY;                           // of a chunk; of all
+    bool none = false;
 #pragma unroll
-    for (int i = 1; i < N; ++i) best = fmaxf(best, p.at(i));
-    if (!(best >= -INFINITY)) best = -INFINITY;                // all of them NaN
+    for (int c = 0; c < C; ++c) {
+        const int i = c * Part::V;
+        tops[c] = max3(p.at(i), p.at(i + 1), p.at(i + 2));
+        if constexpr (Part::V == 8) tops[c] = max3(max3(tops[c], p.at(i + 3), p.at(i + 4)), p.at(i + 5), p.at(i + 6));
+        tops[c] = max3(tops[c], tops[c], p.at(i + Part::V - 1));
+        none |= tops[c] != tops[c];
+    }
+    if (none) {                                                // all of a chunk NaN, or signalling ones, which that instruction hands on
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            tops[c] = -INFINITY;
+#pragma unroll
+            for (int i = c * Part::V; i < (c + 1) * Part::V; ++i) tops[c] = p.at(i) > tops[c] ? p.at(i) : tops[c];
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) best = fmaxf(best, tops[c]);
     const float most = lanes_max(best), R = most == -INFINITY ? 0.f : most * a.c;
     float S = 0.f, Y = 0.f;
     auto add = [&](float z) {
@@ -178,67 +213,95 @@ template <typename T, int C> __global__ __launch_bounds__(LP_THREADS) void logpr
     S = wave_sum(S);
     Y = wave_sum(Y);
     if (lane == 0) s_sums[wave] = Sums{most, S, Y};
-    if (a.k) {
-        // The waves' (k / 4)-th largest of their lanes' best: k logits or more are no smaller than the least of these.
-        float b = best, least = most;
-        for (int i = 1; i < (a.k + LP_WAVES - 1) / LP_WAVES; ++i) {
-            if (lane == __builtin_ctzll(__builtin_amdgcn_ballot_w64(b == least))) b = -INFINITY;
-            least = lanes_max(b);
-        }
-        if (lane == 0) s_least[wave] = least;
-    }
+    s_best[tid] = best;
     __syncthreads();
-    const Sums t = join_sums(lane < LP_WAVES ? s_sums[lane] : Sums{-INFINITY, 0.f, 0.f}, a.c);
+    Sums t{-INFINITY, 0.f, 0.f};
+    if (wave == 0 || a.parts == 1) {
+        t.M = fmaxf(fmaxf(s_sums[0].M, s_sums[1].M), fmaxf(s_sums[2].M, s_sums[3].M));
+#pragma unroll
+        for (int w = 0; w < LP_WAVES; ++w) {
+            Sums p = s_sums[w];
+            sums_to(p, t.M, a.c);
+            t.S += p.S;
+            t.Y += p.Y;
+        }
+    }
     if (a.k) {
-        float least = s_least[0];
+        // k logits or more are no smaller than the k-th largest of the threads' best ones, of which four at a time will do where k is small: that many
+        // take part in a search for its upper 16 bits, a number no larger.
+        const f32x4 b4 = *(const f32x4*)(s_best + 4 * lane);
+        const float b1 = fmaxf(fmaxf(b4[0], b4[1]), fmaxf(b4[2], b4[3]));
+        unsigned kth = 0;
+        if (a.k <= 32) {
+            const unsigned o = logit_order(b1);
+            for (unsigned bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
+                if (__popcll(__builtin_amdgcn_ballot_w64(o >= (kth | bit))) >= a.k) kth |= bit;
+        } else {
+            const unsigned o[4] = {logit_order(b4[0]), logit_order(b4[1]), logit_order(b4[2]), logit_order(b4[3])};
+            for (unsigned bit = 1u << 31; bit >= 1u << 16; bit >>= 1) {
+                int n = 0;
 #pragma unroll
-        for (int w = 1; w < LP_WAVES; ++w) least = fminf(least, s_least[w]);
-        if (best >= least) {
+                for (int i = 0; i < 4; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(o[i] >= (kth | bit)));
+                if (n >= a.k) kth |= bit;
+            }
+        }
+        p.renew();
+        float least = order_logit(kth);
+        least = least >= -3.4028235e38f ? least : -3.4028235e38f;              // those of -inf are ruled out; not a number: fewer than k
+        unsigned have[(N + 31) / 32] = {};                     // a bit for each
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float v = p.at(i);
-                if (v >= least && v > -INFINITY) {
-                    const int at = atomicAdd(&s_count, 1);     // in any order: they are sorted
-                    if (at < LP_CAP) s_keys[at] = logit_key(logit_order(v), first + Part::place(i));
+        for (int c = 0; c < C; ++c) {
+            if (!__builtin_amdgcn_ballot_w64(tops[c] >= least)) continue;
+#pragma unroll
+            for (int i = c * Part::V; i < (c + 1) * Part::V; ++i) have[i / 32] |= p.at(i) >= least ? 1u << i % 32 : 0u;
+        }
+        // One of each lane that has some at a time, in any order: they are sorted.  From memory again: a branch for each register would cost more.
+#pragma unroll
+        for (int w = 0; w < (N + 31) / 32; ++w) {
+            for (u64 some; (some = __builtin_amdgcn_ballot_w64(have[w] != 0)); have[w] &= have[w] - 1) {
+                int at = 0;
+                if (lane == 0) at = atomicAdd(&s_count, __popcll(some));
+                at = __builtin_amdgcn_readfirstlane(at) + __builtin_amdgcn_mbcnt_hi((unsigned)(some >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)some, 0));
+                if (have[w] && at < LP_CAP) {
+                    const unsigned i = first + Part::place(w * 32 + __builtin_ctz(have[w]));
+                    s_keys[at] = logit_key(logit_order(to_f32(x[i])), i);
                 }
             }
         }
         __syncthreads();
         int count = s_count;
         if (count > LP_CAP) {
-            // Many equal ones, or most of a wave's ruled out: the k-th largest, bit by bit, and of those that equal it the lowest places.
-            auto count_of = [&](int slot, auto take) {
-                int n = 0;
-                // a new value to the compiler: it would keep orders and masks of all elements over the loops
-#pragma unroll
-                for (int c = 0; c < C; ++c) asm volatile("" : "+v"(p.raw[c].x), "+v"(p.raw[c].y), "+v"(p.raw[c].z), "+v"(p.raw[c].w));
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    const float v = p.at(i);
-                    n += v > -INFINITY && take(logit_order(v), Part::place(i));
-                }
-                if (n) atomicAdd(&s_counts[slot], n);
-                __syncthreads();
-                return s_counts[slot];
+            // Many equal ones, or most of a wave's ruled out: the k-th largest of (logit, place), 8 bits a round, from memory again; then those from it on.
+            auto key_at = [&](unsigned i, unsigned place) {
+                const float v = to_f32(x[i]);
+                return v > -INFINITY ? (u64)logit_order(v) << 16 | (0xffff - place) : 0ull;
             };
-            unsigned kth = 0, last = 0;
-            for (int bit = 31; bit >= 0; --bit) {
-                const unsigned from = kth | 1u << bit;
-                if (count_of(bit, [&](unsigned o, unsigned) { return o >= from; }) >= a.k) kth = from;
-            }
-            const int equal = a.k - count_of(32, [&](unsigned o, unsigned) { return o > kth; });
-            static_assert(Part::SPAN <= 1 << 15, "a count for each bit of a place");
-            for (int bit = 14; bit >= 0; --bit) {
-                const unsigned below = last | 1u << bit;
-                if (count_of(33 + bit, [&](unsigned o, unsigned i) { return o == kth && i < below; }) < equal) last = below;
+            u64 kth = 0;
+            int need = a.k;
+            for (int shift = 40; shift >= 0; shift -= 8) {
+                s_counts[tid] = 0;
+                __syncthreads();
+                for (unsigned i = tid; i < a.span; i += LP_THREADS) {
+                    const u64 key = first + i < end ? key_at(first + i, i) : 0;
+                    if (key && key >> shift >> 8 == kth >> shift >> 8) atomicAdd(&s_counts[key >> shift & 255], 1);
+                }
+                __syncthreads();
+                int above = 0;
+                for (int j = tid + 1; j < 256; ++j) above += s_counts[j];
+                if (above < need && above + s_counts[tid] >= need) {
+                    s_count = above;
+                    s_digit = tid;
+                }
+                __syncthreads();
+                need -= s_count;
+                kth |= (u64)s_digit << shift;
+                __syncthreads();
             }
             if (tid == 0) s_count = 0;
             __syncthreads();
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float v = p.at(i);
-                const unsigned o = logit_order(v);
-                if (v > -INFINITY && (o > kth || (o == kth && Part::place(i) <= last))) s_keys[atomicAdd(&s_count, 1)] = logit_key(o, first + Part::place(i));
+            for (unsigned i = tid; i < a.span; i += LP_THREADS) {
+                const u64 key = first + i < end ? key_at(first + i, i) : 0;
+                if (key >= kth) s_keys[atomicAdd(&s_count, 1)] = logit_key((unsigned)(key >> 16), first + i);
             }
             __syncthreads();
             count = a.k;
@@ -316,7 +379,10 @@ template <typename T> __global__ __launch_bounds__(LP_THREADS) void logprob_join
         }
         __syncthreads();
     }
-    const Sums t = join_sums(Sums{s[0], s[1], s[2]}, a.c);
+    Sums t{lanes_max(s[0]), s[1], s[2]}, mine{s[0], s[1], s[2]};
+    sums_to(mine, t.M, a.c);
+    t.S = wave_sum(mine.S);
+    t.Y = wave_sum(mine.Y);
     if (a.parts > 1) {
         if (tid == 0) *(f32x4*)(a.sums + (int64_t)blockIdx.x * 4) = f32x4{t.M, t.S, t.Y, 0.f};
     } else {
@@ -325,15 +391,17 @@ template <typename T> __global__ __launch_bounds__(LP_THREADS) void logprob_join
 }
 
 // ---------------------------------------------------------------- launches
-struct LogprobPlan { int chunks; unsigned parts; };
+struct LogprobPlan { int chunks; unsigned parts, span; };
 static unsigned parts_of(int64_t n, int span) { return (unsigned)((n + span - 1) / span); }
 static LogprobPlan logprob_plan(const LogprobArgs& a)
 {
     const int v = a.dtype == DT_F32 ? 4 : 8, most = a.dtype == DT_F32 ? 8 : 4;
     const bool aligned = ((uintptr_t)a.logits & 15) == 0 && a.row_stride % v == 0;
     const int64_t n = (int64_t)a.n + (aligned ? 0 : v - 1);
-    LogprobPlan p{1, parts_of(n, LP_THREADS * v)};
+    LogprobPlan p{1, parts_of(n, LP_THREADS * v), 0};
     while (p.chunks < most && p.parts > 1 && (p.parts > LP_JOIN || (int64_t)p.parts * a.rows > 256)) p.parts = parts_of(n, LP_THREADS * v * (p.chunks *= 2));
+    p.span = (unsigned)((n + p.parts - 1) / p.parts + 64 * v - 1) / (64 * v) * (64 * v);       // equal ones, of whole KB
+    p.parts = parts_of(n, p.span);
     return p;
 }
 static size_t level_bytes(int64_t rows, unsigned parts, int k) { return (size_t)rows * parts * (16 + 8 * (size_t)k); }
@@ -384,6 +452,7 @@ template <typename T> static hipError_t launch_logprobs_t(const LogprobArgs& a, 
             k.lists = (u64*)(w + (size_t)rows * parts * 16);
             w += level_bytes(rows, parts, a.k);
         };
+        k.span = p.span;
         level(p.parts);
         const unsigned wgs = (unsigned)(rows * p.parts);
         if (p.chunks == 1) logprob_part_kernel<T, 1><<<wgs, LP_THREADS, 0, s>>>(k);
