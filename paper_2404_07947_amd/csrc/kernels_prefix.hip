@@ -8,7 +8,7 @@
 // it; the host's bounds only size the launch.
 #include <algorithm>
 
-#include "chunk.h"
+#include "chunk_tile.h"
 
 namespace exe {
 
@@ -27,7 +27,8 @@ struct PrefixKernelArgs {
     // Keys go to workgroups in parts of `keys`, at most `parts` (the last takes what is left).  Part i of row r: acc[i * rows + r][DH], ml[i * rows +
     // r][maximum, sum], the prefix's parts in front of the own ones'.
     struct Cut { int parts, keys; } shared, own;
-    float *acc, *ml;
+    struct { int64_t rows; float *acc, *ml; } tile;
+    static constexpr int window = 0;
     int slots, own_tiles;             // of prefix tiles; tiles of a sequence's rows side by side
     unsigned shared_units, own_units; // workgroups of each kind
 };
@@ -113,15 +114,16 @@ __device__ __forceinline__ KeyRange part_of(KeyRange k, const PrefixKernelArgs::
 template <typename T, int DH> struct PrefixStream {
     static constexpr int RB = DH * (int)sizeof(T), TILE = PX_STEP * RB, STAGE = 2 * TILE;
     static constexpr int FIT = 16384 / STAGE, STAGES = FIT < 2 ? 2 : FIT, LOADS = TILE / 1024;
-    static constexpr int MERGE = PX_WAVES * 16 * (DH + 4) * 4;            // bytes of the waves' results, over the stages
-    static constexpr int LDS = PX_WAVES * STAGES * STAGE > MERGE ? PX_WAVES * STAGES * STAGE : MERGE;
+    static constexpr int LDS = PX_WAVES * STAGES * STAGE, MERGE = PX_WAVES * 16 * (DH + 4) * 4;      // bytes of the waves' results, over the stages
+    static_assert(MERGE + PX_WAVES * 16 * 8 <= LDS, "results, maxima and sums");
+    static constexpr int QUERIES = 4 * 16 * RB;                           // of four blocks of rows, behind the stages
 };
 
 // Query rows r0 .. r1 - 1 of a run of packed tokens from t0 on (row r: token t0 + r / G, head kvh * G + r % G) against keys k of table row b; row
 // r sees keys lo .. hi(r) - 1 of them.  Every wave takes steps of 16 keys of its own through a ring of stages in LDS, as chunk_stream_kernel does,
 // with QB blocks of 16 rows: S^T = K . Q^T, O^T += V^T . P^T.  The result goes to part `part`.
 template <typename T, int DH, int QB, bool NT, typename F>
-__device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned char* smem, float (*s_ml)[16][2], int b, int kvh, int t0, int r0, int r1,
+__device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned char* smem, int b, int kvh, int t0, int r0, int r1,
                                             KeyRange k, int lo, F hi, int part)
 {
     typedef PrefixStream<T, DH> S;
@@ -133,14 +135,23 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
     const float mul = exponent_scale(a.scale);
     const int limit = table_limit(a.table);
 
-    u32x4 qf[QB][DS];
+    constexpr bool QLDS = QB == 4;                                       // four blocks of queries leave no registers for the sums
+    const int blocks = (r1 - r0 + 15) / 16;                              // those that are there
+    u32x4 qf[QLDS ? 1 : QB][DS];
+    u32x4* s_q = (u32x4*)(smem + S::LDS) + lane;
     int last[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         const int r = r0 + qb * 16 + qi, row = r < r1 ? r : r1 - 1, t = t0 + row / G;
         last[qb] = hi(row);
-        load_query<T, DS>((const T*)a.q + (int64_t)(t >= 0 && t < a.tokens ? t : 0) * a.q_stride + (kvh * G + row % G) * DH, g, a.scale, qf[qb]);
+        if (QLDS && qb != wave) continue;
+        load_query<T, DS>((const T*)a.q + (int64_t)(t >= 0 && t < a.tokens ? t : 0) * a.q_stride + (kvh * G + row % G) * DH, g, a.scale, qf[QLDS ? 0 : qb]);
+        if (QLDS) {
+#pragma unroll
+            for (int ds = 0; ds < DS; ++ds) s_q[(qb * DS + ds) * 64] = qf[0][ds];
+        }
     }
+    if (QLDS) __syncthreads();
     const int least = hi(r0);                                            // the first row sees the fewest
     const int steps = k.last > k.first ? (k.last - k.first + PX_STEP - 1) / PX_STEP : 0, own = steps > wave ? (steps - wave + PX_WAVES - 1) / PX_WAVES : 0;
     typedef RowLoader<T, DH, NT> Loader;
@@ -182,11 +193,25 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
         f32x4 s[QB][2];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) s[qb][0] = s[qb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (QLDS) {
+            u32x4 fk[DS];
 #pragma unroll
-        for (int ds = 0; ds < DS; ++ds) {
-            const u32x4 fk = *(const u32x4*)(sK + qi * RB + (((ds * 4 + g) ^ pf_swz<RB>(qi)) << 4));
+            for (int ds = 0; ds < DS; ++ds) fk[ds] = *(const u32x4*)(sK + qi * RB + (((ds * 4 + g) ^ pf_swz<RB>(qi)) << 4));
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) s[qb][QB < 4 ? ds & 1 : 0] = HalfUnit<T>::mma(fk, qf[qb][ds], s[qb][QB < 4 ? ds & 1 : 0]);
+            for (int qb = 0; qb < QB; ++qb) {
+                if (qb >= blocks) break;
+#pragma unroll
+                for (int ds = 0; ds < DS; ++ds) s[qb][0] = HalfUnit<T>::mma(fk[ds], s_q[(qb * DS + ds) * 64], s[qb][0]);
+                __builtin_amdgcn_sched_barrier(0);                       // queries of one block at a time
+            }
+        } else {
+#pragma unroll
+            for (int ds = 0; ds < DS; ++ds) {
+                const u32x4 fk = *(const u32x4*)(sK + qi * RB + (((ds * 4 + g) ^ pf_swz<RB>(qi)) << 4));
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb)
+                    if (qb < blocks) s[qb][ds & 1] = HalfUnit<T>::mma(fk, qf[qb][ds], s[qb][ds & 1]);
+            }
         }
         const unsigned char* sV = sK + S::TILE;
         const int v_row = 4 * g + (qi >> 2), v_q = qi & 3;
@@ -229,6 +254,7 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
         }
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
+            if (qb >= blocks) break;
             const float ref = m[qb] == -INFINITY ? 0.f : m[qb];
             f32x4& p = s[qb][0];
 #pragma unroll
@@ -271,6 +297,7 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
 
     // the waves' results, joined, 16 rows at a time; lane (qi, g) holds features 16 * dt + 4 * g .. +3 of its row
     float* s_o = (float*)smem;
+    float (*s_ml)[16][2] = (float (*)[16][2])(smem + S::MERGE);
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         if (r0 + qb * 16 >= r1) break;
@@ -300,9 +327,9 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
                 f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int i = 0; i < PX_WAVES; ++i) v += *(const f32x4*)(s_o + (i * 16 + r) * (DH + 4) + f * 64 + 4 * c) * w[i];
-                *(f32x4*)(a.acc + at * DH + f * 64 + 4 * c) = v;
+                *(f32x4*)(a.tile.acc + at * DH + f * 64 + 4 * c) = v;
             }
-            if (c == 0) *(float2*)(a.ml + at * 2) = float2{M, hi(row) > lo ? L : NO_KEYS};
+            if (c == 0) *(float2*)(a.tile.ml + at * 2) = float2{M, hi(row) > lo ? L : NO_KEYS};
         }
     }
     __syncthreads();                                                     // before the next tile's loads overwrite the results
@@ -312,36 +339,41 @@ __device__ __forceinline__ void no_part(const PrefixKernelArgs& a, int kvh, int 
 {
     const int row = r0 + threadIdx.x, t = t0 + row / a.G;
     if (row < r1 && t >= 0 && t < a.tokens)
-        *(float2*)(a.ml + (((int64_t)part * a.tokens + t) * a.H + kvh * a.G + row % a.G) * 2) = float2{-INFINITY, NO_PART};
+        *(float2*)(a.tile.ml + (((int64_t)part * a.tokens + t) * a.H + kvh * a.G + row % a.G) * 2) = float2{-INFINITY, NO_PART};
 }
 
-// Bound by reading the cache where contexts are long.
-template <typename T, int DH, int QB> __global__ __launch_bounds__(PX_THREADS, 2) void prefix_stream_kernel(PrefixKernelArgs a)
+// Tile of the prefix for workgroup wg: of tiles with 2^SHIFT rows, those that read the same keys follow each other on one XCD.  b = -1: there is
+// none.  What the prefix has no keys for is marked here.
+struct PrefixTile { ChunkTile tile; int r1, part; KeyRange k; };
+template <int SHIFT> __device__ __forceinline__ PrefixTile find_prefix(const PrefixKernelArgs& a, unsigned wg, int limit, int lane)
 {
-    constexpr int SHIFT = QB == 1 ? 4 : QB == 2 ? 5 : 6, ROWS = 16 * QB;
-    extern __shared__ __align__(16) unsigned char px_smem[];
-    __shared__ float s_ml[PX_WAVES][16][2];
-    const int lane = threadIdx.x & 63, limit = table_limit(a.table), G = a.G;
-    unsigned wg = blockIdx.x;
-    if (wg < a.shared_units) {
-        // tiles that read the same keys one after the other on one XCD
-        const unsigned u = (wg & 7) + 8 * ((wg >> 3) / a.slots), slot = (wg >> 3) % a.slots;
-        if (u >= (unsigned)(a.Hkv * a.shared.parts)) return;
-        const int kvh = u % a.Hkv, part = u / a.Hkv;
-        const PrefixGroup gr = find_group<true>(a, slot, SHIFT, lane);
-        if (gr.g < 0) return;
-        const int n = gr.t1 - gr.t0 < a.tokens ? gr.t1 - gr.t0 : a.tokens, rows = n * G;
-        const int r0 = (int)(slot - (unsigned)((int)((int64_t)gr.t0 * G >> SHIFT) + gr.g)) << SHIFT;
-        if (n <= 0 || r0 >= rows) return;
-        const int r1 = r0 + ROWS < rows ? r0 + ROWS : rows, end = gr.prefix < limit ? gr.prefix : limit;
-        const KeyRange all{0, end};
-        const int parts = end > 0 ? parts_of(all, a.shared) : 0;
-        if (part >= parts) return no_part(a, kvh, gr.t0, r0, r1, part);
-        stream_rows<T, DH, QB, false>(a, px_smem, s_ml, gr.b0, kvh, gr.t0, r0, r1, part_of(all, a.shared, part, parts), 0, [&](int) { return end; }, part);
-        return;
+    PrefixTile r;
+    r.tile.b = -1;
+    const unsigned u = (wg & 7) + 8 * ((wg >> 3) / a.slots), slot = (wg >> 3) % a.slots;
+    if (u >= (unsigned)(a.Hkv * a.shared.parts)) return r;
+    const int kvh = u % a.Hkv;
+    r.part = u / a.Hkv;
+    const PrefixGroup gr = find_group<true>(a, slot, SHIFT, lane);
+    if (gr.g < 0) return r;
+    const int n = gr.t1 - gr.t0 < a.tokens ? gr.t1 - gr.t0 : a.tokens, rows = n * a.G;
+    const int r0 = (int)(slot - (unsigned)((int)((int64_t)gr.t0 * a.G >> SHIFT) + gr.g)) << SHIFT;
+    if (n <= 0 || r0 >= rows) return r;
+    r.r1 = r0 + (1 << SHIFT) < rows ? r0 + (1 << SHIFT) : rows;
+    const int end = gr.prefix < limit ? gr.prefix : limit;
+    const KeyRange all{0, end};
+    const int parts = end > 0 ? parts_of(all, a.shared) : 0;
+    if (r.part >= parts) {
+        no_part(a, kvh, gr.t0, r0, r.r1, r.part);
+        return r;
     }
-    wg -= a.shared_units;
-    const int part = wg % a.own.parts, tile = wg / a.own.parts % a.own_tiles, head = wg / a.own.parts / a.own_tiles, kvh = head % a.Hkv, b = head / a.Hkv;
+    r.tile = ChunkTile{gr.b0, kvh, gr.t0, r.r1, 0, r0};
+    r.k = part_of(all, a.shared, r.part, parts);
+    return r;
+}
+// A sequence's own positions, by workgroup wg of those.
+template <typename T, int DH> __device__ __forceinline__ void own_rows(const PrefixKernelArgs& a, unsigned char* smem, unsigned wg, int limit, int lane)
+{
+    const int G = a.G, part = wg % a.own.parts, tile = wg / a.own.parts % a.own_tiles, head = wg / a.own.parts / a.own_tiles, kvh = head % a.Hkv, b = head / a.Hkv;
     const int t0 = a.cu[b], end = a.cu[b + 1], p_end = a.len[b], n = end - t0 < a.tokens ? end - t0 : a.tokens, p0 = p_end - n;
     const PrefixGroup gr = find_group<false>(a, b, 0, lane);
     if (n <= 0) return;
@@ -352,8 +384,30 @@ template <typename T, int DH, int QB> __global__ __launch_bounds__(PX_THREADS, 2
         const KeyRange all{lo & -PX_STEP, hi(r1 - 1)};
         const int parts = parts_of(all, a.own);
         if (part >= parts) no_part(a, kvh, t0, r0, r1, a.shared.parts + part);
-        else stream_rows<T, DH, 1, true>(a, px_smem, s_ml, b, kvh, t0, r0, r1, part_of(all, a.own, part, parts), lo, hi, a.shared.parts + part);
+        else stream_rows<T, DH, 1, true>(a, smem, b, kvh, t0, r0, r1, part_of(all, a.own, part, parts), lo, hi, a.shared.parts + part);
     }
+}
+
+// Up to 64 rows of a group and key/value head, and own positions.  Bound by reading the cache where contexts are long.
+template <typename T, int DH, int QB> __global__ __launch_bounds__(PX_THREADS, 2) void prefix_stream_kernel(PrefixKernelArgs a)
+{
+    extern __shared__ __align__(16) unsigned char px_smem[];
+    const int lane = threadIdx.x & 63, limit = table_limit(a.table);
+    if (blockIdx.x >= a.shared_units) return own_rows<T, DH>(a, px_smem, blockIdx.x - a.shared_units, limit, lane);
+    const PrefixTile p = find_prefix<QB == 1 ? 4 : QB == 2 ? 5 : 6>(a, blockIdx.x, limit, lane);
+    if (p.tile.b < 0) return;
+    const int end = p.k.last;
+    stream_rows<T, DH, QB, false>(a, px_smem, p.tile.b, p.tile.kvh, p.tile.t0, p.tile.r0, p.r1, p.k, 0, [&](int) { return end; }, p.part);
+}
+// More rows, in tiles of 128, beside own positions.  Bound by MFMAs and softmax, as chunk_tile_kernel is.
+template <typename T, int DH> __global__ __launch_bounds__(PX_THREADS, 2) void prefix_tile_kernel(PrefixKernelArgs a)
+{
+    extern __shared__ __align__(16) unsigned char px_smem[];
+    const int lane = threadIdx.x & 63, limit = table_limit(a.table);
+    if (blockIdx.x >= a.shared_units) return own_rows<T, DH>(a, px_smem, blockIdx.x - a.shared_units, limit, lane);
+    const PrefixTile p = find_prefix<7>(a, blockIdx.x, limit, lane);
+    if (p.tile.b < 0) return;
+    tile_rows<T, DH, 2, true>(a, px_smem, p.tile, p.k, p.part, 2, [](int, int, KeyRange) {});
 }
 
 // The sum over a row's parts of 2^(m_i - M) times their sums, in their order: a wave per row, DH / 4 lanes a part, 2 or 4 parts at a time.
@@ -366,11 +420,11 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void prefix_join
     const int parts = a.shared.parts + a.own.parts, sub = lane / PER, f = lane % PER * 4;
     const int64_t at = (int64_t)t * a.H + h, step = (int64_t)a.tokens * a.H;
     const int packed = a.cu[a.n_seqs];
-    const float2 x = lane < parts ? *(const float2*)(a.ml + (at + lane * step) * 2) : float2{-INFINITY, NO_PART};
+    const float2 x = lane < parts ? *(const float2*)(a.tile.ml + (at + lane * step) * 2) : float2{-INFINITY, NO_PART};
     if (t >= packed) return;
     const float M = wave_max(x.x), w = x.y == NO_PART ? -1.f : fast_exp2(x.x - (M == -INFINITY ? 0.f : M)), L = wave_sum(x.y < 0.f ? 0.f : x.y * w);
     const bool none = __builtin_amdgcn_ballot_w64(x.y == NO_KEYS);
-    const float* acc = a.acc + at * DH + f;
+    const float* acc = a.tile.acc + at * DH + f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     for (int i = 0; i < parts; i += SUBS) {
         const int k = i + sub;
@@ -407,7 +461,7 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void prefix_join
 
 // ---------------------------------------------------------------- launches
 struct PrefixPlan {
-    int qb;
+    int qb;                                               // blocks of 16 rows of a prefix tile
     PrefixKernelArgs::Cut shared, own;
     int own_tiles;
     int64_t slots, shared_units, own_units;
@@ -425,7 +479,7 @@ static PrefixPlan prefix_plan(const PrefixAttnArgs& a)
 {
     PrefixPlan p{};
     const int64_t G = a.H / a.Hkv, rows = (int64_t)a.max_group * G;
-    p.qb = a.n_groups == 0 || rows <= 16 ? 1 : rows <= 32 || a.dtype == DT_F32 ? 2 : 4;
+    p.qb = a.n_groups == 0 || rows <= 16 ? 1 : rows <= 32 || a.dtype == DT_F32 ? 2 : rows <= 64 ? 4 : 8;
     p.slots = (int64_t)a.tokens * G / (16 * p.qb) + a.n_groups + 1;
     const int64_t most = (int64_t)a.tokens * G / (16 * p.qb) + a.n_groups, each = a.n_groups * ceil_div(rows, 16 * p.qb), tiles = (each < most ? each : most) * a.Hkv;
     const int64_t own = a.n_seqs * a.Hkv, own_rows = ceil_div(a.max_new * G, 16);
@@ -445,28 +499,48 @@ size_t prefix_attn_workspace(const PrefixAttnArgs& a)
     return (size_t)(p.shared.parts + p.own.parts) * a.tokens * a.H * (a.dh + 2) * sizeof(float);
 }
 
+template <typename K> static hipError_t launch_kernel(K kernel, LdsLimit (&limit)[MAX_DEVICES], int lds, const PrefixKernelArgs& k, int64_t wgs, hipStream_t s)
+{
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) dev = 0;
+    hipError_t e = limit[dev].raise((const void*)kernel, lds);
+    if (e != hipSuccess) return e;
+    kernel<<<(unsigned)wgs, PX_THREADS, lds, s>>>(k);
+    return hipGetLastError();
+}
 template <typename T, int DH, int QB> static hipError_t launch_stream(const PrefixKernelArgs& k, int64_t wgs, hipStream_t s)
 {
     static LdsLimit limit[MAX_DEVICES];
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) dev = 0;
-    hipError_t e = limit[dev].raise((const void*)prefix_stream_kernel<T, DH, QB>, PrefixStream<T, DH>::LDS);
-    if (e != hipSuccess) return e;
-    prefix_stream_kernel<T, DH, QB><<<(unsigned)wgs, PX_THREADS, PrefixStream<T, DH>::LDS, s>>>(k);
-    return hipGetLastError();
+    return launch_kernel(prefix_stream_kernel<T, DH, QB>, limit, PrefixStream<T, DH>::LDS + (QB == 4 ? PrefixStream<T, DH>::QUERIES : 0), k, wgs, s);
+}
+template <typename T, int DH> static hipError_t launch_tile(const PrefixKernelArgs& k, int64_t wgs, hipStream_t s)
+{
+    static LdsLimit limit[MAX_DEVICES];
+    return launch_kernel(prefix_tile_kernel<T, DH>, limit, std::max(PrefixStream<T, DH>::LDS, ct_lds<T, DH, 2>()), k, wgs, s);
 }
 template <typename T, int DH> static hipError_t launch_prefix(const PrefixAttnArgs& a, hipStream_t s)
 {
     const PrefixPlan p = prefix_plan(a);
     const int64_t wgs = p.shared_units + p.own_units, rows = (int64_t)a.tokens * a.H;
     if (p.slots > 0x7fffffff || wgs * PX_THREADS > MAX_LAUNCH_THREADS || rows / 4 + a.tokens > MAX_LAUNCH_THREADS / PX_THREADS) return hipErrorInvalidValue;
-    PrefixKernelArgs k{a.cu, a.len, a.cu_groups, a.prefix, a.n_seqs, a.tokens, a.n_groups, a.q, a.q_stride, a.kv_blocks, a.table, a.H, a.Hkv, a.H / a.Hkv, a.scale, a.out,
-                       a.out_stride, p.shared, p.own, a.workspace, a.workspace + (size_t)(p.shared.parts + p.own.parts) * rows * DH, (int)p.slots, p.own_tiles,
-                       (unsigned)p.shared_units, (unsigned)p.own_units};
+    PrefixKernelArgs k{};
+    k.cu = a.cu; k.len = a.len; k.cu_groups = a.cu_groups; k.prefix = a.prefix;
+    k.n_seqs = a.n_seqs; k.tokens = a.tokens; k.n_groups = a.n_groups;
+    k.q = a.q; k.q_stride = a.q_stride;
+    k.kv_blocks = a.kv_blocks;
+    k.table = a.table;
+    k.H = a.H; k.Hkv = a.Hkv; k.G = a.H / a.Hkv;
+    k.scale = a.scale;
+    k.out = a.out; k.out_stride = a.out_stride;
+    k.shared = p.shared; k.own = p.own;
+    k.tile = {rows, a.workspace, a.workspace + (size_t)(p.shared.parts + p.own.parts) * rows * DH};
+    k.slots = (int)p.slots; k.own_tiles = p.own_tiles;
+    k.shared_units = (unsigned)p.shared_units; k.own_units = (unsigned)p.own_units;
     hipError_t e;
     if (p.qb == 1) e = launch_stream<T, DH, 1>(k, wgs, s);
-    else if (sizeof(T) == 4 || p.qb == 2) e = launch_stream<T, DH, 2>(k, wgs, s);
-    else e = launch_stream<T, DH, sizeof(T) == 4 ? 2 : 4>(k, wgs, s);
+    else if (p.qb == 2) e = launch_stream<T, DH, 2>(k, wgs, s);
+    else if constexpr (sizeof(T) == 2) e = p.qb == 4 ? launch_stream<T, DH, 4>(k, wgs, s) : launch_tile<T, DH>(k, wgs, s);
+    else e = hipErrorInvalidValue;
     if (e != hipSuccess) return e;
     prefix_join_kernel<T, DH><<<(unsigned)(a.tokens * ceil_div(a.H, 4)), 256, 0, s>>>(k);
     return hipGetLastError();
