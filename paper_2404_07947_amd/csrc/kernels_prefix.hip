@@ -12,7 +12,7 @@
 
 namespace exe {
 
-constexpr int PX_WAVES = 4, PX_STEP = 16, PX_THREADS = PX_WAVES * WAVE, PX_PARTS = WAVE;
+constexpr int PX_STEP = 16, PX_PARTS = WAVE;
 constexpr float NO_PART = -2.f, NO_KEYS = -1.f;       // in place of a sum of probabilities: a part that is not there, a row without keys
 
 struct PrefixKernelArgs {
@@ -111,52 +111,42 @@ __device__ __forceinline__ KeyRange part_of(KeyRange k, const PrefixKernelArgs::
     return KeyRange{first, part + 1 < parts ? first + cut.keys : k.last};
 }
 
-template <typename T, int DH> struct PrefixStream {
+template <typename T, int DH, int WAVES> struct PrefixStream {
     static constexpr int RB = DH * (int)sizeof(T), TILE = PX_STEP * RB, STAGE = 2 * TILE;
     static constexpr int FIT = 16384 / STAGE, STAGES = FIT < 2 ? 2 : FIT, LOADS = TILE / 1024;
-    static constexpr int LDS = PX_WAVES * STAGES * STAGE, MERGE = PX_WAVES * 16 * (DH + 4) * 4;      // bytes of the waves' results, over the stages
-    static_assert(MERGE + PX_WAVES * 16 * 8 <= LDS, "results, maxima and sums");
-    static constexpr int QUERIES = 4 * 16 * RB;                           // of four blocks of rows, behind the stages
+    static constexpr int LDS = WAVES * STAGES * STAGE, MERGE = WAVES * 16 * (DH + 4) * 4;      // bytes of the waves' results, over the stages
+    static_assert(MERGE + WAVES * 16 * 8 <= LDS, "results, maxima and sums");
 };
 
 // Query rows r0 .. r1 - 1 of a run of packed tokens from t0 on (row r: token t0 + r / G, head kvh * G + r % G) against keys k of table row b; row
 // r sees keys lo .. hi(r) - 1 of them.  Every wave takes steps of 16 keys of its own through a ring of stages in LDS, as chunk_stream_kernel does,
 // with QB blocks of 16 rows: S^T = K . Q^T, O^T += V^T . P^T.  The result goes to part `part`.
-template <typename T, int DH, int QB, bool NT, typename F>
+template <typename T, int DH, int QB, int WAVES, bool NT, typename F>
 __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned char* smem, int b, int kvh, int t0, int r0, int r1,
                                             KeyRange k, int lo, F hi, int part)
 {
-    typedef PrefixStream<T, DH> S;
+    typedef PrefixStream<T, DH, WAVES> S;
     constexpr int RB = S::RB, DS = RB / 64, DT = DH / 16;
-    constexpr bool TWO = sizeof(T) == 2 && QB <= 2;                      // probabilities as two bf16 parts, 2^-17 relative, where loads hide it; else rounded once
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), qi = lane & 15, g = lane >> 4, G = a.G;
     const unsigned lds = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem + wave * (S::STAGES * S::STAGE);
     const unsigned char* mine = smem + wave * (S::STAGES * S::STAGE);
     const float mul = exponent_scale(a.scale);
     const int limit = table_limit(a.table);
 
-    constexpr bool QLDS = QB == 4;                                       // four blocks of queries leave no registers for the sums
     const int blocks = (r1 - r0 + 15) / 16;                              // those that are there
-    u32x4 qf[QLDS ? 1 : QB][DS];
-    u32x4* s_q = (u32x4*)(smem + S::LDS) + lane;
+    u32x4 qf[QB][DS];
     int last[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         const int r = r0 + qb * 16 + qi, row = r < r1 ? r : r1 - 1, t = t0 + row / G;
         last[qb] = hi(row);
-        if (QLDS && qb != wave) continue;
-        load_query<T, DS>((const T*)a.q + (int64_t)(t >= 0 && t < a.tokens ? t : 0) * a.q_stride + (kvh * G + row % G) * DH, g, a.scale, qf[QLDS ? 0 : qb]);
-        if (QLDS) {
-#pragma unroll
-            for (int ds = 0; ds < DS; ++ds) s_q[(qb * DS + ds) * 64] = qf[0][ds];
-        }
+        load_query<T, DS>((const T*)a.q + (int64_t)(t >= 0 && t < a.tokens ? t : 0) * a.q_stride + (kvh * G + row % G) * DH, g, a.scale, qf[qb]);
     }
-    if (QLDS) __syncthreads();
     const int least = hi(r0);                                            // the first row sees the fewest
-    const int steps = k.last > k.first ? (k.last - k.first + PX_STEP - 1) / PX_STEP : 0, own = steps > wave ? (steps - wave + PX_WAVES - 1) / PX_WAVES : 0;
+    const int steps = k.last > k.first ? (k.last - k.first + PX_STEP - 1) / PX_STEP : 0, own = steps > wave ? (steps - wave + WAVES - 1) / WAVES : 0;
     typedef RowLoader<T, DH, NT> Loader;
     const Loader from(a.table, a.kv_blocks, b, kvh, a.Hkv, limit, k.last, lane);
-    auto first_of = [&](int i) { return k.first + (wave + i * PX_WAVES) * PX_STEP; };
+    auto first_of = [&](int i) { return k.first + (wave + i * WAVES) * PX_STEP; };
     typename Loader::Entries en{-1, -1};
     auto issue = [&](int i) {
         const unsigned dst = lds + i % S::STAGES * S::STAGE;
@@ -193,25 +183,12 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
         f32x4 s[QB][2];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) s[qb][0] = s[qb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if constexpr (QLDS) {
-            u32x4 fk[DS];
 #pragma unroll
-            for (int ds = 0; ds < DS; ++ds) fk[ds] = *(const u32x4*)(sK + qi * RB + (((ds * 4 + g) ^ pf_swz<RB>(qi)) << 4));
+        for (int ds = 0; ds < DS; ++ds) {
+            const u32x4 fk = *(const u32x4*)(sK + qi * RB + (((ds * 4 + g) ^ pf_swz<RB>(qi)) << 4));
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
-                if (qb >= blocks) break;
-#pragma unroll
-                for (int ds = 0; ds < DS; ++ds) s[qb][0] = HalfUnit<T>::mma(fk[ds], s_q[(qb * DS + ds) * 64], s[qb][0]);
-                __builtin_amdgcn_sched_barrier(0);                       // queries of one block at a time
-            }
-        } else {
-#pragma unroll
-            for (int ds = 0; ds < DS; ++ds) {
-                const u32x4 fk = *(const u32x4*)(sK + qi * RB + (((ds * 4 + g) ^ pf_swz<RB>(qi)) << 4));
-#pragma unroll
-                for (int qb = 0; qb < QB; ++qb)
-                    if (qb < blocks) s[qb][ds & 1] = HalfUnit<T>::mma(fk, qf[qb][ds], s[qb][ds & 1]);
-            }
+            for (int qb = 0; qb < QB; ++qb)
+                if (qb < blocks) s[qb][ds & 1] = HalfUnit<T>::mma(fk, qf[qb][ds], s[qb][ds & 1]);
         }
         const unsigned char* sV = sK + S::TILE;
         const int v_row = 4 * g + (qi >> 2), v_q = qi & 3;
@@ -228,12 +205,11 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
             asm volatile("" : "+v"(key0));                               // keeps the mask arithmetic inside this branch
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
-                if (QB < 4) s[qb][0] += s[qb][1];
-                s[qb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                s[qb][0] += s[qb][1];
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[qb][0][r] = key0 + r >= lo && key0 + r < last[qb] ? s[qb][0][r] : -INFINITY;
             }
-        } else if (QB < 4) {
+        } else {
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) s[qb][0] += s[qb][1];
         }
@@ -272,7 +248,7 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
                 }
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
-                    if (TWO) o[qb][dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, fv[dt]), __builtin_bit_cast(v4s, low), o[qb][dt], 0, 0, 0);
+                    o[qb][dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, fv[dt]), __builtin_bit_cast(v4s, low), o[qb][dt], 0, 0, 0);
                     o[qb][dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(v4s, fv[dt]), __builtin_bit_cast(v4s, high), o[qb][dt], 0, 0, 0);
                 }
             }
@@ -310,23 +286,26 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
             s_ml[wave][qi][1] = total;
         }
         __syncthreads();
-        const int r = tid >> 4, c = tid & 15, row = r0 + qb * 16 + r, t = t0 + row / G;        // 16 threads a row, features 4 * c .. +3 of every 64
-        float M = -INFINITY, L = 0.f, w[PX_WAVES];
+        // 16 threads a row, features 4 * c .. +3 of every 64
 #pragma unroll
-        for (int i = 0; i < PX_WAVES; ++i) M = fmaxf(M, s_ml[i][r][0]);
-        const float ref = M == -INFINITY ? 0.f : M;
+        for (int r = tid >> 4; r < 16; r += WAVES * 4) {
+            const int c = tid & 15, row = r0 + qb * 16 + r, t = t0 + row / G;
+            float M = -INFINITY, L = 0.f, w[WAVES];
 #pragma unroll
-        for (int i = 0; i < PX_WAVES; ++i) {
-            w[i] = fast_exp2(s_ml[i][r][0] - ref);
-            L += s_ml[i][r][1] * w[i];
-        }
-        if (row < r1 && t >= 0 && t < a.tokens) {
+            for (int i = 0; i < WAVES; ++i) M = fmaxf(M, s_ml[i][r][0]);
+            const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) {
+                w[i] = fast_exp2(s_ml[i][r][0] - ref);
+                L += s_ml[i][r][1] * w[i];
+            }
+            if (row >= r1 || t < 0 || t >= a.tokens) continue;
             const int64_t at = ((int64_t)part * a.tokens + t) * a.H + kvh * G + row % G;
 #pragma unroll
             for (int f = 0; f < DH / 64; ++f) {
                 f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < PX_WAVES; ++i) v += *(const f32x4*)(s_o + (i * 16 + r) * (DH + 4) + f * 64 + 4 * c) * w[i];
+                for (int i = 0; i < WAVES; ++i) v += *(const f32x4*)(s_o + (i * 16 + r) * (DH + 4) + f * 64 + 4 * c) * w[i];
                 *(f32x4*)(a.tile.acc + at * DH + f * 64 + 4 * c) = v;
             }
             if (c == 0) *(float2*)(a.tile.ml + at * 2) = float2{M, hi(row) > lo ? L : NO_KEYS};
@@ -349,7 +328,7 @@ template <int SHIFT> __device__ __forceinline__ PrefixTile find_prefix(const Pre
 {
     PrefixTile r;
     r.tile.b = -1;
-    const unsigned u = (wg & 7) + 8 * ((wg >> 3) / a.slots), slot = (wg >> 3) % a.slots;
+    const unsigned units = (a.Hkv * a.shared.parts + 7) & ~7, slot = wg / units, u = wg - slot * units;
     if (u >= (unsigned)(a.Hkv * a.shared.parts)) return r;
     const int kvh = u % a.Hkv;
     r.part = u / a.Hkv;
@@ -371,7 +350,7 @@ template <int SHIFT> __device__ __forceinline__ PrefixTile find_prefix(const Pre
     return r;
 }
 // A sequence's own positions, by workgroup wg of those.
-template <typename T, int DH> __device__ __forceinline__ void own_rows(const PrefixKernelArgs& a, unsigned char* smem, unsigned wg, int limit, int lane)
+template <typename T, int DH, int WAVES> __device__ __forceinline__ void own_rows(const PrefixKernelArgs& a, unsigned char* smem, unsigned wg, int limit, int lane)
 {
     const int G = a.G, part = wg % a.own.parts, tile = wg / a.own.parts % a.own_tiles, head = wg / a.own.parts / a.own_tiles, kvh = head % a.Hkv, b = head / a.Hkv;
     const int t0 = a.cu[b], end = a.cu[b + 1], p_end = a.len[b], n = end - t0 < a.tokens ? end - t0 : a.tokens, p0 = p_end - n;
@@ -384,27 +363,27 @@ template <typename T, int DH> __device__ __forceinline__ void own_rows(const Pre
         const KeyRange all{lo & -PX_STEP, hi(r1 - 1)};
         const int parts = parts_of(all, a.own);
         if (part >= parts) no_part(a, kvh, t0, r0, r1, a.shared.parts + part);
-        else stream_rows<T, DH, 1, true>(a, smem, b, kvh, t0, r0, r1, part_of(all, a.own, part, parts), lo, hi, a.shared.parts + part);
+        else stream_rows<T, DH, 1, WAVES, true>(a, smem, b, kvh, t0, r0, r1, part_of(all, a.own, part, parts), lo, hi, a.shared.parts + part);
     }
 }
 
-// Up to 64 rows of a group and key/value head, and own positions.  Bound by reading the cache where contexts are long.
-template <typename T, int DH, int QB> __global__ __launch_bounds__(PX_THREADS, 2) void prefix_stream_kernel(PrefixKernelArgs a)
+// Up to 32 rows of a group and key/value head (float: in tiles of 32), and own positions.  Bound by reading the cache where contexts are long.
+template <typename T, int DH, int QB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void prefix_stream_kernel(PrefixKernelArgs a)
 {
     extern __shared__ __align__(16) unsigned char px_smem[];
     const int lane = threadIdx.x & 63, limit = table_limit(a.table);
-    if (blockIdx.x >= a.shared_units) return own_rows<T, DH>(a, px_smem, blockIdx.x - a.shared_units, limit, lane);
-    const PrefixTile p = find_prefix<QB == 1 ? 4 : QB == 2 ? 5 : 6>(a, blockIdx.x, limit, lane);
+    if (blockIdx.x >= a.shared_units) return own_rows<T, DH, WAVES>(a, px_smem, blockIdx.x - a.shared_units, limit, lane);
+    const PrefixTile p = find_prefix<QB == 1 ? 4 : 5>(a, blockIdx.x, limit, lane);
     if (p.tile.b < 0) return;
     const int end = p.k.last;
-    stream_rows<T, DH, QB, false>(a, px_smem, p.tile.b, p.tile.kvh, p.tile.t0, p.tile.r0, p.r1, p.k, 0, [&](int) { return end; }, p.part);
+    stream_rows<T, DH, QB, WAVES, false>(a, px_smem, p.tile.b, p.tile.kvh, p.tile.t0, p.tile.r0, p.r1, p.k, 0, [&](int) { return end; }, p.part);
 }
 // More rows, in tiles of 128, beside own positions.  Bound by MFMAs and softmax, as chunk_tile_kernel is.
-template <typename T, int DH> __global__ __launch_bounds__(PX_THREADS, 2) void prefix_tile_kernel(PrefixKernelArgs a)
+template <typename T, int DH> __global__ __launch_bounds__(CT_WAVES * 64, 2) void prefix_tile_kernel(PrefixKernelArgs a)
 {
     extern __shared__ __align__(16) unsigned char px_smem[];
     const int lane = threadIdx.x & 63, limit = table_limit(a.table);
-    if (blockIdx.x >= a.shared_units) return own_rows<T, DH>(a, px_smem, blockIdx.x - a.shared_units, limit, lane);
+    if (blockIdx.x >= a.shared_units) return own_rows<T, DH, CT_WAVES>(a, px_smem, blockIdx.x - a.shared_units, limit, lane);
     const PrefixTile p = find_prefix<7>(a, blockIdx.x, limit, lane);
     if (p.tile.b < 0) return;
     tile_rows<T, DH, 2, true>(a, px_smem, p.tile, p.k, p.part, 2, [](int, int, KeyRange) {});
@@ -461,7 +440,7 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void prefix_join
 
 // ---------------------------------------------------------------- launches
 struct PrefixPlan {
-    int qb;                                               // blocks of 16 rows of a prefix tile
+    int qb, waves;                                        // blocks of 16 rows of a prefix tile; waves of a streaming workgroup
     PrefixKernelArgs::Cut shared, own;
     int own_tiles;
     int64_t slots, shared_units, own_units;
@@ -479,12 +458,20 @@ static PrefixPlan prefix_plan(const PrefixAttnArgs& a)
 {
     PrefixPlan p{};
     const int64_t G = a.H / a.Hkv, rows = (int64_t)a.max_group * G;
-    p.qb = a.n_groups == 0 || rows <= 16 ? 1 : rows <= 32 || a.dtype == DT_F32 ? 2 : rows <= 64 ? 4 : 8;
+    // Tiles of 128 rows beyond 32 (us, streaming in blocks of 64 and of 32 rows, tiles: 12 groups of 1 to 16 sequences, 32 heads over 8 x 128, 400 to 3000
+    // shared positions 41, 48, 43; 96 rows of 32 heads each over 30000 230, 278, 189; 32 rows 121, 110, 107; 80 rows of 8 heads 41, 55, 38).
+    p.qb = a.n_groups == 0 || rows <= 16 ? 1 : rows <= 32 || a.dtype == DT_F32 ? 2 : 8;
     p.slots = (int64_t)a.tokens * G / (16 * p.qb) + a.n_groups + 1;
     const int64_t most = (int64_t)a.tokens * G / (16 * p.qb) + a.n_groups, each = a.n_groups * ceil_div(rows, 16 * p.qb), tiles = (each < most ? each : most) * a.Hkv;
-    const int64_t own = a.n_seqs * a.Hkv, own_rows = ceil_div(a.max_new * G, 16);
-    const int64_t wgs = a.dtype == DT_F32 && a.dh == 128 ? 256 : 512;
-    int64_t target = ceil_div(tiles * a.max_prefix + own * own_rows * a.max_own, wgs);
+    const int64_t own = (int64_t)a.n_seqs * a.Hkv, own_rows = ceil_div(a.max_new * G, 16);
+    // Keys for a workgroup so that the chip, two of 4 waves a CU (float x 128: one), is filled once; parts of less than 128 gain nothing.
+    const int64_t keys = tiles * a.max_prefix + own * own_rows * a.max_own, wgs = a.dtype == DT_F32 && a.dh == 128 ? 256 : 512;
+    int64_t target = ceil_div(keys, wgs);
+    // Workgroups of 2 waves, five a CU, where one round of 4 waves would have to hold parts of very different lengths (us of 4 / 2: 8 sequences of 40 heads, 1500 shared
+    // positions and 40 to 300 own ones 21.8 / 17.3; 20 groups of 2, 4 heads 24.3 / 18.8; 8 of 16 heads, 6000 shared 17.3 / 15.7); not for shorter ones,
+    // where both waves start late, or longer ones, whose rounds even out (6 groups of 8 of 40 heads 75 / 87).
+    p.waves = p.qb == 1 && target >= 128 && target < 384 && wgs == 512 ? 2 : 4;
+    if (p.waves == 2) target = ceil_div(keys, 768);
     target = target < 128 ? 128 : target;
     p.own = cut_keys(a.max_own, target, 16);
     p.shared = a.n_groups ? cut_keys(a.max_prefix, target, PX_PARTS - p.own.parts) : PrefixKernelArgs::Cut{0, 0x7fffffff};
@@ -499,30 +486,31 @@ size_t prefix_attn_workspace(const PrefixAttnArgs& a)
     return (size_t)(p.shared.parts + p.own.parts) * a.tokens * a.H * (a.dh + 2) * sizeof(float);
 }
 
-template <typename K> static hipError_t launch_kernel(K kernel, LdsLimit (&limit)[MAX_DEVICES], int lds, const PrefixKernelArgs& k, int64_t wgs, hipStream_t s)
+template <typename K> static hipError_t launch_kernel(K kernel, LdsLimit (&limit)[MAX_DEVICES], int waves, int lds, const PrefixKernelArgs& k, int64_t wgs, hipStream_t s)
 {
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) dev = 0;
     hipError_t e = limit[dev].raise((const void*)kernel, lds);
     if (e != hipSuccess) return e;
-    kernel<<<(unsigned)wgs, PX_THREADS, lds, s>>>(k);
+    kernel<<<(unsigned)wgs, waves * 64, lds, s>>>(k);
     return hipGetLastError();
 }
-template <typename T, int DH, int QB> static hipError_t launch_stream(const PrefixKernelArgs& k, int64_t wgs, hipStream_t s)
+template <typename T, int DH, int QB, int WAVES> static hipError_t launch_stream(const PrefixKernelArgs& k, int64_t wgs, hipStream_t s)
 {
     static LdsLimit limit[MAX_DEVICES];
-    return launch_kernel(prefix_stream_kernel<T, DH, QB>, limit, PrefixStream<T, DH>::LDS + (QB == 4 ? PrefixStream<T, DH>::QUERIES : 0), k, wgs, s);
+    typedef PrefixStream<T, DH, WAVES> S;
+    return launch_kernel(prefix_stream_kernel<T, DH, QB, WAVES>, limit, WAVES, S::LDS, k, wgs, s);
 }
 template <typename T, int DH> static hipError_t launch_tile(const PrefixKernelArgs& k, int64_t wgs, hipStream_t s)
 {
     static LdsLimit limit[MAX_DEVICES];
-    return launch_kernel(prefix_tile_kernel<T, DH>, limit, std::max(PrefixStream<T, DH>::LDS, ct_lds<T, DH, 2>()), k, wgs, s);
+    return launch_kernel(prefix_tile_kernel<T, DH>, limit, CT_WAVES, std::max(PrefixStream<T, DH, CT_WAVES>::LDS, ct_lds<T, DH, 2>()), k, wgs, s);
 }
 template <typename T, int DH> static hipError_t launch_prefix(const PrefixAttnArgs& a, hipStream_t s)
 {
     const PrefixPlan p = prefix_plan(a);
     const int64_t wgs = p.shared_units + p.own_units, rows = (int64_t)a.tokens * a.H;
-    if (p.slots > 0x7fffffff || wgs * PX_THREADS > MAX_LAUNCH_THREADS || rows / 4 + a.tokens > MAX_LAUNCH_THREADS / PX_THREADS) return hipErrorInvalidValue;
+    if (p.slots > 0x7fffffff || wgs * 256 > MAX_LAUNCH_THREADS || rows / 4 + a.tokens > MAX_LAUNCH_THREADS / 256) return hipErrorInvalidValue;
     PrefixKernelArgs k{};
     k.cu = a.cu; k.len = a.len; k.cu_groups = a.cu_groups; k.prefix = a.prefix;
     k.n_seqs = a.n_seqs; k.tokens = a.tokens; k.n_groups = a.n_groups;
@@ -537,9 +525,9 @@ template <typename T, int DH> static hipError_t launch_prefix(const PrefixAttnAr
     k.slots = (int)p.slots; k.own_tiles = p.own_tiles;
     k.shared_units = (unsigned)p.shared_units; k.own_units = (unsigned)p.own_units;
     hipError_t e;
-    if (p.qb == 1) e = launch_stream<T, DH, 1>(k, wgs, s);
-    else if (p.qb == 2) e = launch_stream<T, DH, 2>(k, wgs, s);
-    else if constexpr (sizeof(T) == 2) e = p.qb == 4 ? launch_stream<T, DH, 4>(k, wgs, s) : launch_tile<T, DH>(k, wgs, s);
+    if (p.qb == 1) e = p.waves == 2 ? launch_stream<T, DH, 1, 2>(k, wgs, s) : launch_stream<T, DH, 1, 4>(k, wgs, s);
+    else if (p.qb == 2) e = launch_stream<T, DH, 2, 4>(k, wgs, s);
+    else if constexpr (sizeof(T) == 2) e = launch_tile<T, DH>(k, wgs, s);
     else e = hipErrorInvalidValue;
     if (e != hipSuccess) return e;
     prefix_join_kernel<T, DH><<<(unsigned)(a.tokens * ceil_div(a.H, 4)), 256, 0, s>>>(k);
