@@ -502,7 +502,7 @@ uint64_t exe_op_chunk_attention_paged_workspace(int32_t dtype, int32_t n_seqs, i
  * values, and 8 in that with a prefix that more than 32 query rows share per key/value head (new tokens of the group times H / Hkv; bf16: max_group chooses).
  * Made for single and drafted tokens: chunks of many tokens run in tiles of 16 rows a sequence here.
  * Everything else as exe_op_chunk_attention_paged has it: rows without keys are 0, with a missing block NaN, spoilt ones computed once more; workspace:
- * exe_op_prefix_attention_paged_workspace bytes, always some (0 for bad arguments). */
+ * exe_op_prefix_attention_paged_workspace bytes (0 for bad arguments), NULL if that is 0. */
 int exe_op_prefix_attention_paged(void* hip_stream, int32_t dtype, int32_t n_seqs, const int32_t* cu_seqlens, int32_t T, int32_t max_new,
                                   int32_t n_groups, const int32_t* cu_groups, const int32_t* prefix, int32_t max_group, int32_t max_prefix,
                                   const void* q, int64_t q_stride, const void* kv_blocks, int32_t n_blocks, const int32_t* block_table,

@@ -118,12 +118,22 @@ template <typename T, int DH, int WAVES> struct PrefixStream {
     static_assert(MERGE + WAVES * 16 * 8 <= LDS, "results, maxima and sums");
 };
 
+// Row (t, h) of sequence b at position p, by one wave (see chunk_row).
+template <typename T, int DH> __device__ __forceinline__ void prefix_row(const PrefixKernelArgs& a, const PrefixGroup& gr, int b, int p, int t, int h, int lane)
+{
+    const int64_t head = (int64_t)DH << a.table.shift;
+    chunk_row<T, DH>((const T*)a.q + (int64_t)t * a.q_stride + h * DH, (const T*)a.kv_blocks + h / a.G * head, 2 * a.Hkv * head, a.Hkv * head, a.table.shift,
+                     [&](int j) { return a.table.block(j < gr.prefix ? gr.b0 : b, j); }, keys_of(p, 0, table_limit(a.table)), a.scale * LOG2E, lane,
+                     (T*)a.out + (int64_t)t * a.out_stride + h * DH);
+}
+
 // Query rows r0 .. r1 - 1 of a run of packed tokens from t0 on (row r: token t0 + r / G, head kvh * G + r % G) against keys k of table row b; row
 // r sees keys lo .. hi(r) - 1 of them.  Every wave takes steps of 16 keys of its own through a ring of stages in LDS, as chunk_stream_kernel does,
 // with QB blocks of 16 rows: S^T = K . Q^T, O^T += V^T . P^T.  The result goes to part `part`.
-template <typename T, int DH, int QB, int WAVES, bool NT, typename F>
-__device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned char* smem, int b, int kvh, int t0, int r0, int r1,
-                                            KeyRange k, int lo, F hi, int part)
+// WHOLE: behind the keys 0 .. lo - 1 of table row b0, which all rows see, and to the results themselves; again: computes a row once more.
+template <typename T, int DH, int QB, int WAVES, bool NT, bool WHOLE, typename F, typename R>
+__device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned char* smem, int b0, int b, int kvh, int t0, int r0, int r1,
+                                            KeyRange k, int lo, F hi, int part, R again)
 {
     typedef PrefixStream<T, DH, WAVES> S;
     constexpr int RB = S::RB, DS = RB / 64, DT = DH / 16;
@@ -143,16 +153,20 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
         load_query<T, DS>((const T*)a.q + (int64_t)(t >= 0 && t < a.tokens ? t : 0) * a.q_stride + (kvh * G + row % G) * DH, g, a.scale, qf[qb]);
     }
     const int least = hi(r0);                                            // the first row sees the fewest
-    const int steps = k.last > k.first ? (k.last - k.first + PX_STEP - 1) / PX_STEP : 0, own = steps > wave ? (steps - wave + WAVES - 1) / WAVES : 0;
+    const int shared = WHOLE ? (lo + PX_STEP - 1) / PX_STEP : 0;             // steps in front
+    const int steps = shared + (k.last > k.first ? (k.last - k.first + PX_STEP - 1) / PX_STEP : 0), own = steps > wave ? (steps - wave + WAVES - 1) / WAVES : 0;
     typedef RowLoader<T, DH, NT> Loader;
-    const Loader from(a.table, a.kv_blocks, b, kvh, a.Hkv, limit, k.last, lane);
-    auto first_of = [&](int i) { return k.first + (wave + i * WAVES) * PX_STEP; };
+    const Loader from(a.table, a.kv_blocks, b, kvh, a.Hkv, limit, k.last, lane), front(a.table, a.kv_blocks, WHOLE ? b0 : b, kvh, a.Hkv, limit, WHOLE ? lo : k.last, lane);
+    auto in_front = [&](int i) { return WHOLE && wave + i * WAVES < shared; };
+    auto first_of = [&](int i) { return in_front(i) ? (wave + i * WAVES) * PX_STEP : k.first + (wave + i * WAVES - shared) * PX_STEP; };
+    auto lookup = [&](int i) { return in_front(i) ? front.lookup(first_of(i)) : from.lookup(first_of(i)); };
     typename Loader::Entries en{-1, -1};
     auto issue = [&](int i) {
         const unsigned dst = lds + i % S::STAGES * S::STAGE;
-        const typename Loader::Rows r = from.rows(first_of(i), en);
-        from.keys(first_of(i), r, dst);
-        from.values(first_of(i), r, dst + S::TILE);
+        const Loader& f = in_front(i) ? front : from;
+        const typename Loader::Rows r = f.rows(first_of(i), en);
+        f.keys(first_of(i), r, dst);
+        f.values(first_of(i), r, dst + S::TILE);
     };
 
     float m[QB], l[QB];                                                  // l: this lane's share of the sum
@@ -166,15 +180,15 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
     }
     const int ahead = S::STAGES - 1;
     for (int i = 0; i < ahead && i < own; ++i) {
-        en = from.lookup(first_of(i));
+        en = lookup(i);
         issue(i);
     }
-    if (ahead < own) en = from.lookup(first_of(ahead));
+    if (ahead < own) en = lookup(ahead);
     for (int i = 0; i < own; ++i) {
         if (i + ahead < own) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // step i - 1 has left its stage
             issue(i + ahead);
-            if (i + ahead + 1 < own) en = from.lookup(first_of(i + ahead + 1));
+            if (i + ahead + 1 < own) en = lookup(i + ahead + 1);
             wait_loads<2 * S::LOADS * (S::STAGES - 1)>();
         } else {
             wait_loads<0>();
@@ -200,14 +214,15 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
         const int j = first_of(i);
         float mx[QB];
         bool grew = false;
-        if (j + PX_STEP > least || j < lo) {
+        const bool whole = in_front(i);
+        if (whole ? j + PX_STEP > lo : j + PX_STEP > least || j < lo) {
             int key0 = j + 4 * g;
             asm volatile("" : "+v"(key0));                               // keeps the mask arithmetic inside this branch
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
                 s[qb][0] += s[qb][1];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) s[qb][0][r] = key0 + r >= lo && key0 + r < last[qb] ? s[qb][0][r] : -INFINITY;
+                for (int r = 0; r < 4; ++r) s[qb][0][r] = (whole || key0 + r >= lo) && key0 + r < (whole ? lo : last[qb]) ? s[qb][0][r] : -INFINITY;
             }
         } else {
 #pragma unroll
@@ -288,7 +303,7 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
         __syncthreads();
         // 16 threads a row, features 4 * c .. +3 of every 64
 #pragma unroll
-        for (int r = tid >> 4; r < 16; r += WAVES * 4) {
+        for (int r = tid >> 4; r < 16; r += WAVES * 4) {                 // beyond 4 waves: nothing to do
             const int c = tid & 15, row = r0 + qb * 16 + r, t = t0 + row / G;
             float M = -INFINITY, L = 0.f, w[WAVES];
 #pragma unroll
@@ -299,7 +314,37 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
                 w[i] = fast_exp2(s_ml[i][r][0] - ref);
                 L += s_ml[i][r][1] * w[i];
             }
-            if (row >= r1 || t < 0 || t >= a.tokens) continue;
+            const bool write = row < r1 && t >= 0 && t < a.tokens;
+            if constexpr (WHOLE) {
+                f32x4 v[DH / 64];
+                float most = 0.f;
+                const bool any = hi(row < r1 ? row : r1 - 1) > 0;
+#pragma unroll
+                for (int f = 0; f < DH / 64; ++f) {
+                    v[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < WAVES; ++i) v[f] += *(const f32x4*)(s_o + (i * 16 + r) * (DH + 4) + f * 64 + 4 * c) * w[i];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[f][e] = any ? v[f][e] / L : 0.f;
+                        most = magnitude(most, v[f][e]);
+                    }
+                }
+                const unsigned long long bad = __builtin_amdgcn_ballot_w64(write && spoilt(most, L));
+                if (write && !(bad >> (lane & 48) & 0xffff)) {
+#pragma unroll
+                    for (int f = 0; f < DH / 64; ++f) {
+                        typename Vec4<T>::type y;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] = from_f32<T>(v[f][e]);
+                        *(typename Vec4<T>::type*)((T*)a.out + (int64_t)t * a.out_stride + (kvh * G + row % G) * DH + f * 64 + 4 * c) = y;
+                    }
+                }
+                for (int i = 0; i < 4; ++i)                              // the four rows of this wave
+                    if (bad >> (16 * i) & 0xffff) again(r0 + qb * 16 + (r & ~3) + i);
+                continue;
+            }
+            if (!write) continue;
             const int64_t at = ((int64_t)part * a.tokens + t) * a.H + kvh * G + row % G;
 #pragma unroll
             for (int f = 0; f < DH / 64; ++f) {
@@ -363,7 +408,7 @@ template <typename T, int DH, int WAVES> __device__ __forceinline__ void own_row
         const KeyRange all{lo & -PX_STEP, hi(r1 - 1)};
         const int parts = parts_of(all, a.own);
         if (part >= parts) no_part(a, kvh, t0, r0, r1, a.shared.parts + part);
-        else stream_rows<T, DH, 1, WAVES, true>(a, smem, b, kvh, t0, r0, r1, part_of(all, a.own, part, parts), lo, hi, a.shared.parts + part);
+        else stream_rows<T, DH, 1, WAVES, true, false>(a, smem, b, b, kvh, t0, r0, r1, part_of(all, a.own, part, parts), lo, hi, a.shared.parts + part, [](int) {});
     }
 }
 
@@ -376,7 +421,23 @@ template <typename T, int DH, int QB, int WAVES> __global__ __launch_bounds__(WA
     const PrefixTile p = find_prefix<QB == 1 ? 4 : 5>(a, blockIdx.x, limit, lane);
     if (p.tile.b < 0) return;
     const int end = p.k.last;
-    stream_rows<T, DH, QB, WAVES, false>(a, px_smem, p.tile.b, p.tile.kvh, p.tile.t0, p.tile.r0, p.r1, p.k, 0, [&](int) { return end; }, p.part);
+    stream_rows<T, DH, QB, WAVES, false, false>(a, px_smem, p.tile.b, p.tile.b, p.tile.kvh, p.tile.t0, p.tile.r0, p.r1, p.k, 0, [&](int) { return end; }, p.part, [](int) {});
+}
+// Few and short sequences, each with its prefix by itself: the prefix, that comes from L2 for all but the first, costs less than a second launch.
+template <typename T, int DH, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void prefix_whole_kernel(PrefixKernelArgs a)
+{
+    extern __shared__ __align__(16) unsigned char px_smem[];
+    const int lane = threadIdx.x & 63, limit = table_limit(a.table), G = a.G, tile = blockIdx.x % a.own_tiles, head = blockIdx.x / a.own_tiles, kvh = head % a.Hkv, b = head / a.Hkv;
+    const int t0 = a.cu[b], end = a.cu[b + 1], p_end = a.len[b], n = end - t0 < a.tokens ? end - t0 : a.tokens, p0 = p_end - n;
+    const PrefixGroup gr = find_group<false>(a, b, 0, lane);
+    if (n <= 0) return;
+    const int lo = gr.prefix < limit ? gr.prefix : limit;
+    auto hi = [&](int row) { return keys_of(p0 + row / G, 0, limit).last; };
+    auto again = [&](int row) { prefix_row<T, DH>(a, gr, b, p0 + row / G, t0 + row / G, kvh * G + row % G, lane); };
+    for (int r0 = tile * 16; r0 < n * G; r0 += a.own_tiles * 16) {
+        const int r1 = r0 + 16 < n * G ? r0 + 16 : n * G;
+        stream_rows<T, DH, 1, WAVES, false, true>(a, px_smem, gr.g < 0 || !lo ? b : gr.b0, b, kvh, t0, r0, r1, KeyRange{lo & -PX_STEP, hi(r1 - 1)}, lo, hi, 0, again);
+    }
 }
 // More rows, in tiles of 128, beside own positions.  Bound by MFMAs and softmax, as chunk_tile_kernel is.
 template <typename T, int DH> __global__ __launch_bounds__(CT_WAVES * 64, 2) void prefix_tile_kernel(PrefixKernelArgs a)
@@ -426,10 +487,7 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void prefix_join
         const ChunkSeq sq = seq_of_token(a.cu, a.n_seqs, t, lane);
         if (sq.b < 0) return;
         const PrefixGroup gr = find_group<false>(a, sq.b, 0, lane);
-        const int limit = table_limit(a.table);
-        const int64_t head = (int64_t)DH << a.table.shift;
-        chunk_row<T, DH>((const T*)a.q + (int64_t)t * a.q_stride + h * DH, (const T*)a.kv_blocks + h / a.G * head, 2 * a.Hkv * head, a.Hkv * head, a.table.shift,
-                         [&](int j) { return a.table.block(j < gr.prefix ? gr.b0 : sq.b, j); }, keys_of(a.len[sq.b] - sq.n + (t - sq.t0), 0, limit), a.scale * LOG2E, lane, out);
+        prefix_row<T, DH>(a, gr, sq.b, a.len[sq.b] - sq.n + (t - sq.t0), t, h, lane);
     } else if (sub == 0) {
         typename Vec4<T>::type y;
 #pragma unroll
@@ -440,6 +498,7 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void prefix_join
 
 // ---------------------------------------------------------------- launches
 struct PrefixPlan {
+    bool whole;
     int qb, waves;                                        // blocks of 16 rows of a prefix tile; waves of a streaming workgroup
     PrefixKernelArgs::Cut shared, own;
     int own_tiles;
@@ -464,6 +523,16 @@ static PrefixPlan prefix_plan(const PrefixAttnArgs& a)
     p.slots = (int64_t)a.tokens * G / (16 * p.qb) + a.n_groups + 1;
     const int64_t most = (int64_t)a.tokens * G / (16 * p.qb) + a.n_groups, each = a.n_groups * ceil_div(rows, 16 * p.qb), tiles = (each < most ? each : most) * a.Hkv;
     const int64_t own = (int64_t)a.n_seqs * a.Hkv, own_rows = ceil_div(a.max_new * G, 16);
+    // us of both launches / one: 2 sequences of 12 heads x 64 over 200 + 60 keys 9.0 / 6.9, 450 + 60 9.1 / 8.7, 800 + 60 9.4 / 10.6; 4 of 40 heads x 128, 300 + 60
+    // 10.7 / 9.0; 4 of 32 over 8, 400 + 60 10.0 / 10.0; more than one workgroup a CU: 12 of 40, 300 + 60 15.0 / 16.9; float, 400 + 60 10.4 / 12.0; and a launch's
+    // 4 us of the host.
+    p.whole = own * own_rows <= 256 && (int64_t)a.max_prefix + a.max_own <= (a.dtype == DT_F32 ? 256 : 512);
+    if (p.whole) {
+        p.waves = a.dtype == DT_F32 && a.dh == 128 ? 4 : 8;
+        p.own_tiles = (int)own_rows;
+        p.own_units = own * own_rows;
+        return p;
+    }
     // Keys for a workgroup so that the chip, two of 4 waves a CU (float x 128: one), is filled once; parts of less than 128 gain nothing.
     const int64_t keys = tiles * a.max_prefix + own * own_rows * a.max_own, wgs = a.dtype == DT_F32 && a.dh == 128 ? 256 : 512;
     int64_t target = ceil_div(keys, wgs);
@@ -483,6 +552,7 @@ static PrefixPlan prefix_plan(const PrefixAttnArgs& a)
 size_t prefix_attn_workspace(const PrefixAttnArgs& a)
 {
     const PrefixPlan p = prefix_plan(a);
+    if (p.whole) return 0;
     return (size_t)(p.shared.parts + p.own.parts) * a.tokens * a.H * (a.dh + 2) * sizeof(float);
 }
 
@@ -501,6 +571,11 @@ template <typename T, int DH, int QB, int WAVES> static hipError_t launch_stream
     typedef PrefixStream<T, DH, WAVES> S;
     return launch_kernel(prefix_stream_kernel<T, DH, QB, WAVES>, limit, WAVES, S::LDS, k, wgs, s);
 }
+template <typename T, int DH, int WAVES> static hipError_t launch_whole(const PrefixKernelArgs& k, int64_t wgs, hipStream_t s)
+{
+    static LdsLimit limit[MAX_DEVICES];
+    return launch_kernel(prefix_whole_kernel<T, DH, WAVES>, limit, WAVES, PrefixStream<T, DH, WAVES>::LDS, k, wgs, s);
+}
 template <typename T, int DH> static hipError_t launch_tile(const PrefixKernelArgs& k, int64_t wgs, hipStream_t s)
 {
     static LdsLimit limit[MAX_DEVICES];
@@ -510,7 +585,7 @@ template <typename T, int DH> static hipError_t launch_prefix(const PrefixAttnAr
 {
     const PrefixPlan p = prefix_plan(a);
     const int64_t wgs = p.shared_units + p.own_units, rows = (int64_t)a.tokens * a.H;
-    if (p.slots > 0x7fffffff || wgs * 256 > MAX_LAUNCH_THREADS || rows / 4 + a.tokens > MAX_LAUNCH_THREADS / 256) return hipErrorInvalidValue;
+    if (p.slots > 0x7fffffff || wgs * 512 > MAX_LAUNCH_THREADS || rows / 4 + a.tokens > MAX_LAUNCH_THREADS / 256) return hipErrorInvalidValue;
     PrefixKernelArgs k{};
     k.cu = a.cu; k.len = a.len; k.cu_groups = a.cu_groups; k.prefix = a.prefix;
     k.n_seqs = a.n_seqs; k.tokens = a.tokens; k.n_groups = a.n_groups;
@@ -525,6 +600,10 @@ template <typename T, int DH> static hipError_t launch_prefix(const PrefixAttnAr
     k.slots = (int)p.slots; k.own_tiles = p.own_tiles;
     k.shared_units = (unsigned)p.shared_units; k.own_units = (unsigned)p.own_units;
     hipError_t e;
+    if (p.whole) {
+        if constexpr (sizeof(T) == 4 && DH == 128) return launch_whole<T, DH, 4>(k, wgs, s);
+        else return launch_whole<T, DH, 8>(k, wgs, s);
+    }
     if (p.qb == 1) e = p.waves == 2 ? launch_stream<T, DH, 1, 2>(k, wgs, s) : launch_stream<T, DH, 1, 4>(k, wgs, s);
     else if (p.qb == 2) e = launch_stream<T, DH, 2, 4>(k, wgs, s);
     else if constexpr (sizeof(T) == 2) e = launch_tile<T, DH>(k, wgs, s);

@@ -10,6 +10,15 @@ from chunk_util import DEV, Batch, check
 pytestmark = pytest.mark.gpu
 
 
+BOUND = 1          # of own positions, at least: sizes the launch, so a larger one brings small cases to the kernels of larger ones
+
+
+@pytest.fixture(autouse=True, params=[1, 1100], ids=["own", "parts"])
+def bound(request, monkeypatch):
+    """Calls of few and short sequences take one kernel: with a larger bound of the own positions, those of longer ones and the join."""
+    monkeypatch.setitem(globals(), "BOUND", request.param)
+
+
 class Groups(Batch):
     """groups = [(prefix, [(new tokens, own positions with them), ..]), ..]; `loose`: sequences behind the last group, (new, positions)."""
 
@@ -42,7 +51,7 @@ class Groups(Batch):
     def sizes(self):
         new = [n for n, _ in self.seqs]
         return dict(max_new=max(new + [1]), max_group=max([sum(n for n, _ in s) for _, s in self.groups] + [1]), max_prefix=max(self.prefix + [0]),
-                    max_own=max([o for _, s in self.groups for _, o in s] + [L for _, L in self.seqs[self.cu_groups[-1]:]] + [1]))
+                    max_own=max([o for _, s in self.groups for _, o in s] + [L for _, L in self.seqs[self.cu_groups[-1]:]] + [BOUND]))
 
     def attend(self, out=None, stream=None, workspace=None, scale=None, q=None, q_stride=None, out_stride=None, **change):
         z = {**self.sizes(), **change}
@@ -52,7 +61,7 @@ class Groups(Batch):
         if workspace is None:
             need = exe.exe_op_prefix_attention_paged_workspace(self.code, len(self.seqs), self.rows, z["max_new"], len(self.groups), z["max_group"], z["max_prefix"], z["max_own"],
                                                                self.H, self.Hkv, self.dh)
-            workspace = torch.full((need // 4,), float("nan"), dtype=torch.float32, device=DEV)
+            workspace = torch.full((need // 4,), float("nan"), dtype=torch.float32, device=DEV) if need else None
         exe.exe_op_prefix_attention_paged(self.code, len(self.seqs), self.d_cu, self.rows, z["max_new"], len(self.groups), self.d_groups, self.d_prefix, z["max_group"],
                                           z["max_prefix"], self.d_q if q is None else q, q_stride or w, self.d_pool, self.n_blocks, self.d_table, self.max_blocks, self.block,
                                           self.d_len, z["max_own"], self.H, self.Hkv, self.dh, self.scale if scale is None else scale, out, out_stride or w, workspace,
@@ -107,6 +116,14 @@ def test_many_sequences_and_groups(n):
     check(b.attend(), *b.want())
     b = Groups([(20, [(1, 1)])] * n, 4, 1, 64, 16, "f32", seed=n).fill().device()
     check(b.attend(), *b.want())
+
+
+def test_workgroups_of_two_waves():
+    """40 heads, 8 sequences: sizes that one round of the chip holds in unequal parts."""
+    b = Groups([(1500, [(1, 20 + 40 * i) for i in range(8)])], 40, 40, 128, 64, "bf16").fill().device()
+    check(b.attend(), *b.want())
+    b = Groups([(300 + 20 * g, [(1, 30), (1, 250 - 5 * g)]) for g in range(20)], 32, 4, 128, 16, "bf16").fill().device()
+    check(b.attend(max_prefix=1500, max_own=288), *b.want())
 
 
 def test_no_groups_and_no_prefix():
@@ -259,9 +276,10 @@ def test_two_streams_and_a_replayed_graph():
     b.d_table.copy_(torch.arange(b.d_table.numel(), device=DEV).view(b.d_table.shape) % b.n_blocks)
     for s in range(1, 9):
         b.d_table[s, :18] = b.d_table[0, :18]
-    need = exe.exe_op_prefix_attention_paged_workspace(b.code, 13, b.rows, 1, 2, 9, 400, 100, 8, 2, 64)
-    ws, out = torch.empty(need, dtype=torch.uint8, device=DEV), torch.empty((b.rows, 512), dtype=torch.bfloat16, device=DEV)
-    sizes = dict(max_new=1, max_group=9, max_prefix=400, max_own=100)
+    need = exe.exe_op_prefix_attention_paged_workspace(b.code, 13, b.rows, 1, 2, 9, 400, max(100, BOUND), 8, 2, 64)
+    assert (need == 0) == (BOUND == 1)
+    ws, out = torch.empty(max(need, 16), dtype=torch.uint8, device=DEV), torch.empty((b.rows, 512), dtype=torch.bfloat16, device=DEV)
+    sizes = dict(max_new=1, max_group=9, max_prefix=400, max_own=max(100, BOUND))
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         b.attend(out=out, workspace=ws, **sizes)

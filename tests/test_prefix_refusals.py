@@ -4,7 +4,7 @@ import pytest
 import paper_2404_07947_amd as exe
 
 P = 4096            # an address that no call may follow
-GOOD = dict(dtype=1, n_seqs=2, cu=P, T=4, max_new=2, n_groups=1, cu_groups=P, prefix=P, max_group=4, max_prefix=30, q=P, q_stride=256, kv_blocks=P, n_blocks=4, table=P,
+GOOD = dict(dtype=1, n_seqs=2, cu=P, T=4, max_new=2, n_groups=1, cu_groups=P, prefix=P, max_group=4, max_prefix=900, q=P, q_stride=256, kv_blocks=P, n_blocks=4, table=P,
             max_blocks=2, block=16, length=P, max_own=9, H=4, Hkv=2, dh=64, scale=0.1, out=2 * P, out_stride=256)
 
 
@@ -25,7 +25,7 @@ def test_refusals(change, code):
 
 
 def test_workspaces():
-    good = (1, 2, 4, 2, 1, 4, 30, 9, 4, 2, 64)
+    good = (1, 2, 4, 2, 1, 4, 900, 9, 4, 2, 64)
     need = exe.exe_op_prefix_attention_paged_workspace(*good)
     assert need > 0
     refused(-1, ws_bytes=need - 1)
@@ -33,7 +33,8 @@ def test_workspaces():
     refused(-1, ws=None, ws_bytes=None)
     for i, v in ((0, 2), (1, 0), (2, 0), (3, 0), (4, -1), (5, 0), (6, -1), (7, 0), (8, 3), (8, 0), (9, 0), (10, 96), (2, 1 << 30)):
         assert exe.exe_op_prefix_attention_paged_workspace(*good[:i], v, *good[i + 1:]) == 0
-    assert exe.exe_op_prefix_attention_paged_workspace(1, 2, 4, 2, 0, 0, 0, 9, 4, 2, 64) > 0
+    assert exe.exe_op_prefix_attention_paged_workspace(1, 2, 4, 2, 0, 0, 0, 900, 4, 2, 64) > 0
+    assert exe.exe_op_prefix_attention_paged_workspace(1, 2, 4, 2, 1, 4, 30, 9, 4, 2, 64) == 0          # few and short: one kernel
 
 
 def test_nothing_to_do_is_no_error():
