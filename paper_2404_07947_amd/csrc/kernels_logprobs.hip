@@ -11,8 +11,7 @@
 namespace exe {
 
 typedef unsigned long long u64;
-constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / WAVE, LP_CAP = LP_THREADS, LP_JOIN = 64;
-static_assert(LP_WAVES == 4 && LP_THREADS == 256, "four best ones a lane");
+constexpr int LP_JOIN_THREADS = 256, LP_CAP = 256, LP_JOIN = 64;
 constexpr float LN2 = 0.69314718055994530942f;
 
 struct LogprobKernelArgs {
@@ -61,13 +60,13 @@ __device__ __forceinline__ void sums_to(Sums& p, float M, float c)
 }
 
 // The results of a row, by a workgroup: sums, and the k best keys in LDS (0: there are fewer).
-template <typename T> __device__ __forceinline__ void logprob_finish(const LogprobKernelArgs& a, int64_t row, Sums t, const u64* top)
+template <typename T, int THREADS> __device__ __forceinline__ void logprob_finish(const LogprobKernelArgs& a, int64_t row, Sums t, const u64* top)
 {
     const float L = log2f(t.S) * LN2;
     // in 64 bits: the logits may lie further apart than the largest float
     auto logprob = [&](float x) { return (float)(((double)x - (double)t.M) * (double)a.scale - (double)L); };
     const T* x = (const T*)a.logits + row * a.row_stride;
-    for (int i = threadIdx.x; i < a.n_tokens; i += LP_THREADS) {
+    for (int i = threadIdx.x; i < a.n_tokens; i += THREADS) {
         const unsigned tok = (unsigned)a.tokens[row * a.n_tokens + i];
         a.logprobs[row * a.n_tokens + i] = tok < a.n ? logprob(to_f32(x[tok])) : NAN;
     }
@@ -79,8 +78,9 @@ template <typename T> __device__ __forceinline__ void logprob_finish(const Logpr
     }
 }
 
-template <typename T, int C> struct LogitPart {
-    static constexpr int V = 16 / (int)sizeof(T), N = C * V, SPAN = LP_THREADS * N;
+template <typename T, int THREADS, int C> struct LogitPart {
+    static constexpr bool SOME = THREADS > 256;              // else all chunks are in use
+    static constexpr int V = 16 / (int)sizeof(T), N = C * V, SPAN = THREADS * N;
     uint4 raw[C];
     __device__ __forceinline__ float at(int i) const       // i: a constant after unrolling
     {
@@ -90,7 +90,7 @@ template <typename T, int C> struct LogitPart {
         return sizeof(T) == 4 ? __uint_as_float(d) : i & 1 ? bf16hi(d) : bf16lo(d);
     }
     // place of element i among the part's
-    static __device__ __forceinline__ unsigned place(int i) { return (i / V * LP_THREADS + threadIdx.x) * V + i % V; }
+    static __device__ __forceinline__ unsigned place(int i) { return (i / V * THREADS + threadIdx.x) * V + i % V; }
     // New values to the compiler, which would keep what it made of all of them in registers from one use to the next.
     __device__ __forceinline__ void renew()
     {
@@ -99,20 +99,23 @@ template <typename T, int C> struct LogitPart {
     }
     // Logits first .. end - 1 of the row, the first on 16 bytes: up to V - 1 before the row's first one.  What is not of them is -inf.  All loads go
     // out before anything waits: those of chunks that are not there, or only in part, from the nearest whole one.
-    __device__ __forceinline__ void load(const T* x, unsigned first, unsigned end, unsigned n)
+    // Of the C chunks the first `chunks` are in use.
+    __device__ __forceinline__ void load(const T* x, unsigned first, unsigned end, unsigned n, int chunks)
     {
         const int low = (int)(-(unsigned)((uintptr_t)x & 15) / sizeof(T) % V), high = (int)(n - low) < V ? -1 : low + ((int)n - low - V) / V * V;
         if (high >= 0) {
 #pragma unroll
             for (int c = 0; c < C; ++c) {
+                if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
                 const int i = (int)(first + place(c * V));
                 raw[c] = load_chunk<true>(x + (i < low ? low : i < high ? i : high));
             }
         }
         // the last thread's last chunk is there, and the first thread's first: all are
-        if (first < end && end - first >= SPAN) return;
+        if (first < end && end - first >= (unsigned)chunks * THREADS * V) return;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
+            if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
             const unsigned i = first + place(c * V);
             if (i < end && end - i >= V) continue;
             if (i - first >= end - first) {                    // nothing of it
@@ -154,44 +157,51 @@ __device__ __forceinline__ void sort_keys(const u64* keys, int count, u64* top, 
     if (tid >= count && tid < k) top[tid] = 0;
 }
 
-template <typename T, int C> __global__ __launch_bounds__(LP_THREADS) void logprob_part_kernel(LogprobKernelArgs a)
+template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, THREADS == 1024 && sizeof(T) == 2 ? 8 : 1) void logprob_part_kernel(LogprobKernelArgs a)
 {
-    typedef LogitPart<T, C> Part;
-    constexpr int N = Part::N;
+    typedef LogitPart<T, THREADS, C> Part;
+    constexpr int N = Part::N, WAVES = THREADS / WAVE, V = Part::V;
+    constexpr bool SOME = Part::SOME;
     __shared__ u64 s_keys[LP_CAP], s_top[WAVE];
-    __shared__ Sums s_sums[LP_WAVES];
-    __shared__ __align__(16) float s_best[LP_THREADS];
+    __shared__ Sums s_sums[WAVES];
+    __shared__ __align__(16) float s_best[THREADS];
     __shared__ int s_count, s_digit, s_counts[256];
-    static_assert(LP_THREADS == 256 && Part::SPAN <= 1 << 16, "a count for each digit; 16 bits of a place");
+    static_assert(THREADS % 256 == 0 && WAVES <= WAVE && Part::SPAN <= 1 << 16, "a count for each digit; a lane for each wave; 16 bits of a place");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row = blockIdx.x / a.parts;
     const unsigned part = blockIdx.x - (unsigned)row * a.parts;
     const T* x = (const T*)a.logits + row * a.row_stride;
     const unsigned first = part * a.span - (unsigned)((uintptr_t)x & 15) / sizeof(T), end = first + a.span < a.n ? first + a.span : a.n;
     Part p;
-    p.load(x, first, end, a.n);
+    const int chunks = (a.span + THREADS * V - 1) / (THREADS * V);
+    p.load(x, first, end, a.n, chunks);
     if (tid == 0) s_count = 0;
 
     float tops[C], best = -INFINITY;                           // of a chunk; of all
     bool none = false;
 #pragma unroll
+    for (int c = 0; c < C; ++c) tops[c] = -INFINITY;
+#pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int i = c * Part::V;
+        if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
+        const int i = c * V;
         tops[c] = max3(p.at(i), p.at(i + 1), p.at(i + 2));
-        if constexpr (Part::V == 8) tops[c] = max3(max3(tops[c], p.at(i + 3), p.at(i + 4)), p.at(i + 5), p.at(i + 6));
-        tops[c] = max3(tops[c], tops[c], p.at(i + Part::V - 1));
+        if constexpr (V == 8) tops[c] = max3(max3(tops[c], p.at(i + 3), p.at(i + 4)), p.at(i + 5), p.at(i + 6));
+        tops[c] = max3(tops[c], tops[c], p.at(i + V - 1));
         none |= tops[c] != tops[c];
     }
     if (none) {                                                // all of a chunk NaN, or signalling ones, which that instruction hands on
 #pragma unroll
         for (int c = 0; c < C; ++c) {
+            if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
             tops[c] = -INFINITY;
 #pragma unroll
-            for (int i = c * Part::V; i < (c + 1) * Part::V; ++i) tops[c] = p.at(i) > tops[c] ? p.at(i) : tops[c];
+            for (int i = c * V; i < (c + 1) * V; ++i) tops[c] = p.at(i) > tops[c] ? p.at(i) : tops[c];
         }
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) best = fmaxf(best, tops[c]);
+    if constexpr (N > 32) p.renew();
     const float most = lanes_max(best), R = most == -INFINITY ? 0.f : most * a.c;
     float S = 0.f, Y = 0.f;
     auto add = [&](float z) {
@@ -202,13 +212,21 @@ template <typename T, int C> __global__ __launch_bounds__(LP_THREADS) void logpr
     if (fabsf(R) < 0x1p20f) {
         // One operation a logit: z + off = c * x - R, where off = c * M - R, what R was rounded by, is 1/16 at most, and taken out of the sums.
 #pragma unroll
-        for (int i = 0; i < N; ++i) add(fmaf(p.at(i), a.c, -R));
+        for (int c = 0; c < C; ++c) {
+            if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
+#pragma unroll
+            for (int i = c * V; i < (c + 1) * V; ++i) add(fmaf(p.at(i), a.c, -R));
+        }
         const float off = most == -INFINITY ? 0.f : fmaf(most, a.c, -R), w = fast_exp2(-off);
         Y = (Y - off * S) * w;
         S *= w;
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) add((p.at(i) - most) * a.c);
+        for (int c = 0; c < C; ++c) {
+            if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
+#pragma unroll
+            for (int i = c * V; i < (c + 1) * V; ++i) add((p.at(i) - most) * a.c);
+        }
     }
     S = wave_sum(S);
     Y = wave_sum(Y);
@@ -217,23 +235,25 @@ template <typename T, int C> __global__ __launch_bounds__(LP_THREADS) void logpr
     __syncthreads();
     Sums t{-INFINITY, 0.f, 0.f};
     if (wave == 0 || a.parts == 1) {
-        t.M = fmaxf(fmaxf(s_sums[0].M, s_sums[1].M), fmaxf(s_sums[2].M, s_sums[3].M));
-#pragma unroll
-        for (int w = 0; w < LP_WAVES; ++w) {
-            Sums p = s_sums[w];
-            sums_to(p, t.M, a.c);
-            t.S += p.S;
-            t.Y += p.Y;
-        }
+        Sums p = lane < WAVES ? s_sums[lane] : Sums{-INFINITY, 0.f, 0.f};
+        t.M = lanes_max(p.M);
+        sums_to(p, t.M, a.c);
+        t.S = wave_sum(p.S);
+        t.Y = wave_sum(p.Y);
     }
     if (a.k) {
-        // k logits or more are no smaller than the k-th largest of the threads' best ones, of which four at a time will do where k is small: that many
-        // take part in a search for its upper 16 bits, a number no larger.
-        const f32x4 b4 = *(const f32x4*)(s_best + 4 * lane);
-        const float b1 = fmaxf(fmaxf(b4[0], b4[1]), fmaxf(b4[2], b4[3]));
+        // k logits or more are no smaller than the k-th largest of the threads' best ones, of which the largest of each 64th of them will do where k is small:
+        // these take part in a search for its upper 16 bits, a number no larger.
+        f32x4 b4 = *(const f32x4*)(s_best + 4 * lane);
+#pragma unroll
+        for (int i = 1; i < THREADS / 256; ++i) {
+            const f32x4 more = *(const f32x4*)(s_best + 256 * i + 4 * lane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b4[e] = fmaxf(b4[e], more[e]);
+        }
         unsigned kth = 0;
         if (a.k <= 32) {
-            const unsigned o = logit_order(b1);
+            const unsigned o = logit_order(fmaxf(fmaxf(b4[0], b4[1]), fmaxf(b4[2], b4[3])));
             for (unsigned bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
                 if (__popcll(__builtin_amdgcn_ballot_w64(o >= (kth | bit))) >= a.k) kth |= bit;
         } else {
@@ -253,7 +273,7 @@ template <typename T, int C> __global__ __launch_bounds__(LP_THREADS) void logpr
         for (int c = 0; c < C; ++c) {
             if (!__builtin_amdgcn_ballot_w64(tops[c] >= least)) continue;
 #pragma unroll
-            for (int i = c * Part::V; i < (c + 1) * Part::V; ++i) have[i / 32] |= p.at(i) >= least ? 1u << i % 32 : 0u;
+            for (int i = c * V; i < (c + 1) * V; ++i) have[i / 32] |= p.at(i) >= least ? 1u << i % 32 : 0u;
         }
         // One of each lane that has some at a time, in any order: they are sorted.  From memory again: a branch for each register would cost more.
 #pragma unroll
@@ -279,16 +299,16 @@ template <typename T, int C> __global__ __launch_bounds__(LP_THREADS) void logpr
             u64 kth = 0;
             int need = a.k;
             for (int shift = 40; shift >= 0; shift -= 8) {
-                s_counts[tid] = 0;
+                if (tid < 256) s_counts[tid] = 0;
                 __syncthreads();
-                for (unsigned i = tid; i < a.span; i += LP_THREADS) {
+                for (unsigned i = tid; i < a.span; i += THREADS) {
                     const u64 key = first + i < end ? key_at(first + i, i) : 0;
                     if (key && key >> shift >> 8 == kth >> shift >> 8) atomicAdd(&s_counts[key >> shift & 255], 1);
                 }
                 __syncthreads();
                 int above = 0;
                 for (int j = tid + 1; j < 256; ++j) above += s_counts[j];
-                if (above < need && above + s_counts[tid] >= need) {
+                if (tid < 256 && above < need && above + s_counts[tid] >= need) {
                     s_count = above;
                     s_digit = tid;
                 }
@@ -299,7 +319,7 @@ template <typename T, int C> __global__ __launch_bounds__(LP_THREADS) void logpr
             }
             if (tid == 0) s_count = 0;
             __syncthreads();
-            for (unsigned i = tid; i < a.span; i += LP_THREADS) {
+            for (unsigned i = tid; i < a.span; i += THREADS) {
                 const u64 key = first + i < end ? key_at(first + i, i) : 0;
                 if (key >= kth) s_keys[atomicAdd(&s_count, 1)] = logit_key((unsigned)(key >> 16), first + i);
             }
@@ -316,13 +336,13 @@ template <typename T, int C> __global__ __launch_bounds__(LP_THREADS) void logpr
     if (a.parts > 1) {
         if (tid == 0) *(f32x4*)(a.sums + (int64_t)blockIdx.x * 4) = f32x4{t.M, t.S, t.Y, 0.f};
     } else {
-        logprob_finish<T>(a, row, t, s_top);
+        logprob_finish<T, THREADS>(a, row, t, s_top);
     }
 }
 
 // Lists i of up to 64, sorted, each of k keys: the k best of them all.  What the m-th of every list (k of them or more together) and the k-th of
 // one are not below is left out, the rest sorted by counting; if that leaves too many, one wave takes the largest of the lists' heads k times.
-template <typename T> __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(LogprobKernelArgs a)
+template <typename T> __global__ __launch_bounds__(LP_JOIN_THREADS) void logprob_join_kernel(LogprobKernelArgs a)
 {
     extern __shared__ __align__(16) unsigned char lp_smem[];
     u64* s_all = (u64*)lp_smem;                                // [lists][k]
@@ -344,7 +364,7 @@ template <typename T> __global__ __launch_bounds__(LP_THREADS) void logprob_join
             high = in[lane * a.k + a.k - 1];
         }
         if (tid == 0) s_count = 0;
-        for (int i = tid; i < lists * a.k; i += LP_THREADS) s_all[i] = in[i];
+        for (int i = tid; i < lists * a.k; i += LP_JOIN_THREADS) s_all[i] = in[i];
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) {
             const u64 l = __shfl_xor(low, o, WAVE), h = __shfl_xor(high, o, WAVE);
@@ -354,7 +374,7 @@ template <typename T> __global__ __launch_bounds__(LP_THREADS) void logprob_join
         u64 least = low > high ? low : high;
         if (!least) least = 1;                                 // 0 is no key
         __syncthreads();
-        for (int i = tid; i < lists * a.k; i += LP_THREADS)
+        for (int i = tid; i < lists * a.k; i += LP_JOIN_THREADS)
             if (s_all[i] >= least) {
                 const int at = atomicAdd(&s_count, 1);
                 if (at < LP_CAP) s_keys[at] = s_all[i];
@@ -386,20 +406,30 @@ template <typename T> __global__ __launch_bounds__(LP_THREADS) void logprob_join
     if (a.parts > 1) {
         if (tid == 0) *(f32x4*)(a.sums + (int64_t)blockIdx.x * 4) = f32x4{t.M, t.S, t.Y, 0.f};
     } else {
-        logprob_finish<T>(a, row, t, s_top);
+        logprob_finish<T, LP_JOIN_THREADS>(a, row, t, s_top);
     }
 }
 
 // ---------------------------------------------------------------- launches
-struct LogprobPlan { int chunks; unsigned parts, span; };
+struct LogprobPlan { int threads, chunks; unsigned parts, span; };
 static unsigned parts_of(int64_t n, int span) { return (unsigned)((n + span - 1) / span); }
 static LogprobPlan logprob_plan(const LogprobArgs& a)
 {
-    const int v = a.dtype == DT_F32 ? 4 : 8, most = a.dtype == DT_F32 ? 8 : 4;
+    const int v = a.dtype == DT_F32 ? 4 : 8;
     const bool aligned = ((uintptr_t)a.logits & 15) == 0 && a.row_stride % v == 0;
     const int64_t n = (int64_t)a.n + (aligned ? 0 : v - 1);
-    LogprobPlan p{1, parts_of(n, LP_THREADS * v), 0};
-    while (p.chunks < most && p.parts > 1 && (p.parts > LP_JOIN || (int64_t)p.parts * a.rows > 256)) p.parts = parts_of(n, LP_THREADS * v * (p.chunks *= 2));
+    // 256 threads, up to 32 logits each: as many parts as that makes, or, where they would not fill the chip, more of fewer logits.
+    LogprobPlan p{256, 1, parts_of(n, 256 * v), 0};
+    const int most = 32 / v;
+    while (p.chunks < most && p.parts > 1 && (p.parts > LP_JOIN || (int64_t)p.parts * a.rows > 256)) p.parts = parts_of(n, 256 * v * (p.chunks *= 2));
+    // Rows of several such parts: more threads save the second launch.  us of both launches / with more threads: bf16, 2048 rows of 50272 47.5 + 6.0 / 45.2,
+    // 256 rows 12.8 + 5.3 / 11.2, 700 of 128256 47.6 + 7.4 / 42.2 + 5.2, 1000 of 12000 13.4 + 5.8 / 11.7; float, a row a CU at most: 1 row of 50272 4.0 + 4.2 / 8.8,
+    // 64 rows 8.3 + 4.3 / 11.9, 256 rows 14.2 + 4.7 / 15.3, but 1000 rows 48 + 9 / 63.
+    if (n > 256 * 32) {
+        const int chunks = a.dtype == DT_F32 ? 13 : 8, threads = a.dtype == DT_BF16 && n <= 512 * v * chunks ? 512 : 1024;
+        const unsigned parts = parts_of(n, threads * v * chunks);
+        if (a.dtype == DT_F32 ? parts == 1 && a.rows <= 256 : parts == 1 || (int64_t)parts * a.rows >= 192) p = LogprobPlan{threads, chunks, parts, 0};
+    }
     p.span = (unsigned)((n + p.parts - 1) / p.parts + 64 * v - 1) / (64 * v) * (64 * v);       // equal ones, of whole KB
     p.parts = parts_of(n, p.span);
     return p;
@@ -424,7 +454,7 @@ template <typename T> static hipError_t launch_logprobs_t(const LogprobArgs& a, 
 {
     const LogprobPlan p = logprob_plan(a);
     // a launch has fewer than 2^32 threads
-    const int64_t fit = MAX_LAUNCH_THREADS / LP_THREADS / p.parts;
+    const int64_t fit = MAX_LAUNCH_THREADS / p.threads / p.parts;
     for (int64_t r0 = 0; r0 < a.rows; r0 += fit) {
         const int64_t rows = a.rows - r0 < fit ? a.rows - r0 : fit;
         LogprobKernelArgs k{};
@@ -455,10 +485,14 @@ template <typename T> static hipError_t launch_logprobs_t(const LogprobArgs& a, 
         k.span = p.span;
         level(p.parts);
         const unsigned wgs = (unsigned)(rows * p.parts);
-        if (p.chunks == 1) logprob_part_kernel<T, 1><<<wgs, LP_THREADS, 0, s>>>(k);
-        else if (p.chunks == 2) logprob_part_kernel<T, 2><<<wgs, LP_THREADS, 0, s>>>(k);
-        else if (p.chunks == 4) logprob_part_kernel<T, 4><<<wgs, LP_THREADS, 0, s>>>(k);
-        else if constexpr (sizeof(T) == 4) logprob_part_kernel<T, 8><<<wgs, LP_THREADS, 0, s>>>(k);
+        constexpr int V = 16 / (int)sizeof(T);
+        if (p.threads == 1024) logprob_part_kernel<T, 1024, (V == 4 ? 13 : 8)><<<wgs, 1024, 0, s>>>(k);
+        else if (p.threads == 512) {
+            if constexpr (V == 8) logprob_part_kernel<T, 512, 8><<<wgs, 512, 0, s>>>(k);
+        } else if (p.chunks == 1) logprob_part_kernel<T, 256, 1><<<wgs, 256, 0, s>>>(k);
+        else if (p.chunks == 2) logprob_part_kernel<T, 256, 2><<<wgs, 256, 0, s>>>(k);
+        else if (p.chunks == 4) logprob_part_kernel<T, 256, 4><<<wgs, 256, 0, s>>>(k);
+        else if constexpr (V == 4) logprob_part_kernel<T, 256, 8><<<wgs, 256, 0, s>>>(k);
         hipError_t e = hipGetLastError();
         for (unsigned parts = p.parts; e == hipSuccess && parts > 1; parts = k.parts) {
             k.from_parts = parts;
@@ -466,7 +500,7 @@ template <typename T> static hipError_t launch_logprobs_t(const LogprobArgs& a, 
             k.from_lists = k.lists;
             level(parts_of(parts, LP_JOIN));
             const unsigned lists = parts < LP_JOIN ? parts : LP_JOIN;
-            logprob_join_kernel<T><<<(unsigned)(rows * k.parts), LP_THREADS, lists * a.k * sizeof(u64), s>>>(k);
+            logprob_join_kernel<T><<<(unsigned)(rows * k.parts), LP_JOIN_THREADS, lists * a.k * sizeof(u64), s>>>(k);
             e = hipGetLastError();
         }
         if (e != hipSuccess) return e;

@@ -78,6 +78,18 @@ def test_sizes(dtype, n, rows):
         check(x, scale, tokens, k, call(x.to(DEV), n, scale, tokens, k))
 
 
+@pytest.mark.parametrize("dtype,rows,n", [("f32", 300, 8200), ("f32", 300, 50272), ("f32", 257, 53249), ("f32", 3, 53248), ("f32", 3, 53249), ("bf16", 300, 32768), ("bf16", 300, 32769),
+                                          ("bf16", 2, 65536), ("bf16", 2, 65537), ("bf16", 200, 70001), ("bf16", 80, 70001)])
+def test_launches(dtype, rows, n):
+    """Each number of threads, one launch and two; rows on either side of what a workgroup holds."""
+    g = torch.Generator().manual_seed(n)
+    x = (torch.randn((rows, n), generator=g) * 2.5).to(TYPES[dtype][1])
+    x[0], x[1, :n - 50] = 0.25, -math.inf
+    tokens = torch.randint(n - 50, n, (rows, 1), generator=g, dtype=torch.int32).to(DEV)
+    check(x, 1.0, tokens, 20, call(x.to(DEV), n, 1.0, tokens, 20))
+    check(x[:3], 1.0, tokens[:3], 50, call(x[:3].to(DEV), n, 1.0, tokens[:3], 50))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("n", [600000, 4300001])
 def test_long_rows(dtype, n):
@@ -253,4 +265,4 @@ def test_tensors_that_would_be_misread_are_refused():
         with pytest.raises(AssertionError):
             exe.exe_op_logprobs(**{**good, **change})
     with pytest.raises(exe.ExeError):
-        exe.exe_op_logprobs(**{**good, "logits": torch.zeros((4, 30000), device=DEV), "row_stride": 30000, "n": 30000})      # no workspace
+        exe.exe_op_logprobs(**{**good, "logits": torch.zeros((4, 60000), device=DEV), "row_stride": 60000, "n": 60000})      # no workspace

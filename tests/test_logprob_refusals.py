@@ -43,20 +43,20 @@ def test_append_refusals(change, code):
 @pytest.mark.parametrize("change,code", [
     (dict(dtype=2), -1), (dict(rows=-1), -1), (dict(n=0), -1), (dict(n_tokens=-1), -1), (dict(top_k=-1), -2), (dict(top_k=65), -2), (dict(n=4, top_k=5), -2), (dict(scale=0.0), -1),
     (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(row_stride=99), -2), (dict(logits=None), -1), (dict(tokens=None), -1),
-    (dict(logprobs=None), -1), (dict(top_ids=None), -1), (dict(top_logprobs=None), -1), (dict(logits=P + 2), -1), (dict(dtype=1, logits=P + 1), -1), (dict(n=50000, row_stride=50000), -1)])
+    (dict(logprobs=None), -1), (dict(top_ids=None), -1), (dict(top_logprobs=None), -1), (dict(logits=P + 2), -1), (dict(dtype=1, logits=P + 1), -1), (dict(n=200000, row_stride=200000), -1)])
 def test_logprob_refusals(change, code):
     refused(exe.exe_op_logprobs, LOGPROBS, code, **change)
 
 
 def test_workspaces():
-    need = exe.exe_op_logprobs_workspace(0, 3, 50000, 5)
+    need = exe.exe_op_logprobs_workspace(0, 3, 200000, 5)
     assert need > 0 and exe.exe_op_logprobs_workspace(0, 3, 100, 5) == 0
     for ws, size in ((P, need - 1), (P + 8, need)):
         with pytest.raises(exe.ExeError):
-            exe.exe_op_logprobs(*{**LOGPROBS, "n": 50000, "row_stride": 50000, "rows": 3}.values(), ws, stream=1, ws_bytes=size)
+            exe.exe_op_logprobs(*{**LOGPROBS, "n": 200000, "row_stride": 200000, "rows": 3}.values(), ws, stream=1, ws_bytes=size)
     with pytest.raises(AssertionError):
-        exe.exe_op_logprobs(*{**LOGPROBS, "n": 50000, "row_stride": 50000, "rows": 3}.values(), P, stream=1)
-    good = (0, 3, 50000, 5)
+        exe.exe_op_logprobs(*{**LOGPROBS, "n": 200000, "row_stride": 200000, "rows": 3}.values(), P, stream=1)
+    good = (0, 3, 200000, 5)
     for i, v in ((0, 2), (1, 0), (1, -1), (2, 0), (3, -1), (3, 65)):
         assert exe.exe_op_logprobs_workspace(*good[:i], v, *good[i + 1:]) == 0
     # sizes do not shrink where rows begin on single elements, or rows and tokens are more
