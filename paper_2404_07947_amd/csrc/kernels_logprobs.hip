@@ -5,6 +5,8 @@
 //  * logprob_part_kernel: a workgroup takes 256 * C chunks of 16 bytes of a row into registers, in one round of loads, and makes the sums and the sorted
 //    list of its k best from there: the logits are read once.
 //  * logprob_join_kernel: where a row has several parts, adds up their sums and merges their lists, 64 parts at a time.
+#include <type_traits>
+
 #include "attn_row.h"
 #include "kernels.h"
 
@@ -78,6 +80,17 @@ template <typename T, int THREADS> __device__ __forceinline__ void logprob_finis
     }
 }
 
+// f of 0 .. C - 1 as constants, as far as `chunks` goes (SOME; else all): one branch around all that follow, where the compiler makes of a loop with a
+// condition one for each, which it then moves together (bf16 rows 45 us, so 59), and of a longer one with a break no constants.
+template <int C, bool SOME, int I = 0, typename F> __device__ __forceinline__ void each_chunk(int chunks, F f)
+{
+    if constexpr (I < C) {
+        if (SOME && I >= chunks) return;
+        f(std::integral_constant<int, I>{});
+        each_chunk<C, SOME, I + 1>(chunks, f);
+    }
+}
+
 template <typename T, int THREADS, int C> struct LogitPart {
     static constexpr bool SOME = THREADS > 256;              // else all chunks are in use
     static constexpr int V = 16 / (int)sizeof(T), N = C * V, SPAN = THREADS * N;
@@ -102,26 +115,26 @@ template <typename T, int THREADS, int C> struct LogitPart {
     // Of the C chunks the first `chunks` are in use.
     __device__ __forceinline__ void load(const T* x, unsigned first, unsigned end, unsigned n, int chunks)
     {
-        const int low = (int)(-(unsigned)((uintptr_t)x & 15) / sizeof(T) % V), high = (int)(n - low) < V ? -1 : low + ((int)n - low - V) / V * V;
-        if (high >= 0) {
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
-                const int i = (int)(first + place(c * V));
-                raw[c] = load_chunk<true>(x + (i < low ? low : i < high ? i : high));
-            }
+        // whole chunks of the row: from its first or second one on, up to `high`, both counted from `first`
+        const int lead = (int)((uintptr_t)x & 15) / (int)sizeof(T), low = first > n && lead ? V : 0;
+        const int64_t at = first > n ? -(int64_t)lead : (int64_t)first, high = at + ((int64_t)n - at) / V * V - V - at;
+        if (high >= low) {
+            const char* base = (const char*)(x + at);
+            const int most = high < SPAN ? (int)high : SPAN;
+            each_chunk<C, SOME>(chunks, [&](auto c) {
+                int i = (int)place(c * V);
+                i = i < low ? low : i < most ? i : most;
+                raw[c] = load_chunk<true>((const uint4*)(base + (unsigned)(i * (int)sizeof(T))));
+            });
         }
-        // the last thread's last chunk is there, and the first thread's first: all are
-        if (first < end && end - first >= (unsigned)chunks * THREADS * V) return;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
+        if (first < end && end - first >= SPAN) return;        // all of them whole
+        each_chunk<C, SOME>(chunks, [&](auto c) {
             const unsigned i = first + place(c * V);
-            if (i < end && end - i >= V) continue;
-            if (i - first >= end - first) {                    // nothing of it
+            if (i < end && end - i >= V) return;
+            if ((int)(end - i) <= 0) {                         // nothing of it
                 const unsigned none = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
                 raw[c] = uint4{none, none, none, none};
-                continue;
+                return;
             }
             unsigned w[4];
 #pragma unroll
@@ -134,7 +147,7 @@ template <typename T, int THREADS, int C> struct LogitPart {
                 }
             }
             raw[c] = uint4{w[0], w[1], w[2], w[3]};
-        }
+        });
     }
 };
 __device__ __forceinline__ float max3(float a, float b, float c)
@@ -173,7 +186,8 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
     const T* x = (const T*)a.logits + row * a.row_stride;
     const unsigned first = part * a.span - (unsigned)((uintptr_t)x & 15) / sizeof(T), end = first + a.span < a.n ? first + a.span : a.n;
     Part p;
-    const int chunks = (a.span + THREADS * V - 1) / (THREADS * V);
+    // chunks of which this wave has something
+    const int there = (int)(end - first) - __builtin_amdgcn_readfirstlane(wave) * (WAVE * V), chunks = there > 0 ? (there + THREADS * V - 1) / (THREADS * V) : 0;
     p.load(x, first, end, a.n, chunks);
     if (tid == 0) s_count = 0;
 
@@ -181,23 +195,19 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
     bool none = false;
 #pragma unroll
     for (int c = 0; c < C; ++c) tops[c] = -INFINITY;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
+    each_chunk<C, SOME>(chunks, [&](auto c) {
         const int i = c * V;
         tops[c] = max3(p.at(i), p.at(i + 1), p.at(i + 2));
         if constexpr (V == 8) tops[c] = max3(max3(tops[c], p.at(i + 3), p.at(i + 4)), p.at(i + 5), p.at(i + 6));
         tops[c] = max3(tops[c], tops[c], p.at(i + V - 1));
         none |= tops[c] != tops[c];
-    }
+    });
     if (none) {                                                // all of a chunk NaN, or signalling ones, which that instruction hands on
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
+        each_chunk<C, SOME>(chunks, [&](auto c) {
             tops[c] = -INFINITY;
 #pragma unroll
             for (int i = c * V; i < (c + 1) * V; ++i) tops[c] = p.at(i) > tops[c] ? p.at(i) : tops[c];
-        }
+        });
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) best = fmaxf(best, tops[c]);
@@ -211,22 +221,18 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
     };
     if (fabsf(R) < 0x1p20f) {
         // One operation a logit: z + off = c * x - R, where off = c * M - R, what R was rounded by, is 1/16 at most, and taken out of the sums.
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
+        each_chunk<C, SOME>(chunks, [&](auto c) {
 #pragma unroll
             for (int i = c * V; i < (c + 1) * V; ++i) add(fmaf(p.at(i), a.c, -R));
-        }
+        });
         const float off = most == -INFINITY ? 0.f : fmaf(most, a.c, -R), w = fast_exp2(-off);
         Y = (Y - off * S) * w;
         S *= w;
     } else {
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            if (SOME && c >= chunks) { if constexpr (C > 8) continue; else break; }     // longer loops with a break stay loops
+        each_chunk<C, SOME>(chunks, [&](auto c) {
 #pragma unroll
             for (int i = c * V; i < (c + 1) * V; ++i) add((p.at(i) - most) * a.c);
-        }
+        });
     }
     S = wave_sum(S);
     Y = wave_sum(Y);
@@ -423,8 +429,8 @@ static LogprobPlan logprob_plan(const LogprobArgs& a)
     const int most = 32 / v;
     while (p.chunks < most && p.parts > 1 && (p.parts > LP_JOIN || (int64_t)p.parts * a.rows > 256)) p.parts = parts_of(n, 256 * v * (p.chunks *= 2));
     // Rows of several such parts: more threads save the second launch.  us of both launches / with more threads: bf16, 2048 rows of 50272 47.5 + 6.0 / 45.2,
-    // 256 rows 12.8 + 5.3 / 11.2, 700 of 128256 47.6 + 7.4 / 42.2 + 5.2, 1000 of 12000 13.4 + 5.8 / 11.7; float, a row a CU at most: 1 row of 50272 4.0 + 4.2 / 8.8,
-    // 64 rows 8.3 + 4.3 / 11.9, 256 rows 14.2 + 4.7 / 15.3, but 1000 rows 48 + 9 / 63.
+    // 256 rows 12.8 + 5.3 / 11.2, 700 of 128256 47.6 + 7.4 / 42.2 + 5.2, 1000 of 12000 13.4 + 5.8 / 11.7; float, a row a CU at most: 1 row of 50272 4.0 + 4.2 / 7.7,
+    // 64 rows 8.3 + 4.3 / 11.9, 256 rows 14.2 + 4.7 / 14.6, but 1000 rows 48 + 9 / 63.
     if (n > 256 * 32) {
         const int chunks = a.dtype == DT_F32 ? 13 : 8, threads = a.dtype == DT_BF16 && n <= 512 * v * chunks ? 512 : 1024;
         const unsigned parts = parts_of(n, threads * v * chunks);
