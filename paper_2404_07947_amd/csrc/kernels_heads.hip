@@ -11,7 +11,10 @@ namespace exe {
 // each, which are those of its turned pairs: statistics, gain and turn are made in registers, in float, and rounded once.  Since
 // a wave's 64 lanes are whole heads, a lane has the same place in each of its heads, and keeps its sines and cosines.
 //
-// Bound by memory where tokens are many: every element is read once and written once.
+// Bound by memory where tokens are many: every element is read once and written once.  4000 tokens of OPT-13B's 120 heads x 128 in chunks 54 us, 4.3 TB/s
+// (rotary_append_kernel 50, a large copy 46); two slots in flight a lane, as there, 59, and three 65, for their registers take away waves; ordinary
+// loads and, into the cache, stores (nontemporal ones 56 and 57).  4099 x 20 x 64 in float 11 us.  Few tokens: the call, of which the
+// kernel takes 2.8 us (one token) or 4.4 (64 sequences; their place in the cache is found while the rows are on their way).
 template <int P> __device__ __forceinline__ float head_sum(float d)
 {
     if constexpr (P == 64) return wave_sum(d);
@@ -79,19 +82,16 @@ __global__ __launch_bounds__(ROT_WAVES * 64) void head_norm_kernel(HeadNormArgs 
     const int normed = a.H + a.Hkv, step = parts * HEADS;
     int heads = a.H + 2 * a.Hkv, h0 = (APPEND && !a.out ? a.H : 0) + part * HEADS + lane / PER;
 
-    E x[ROT_U][2], gain[ROT_U][2];
+    E x[2], gain[2];
     auto load = [&](int h) {
-#pragma unroll
-        for (int u = 0; u < ROT_U; ++u, h += step) {
-            if (h >= heads) continue;
-            x[u][0] = *(const E*)(xr + (int64_t)h * DH + c0);
-            x[u][1] = *(const E*)(xr + (int64_t)h * DH + c1);
-            const T* g = (const T*)(h < a.H ? a.q_gain : a.k_gain);
-            if (!g || h >= normed) continue;
-            g += a.gain_per_head ? (int64_t)(h < a.H ? h : h - a.H) * DH : 0;
-            gain[u][0] = *(const E*)(g + c0);
-            gain[u][1] = *(const E*)(g + c1);
-        }
+        if (h >= heads) return;
+        x[0] = *(const E*)(xr + (int64_t)h * DH + c0);
+        x[1] = *(const E*)(xr + (int64_t)h * DH + c1);
+        const T* g = (const T*)(h < a.H ? a.q_gain : a.k_gain);
+        if (!g || h >= normed) return;
+        g += a.gain_per_head ? (int64_t)(h < a.H ? h : h - a.H) * DH : 0;
+        gain[0] = *(const E*)(g + c0);
+        gain[1] = *(const E*)(g + c1);
     };
     load(h0);                                      // on its way while the token's place is found
     int at = 0, blk = 0;
@@ -114,42 +114,36 @@ __global__ __launch_bounds__(ROT_WAVES * 64) void head_norm_kernel(HeadNormArgs 
     const int rows = APPEND ? 1 << a.table.shift : 0;
     T* kd = APPEND ? (T*)a.kv_blocks + ((int64_t)blk * 2 * a.Hkv * rows + (at & (rows - 1))) * DH : nullptr;   // head g's key at kd + g * rows * DH
     while (h0 < heads) {
+        if (!APPEND || h0 < normed) {              // (asked without need, float rows' stores came out with an address over their data)
+            float v[N];
+            head_norm<DH, N>([&](int e) { return to_f32(x[e / EPL].v[e % EPL]); }, v, a.rms, a.eps);
+            if (h0 < a.H ? a.q_gain : a.k_gain) {
 #pragma unroll
-        for (int u = 0; u < ROT_U; ++u) {
-            const int h = h0 + u * step;
-            if (h < heads) {
-                if (h < normed) {
-                    float v[N];
-                    head_norm<DH, N>([&](int e) { return to_f32(x[u][e / EPL].v[e % EPL]); }, v, a.rms, a.eps);
-                    if (h < a.H ? a.q_gain : a.k_gain) {
+                for (int e = 0; e < N; ++e) v[e] *= to_f32(gain[e / EPL].v[e % EPL]);
+            }
+            if (turn) {
 #pragma unroll
-                        for (int e = 0; e < N; ++e) v[e] *= to_f32(gain[u][e / EPL].v[e % EPL]);
-                    }
-                    if (turn) {
-#pragma unroll
-                        for (int e = 0; e < EPL; ++e) {
-                            if (INTERLEAVED && pair + e >= half) continue;       // rot ends inside the chunks
-                            float &p = v[INTERLEAVED ? 2 * e : e], &q = v[INTERLEAVED ? 2 * e + 1 : EPL + e];
-                            const float b = p, c = q;
-                            p = b * cs[e].x - c * cs[e].y;
-                            q = c * cs[e].x + b * cs[e].y;
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < N; ++e) x[u][e / EPL].v[e % EPL] = from_f32<T>(v[e]);
-                }
-                T* to = !APPEND || h < a.H ? qr + (int64_t)h * DH : kd + (int64_t)(h - a.H) * rows * DH;
-                if constexpr (!APPEND && sizeof(E) == 16) {
-                    typedef unsigned v4u __attribute__((ext_vector_type(4)));
-                    __builtin_nontemporal_store(__builtin_bit_cast(v4u, x[u][0]), (v4u*)(to + c0));
-                    __builtin_nontemporal_store(__builtin_bit_cast(v4u, x[u][1]), (v4u*)(to + c1));
-                } else {
-                    *(E*)(to + c0) = x[u][0];
-                    *(E*)(to + c1) = x[u][1];
+                for (int e = 0; e < EPL; ++e) {
+                    if (INTERLEAVED && pair + e >= half) continue;               // rot ends inside the chunks
+                    float &p = v[INTERLEAVED ? 2 * e : e], &q = v[INTERLEAVED ? 2 * e + 1 : EPL + e];
+                    const float b = p, c = q;
+                    p = b * cs[e].x - c * cs[e].y;
+                    q = c * cs[e].x + b * cs[e].y;
                 }
             }
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[e / EPL].v[e % EPL] = from_f32<T>(v[e]);
         }
-        h0 += ROT_U * step;
+        T* to = !APPEND || h0 < a.H ? qr + (int64_t)h0 * DH : kd + (int64_t)(h0 - a.H) * rows * DH;
+        if constexpr (!APPEND && sizeof(E) == 16) {
+            typedef unsigned v4u __attribute__((ext_vector_type(4)));
+            __builtin_nontemporal_store(__builtin_bit_cast(v4u, x[0]), (v4u*)(to + c0));
+            __builtin_nontemporal_store(__builtin_bit_cast(v4u, x[1]), (v4u*)(to + c1));
+        } else {
+            *(E*)(to + c0) = x[0];
+            *(E*)(to + c1) = x[1];
+        }
+        h0 += step;
         load(h0);
     }
 }
