@@ -1,4 +1,4 @@
-"""Marshalling for include/exe.h, by ctypes and (encode, decode_step, seq_release) csrc/call.c.  No arithmetic of the method lives here."""
+"""Marshalling for include/exe.h, by ctypes and, for the calls of a serving loop, csrc/call.c.  No arithmetic of the method lives here."""
 from __future__ import annotations
 
 import ctypes as C
@@ -118,7 +118,8 @@ def lib():
             raise ImportError(f"{f} is not built; run `python -m paper_2404_07947_amd.build` (needs hipcc)")
     from . import _call
     L = C.CDLL(p)
-    L.at = {f: C.cast(getattr(L, "exe_" + f), C.c_void_p).value for f in ("encode", "decode_step", "seq_release")}
+    L.at = {f: C.cast(getattr(L, "exe_" + f), C.c_void_p).value for f in
+            ("encode", "decode_step", "seq_release", "op_head_norm_rotary", "op_head_norm_rotary_append_paged", "op_prefix_attention_paged", "op_logprobs")}
     vp, i32, ip = C.c_void_p, C.c_int32, C.POINTER(C.c_int32)
     L.exe_expected_weights.argtypes = [C.POINTER(Config)]
     L.exe_model_load.argtypes = [C.POINTER(Config), C.POINTER(Tensor), i32, vp, C.POINTER(vp)]
@@ -229,6 +230,8 @@ def _current():
         torch.cuda.init()
         # torch's own look-up, without the objects
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+        lib()
+        _call.types(torch.float32, torch.bfloat16, torch.int32, torch.float64)
         _torch = torch
     dev = _torch.cuda.current_device()
     return dev, _raw_stream(dev) or None
@@ -263,6 +266,7 @@ def _where(stream):
     except (RuntimeError, AssertionError):
         if stream is None:
             raise
+        lib()
         return None, _stream_ptr(stream)
     if stream is None:
         return dev, current
@@ -567,46 +571,21 @@ def exe_op_rotary_append_paged(dtype, n_seqs, cu_seqlens, T, qkv, row_stride, H,
                                             _array(length, dev, "int32", n_seqs), _rows(q_out, dev, dtype, T, H * dh, q_out_stride), q_out_stride))
 
 
-def _kind(dtype: int) -> str:
-    return "bfloat16" if dtype else "float32"
-
-
 def exe_op_head_norm_rotary(dtype, T, x, x_stride, heads, dh, rms, gain, gain_per_head, eps, rot, interleaved, pos, inv_freq, amplitude, out,
                             out_stride, stream=None):
     """x and out: as exe_op_rotary takes them; gain: [dh] or [heads, dh] of the storage type, or None."""
     dev, s = _where(stream)
-    _check(lib().exe_op_head_norm_rotary(s, dtype, T, _rows(x, dev, dtype, T, heads * dh, x_stride), x_stride, heads, dh, rms,
-                                         _array(gain, dev, _kind(dtype), heads * dh if gain_per_head else dh), gain_per_head, eps, rot, interleaved,
-                                         _array(pos, dev, "int32", T), _array(inv_freq, dev, "float64", rot // 2), amplitude,
-                                         _rows(out, dev, dtype, T, heads * dh, out_stride), out_stride))
+    _check(_call.head_norm_rotary(lib().at["op_head_norm_rotary"], dev, s, dtype, T, x, x_stride, heads, dh, rms, gain, gain_per_head, eps, rot, interleaved,
+                                  pos, inv_freq, amplitude, out, out_stride))
 
 
 def exe_op_head_norm_rotary_append_paged(dtype, n_seqs, cu_seqlens, T, qkv, row_stride, H, Hkv, dh, rms, q_gain, k_gain, gain_per_head, eps, rot,
                                          interleaved, pos, inv_freq, amplitude, kv_blocks, n_blocks, block_table, max_blocks, block_size, length,
                                          q_out, q_out_stride, stream=None):
     dev, s = _where(stream)
-    block = 2 * Hkv * block_size * dh
-    _check(lib().exe_op_head_norm_rotary_append_paged(s, dtype, n_seqs, _array(cu_seqlens, dev, "int32", n_seqs + 1), T,
-                                                      _rows(qkv, dev, dtype, T, (H + 2 * Hkv) * dh, row_stride), row_stride, H, Hkv, dh, rms,
-                                                      _array(q_gain, dev, _kind(dtype), H * dh if gain_per_head else dh),
-                                                      _array(k_gain, dev, _kind(dtype), Hkv * dh if gain_per_head else dh), gain_per_head, eps, rot,
-                                                      interleaved, _array(pos, dev, "int32", T), _array(inv_freq, dev, "float64", rot // 2), amplitude,
-                                                      _rows(kv_blocks, dev, dtype, n_blocks, block, block), n_blocks,
-                                                      _array(block_table, dev, "int32", n_seqs * max_blocks), max_blocks, block_size,
-                                                      _array(length, dev, "int32", n_seqs), _rows(q_out, dev, dtype, T, H * dh, q_out_stride), q_out_stride))
-
-
-def _workspace(workspace, dev, ws_bytes):
-    """(address, bytes) of a device tensor, or of an address and its size."""
-    if workspace is None:
-        return None, 0
-    if isinstance(workspace, int):
-        assert ws_bytes is not None and ws_bytes >= 0, "an address needs its size, ws_bytes"
-        return workspace, ws_bytes
-    assert workspace.get_device() == dev, "expected a workspace on the current device"
-    have = workspace.numel() * workspace.element_size()
-    assert ws_bytes is None or 0 <= ws_bytes <= have, f"a workspace of {have} bytes"
-    return _dev(workspace), have if ws_bytes is None else ws_bytes
+    _check(_call.head_norm_rotary_append_paged(lib().at["op_head_norm_rotary_append_paged"], dev, s, dtype, n_seqs, cu_seqlens, T, qkv, row_stride, H, Hkv, dh,
+                                               rms, q_gain, k_gain, gain_per_head, eps, rot, interleaved, pos, inv_freq, amplitude, kv_blocks, n_blocks,
+                                               block_table, max_blocks, block_size, length, q_out, q_out_stride))
 
 
 def exe_op_chunk_attention_paged_workspace(dtype, n_seqs, T, max_new, max_len, H, Hkv, dh, window=0) -> int:
@@ -644,15 +623,9 @@ def exe_op_prefix_attention_paged(dtype, n_seqs, cu_seqlens, T, max_new, n_group
                                   stream=None, ws_bytes=None):
     """workspace: a device tensor, or an address and ws_bytes."""
     dev, s = _where(stream)
-    ws, ws_bytes = _workspace(workspace, dev, ws_bytes)
-    block = 2 * Hkv * block_size * dh
-    _check(lib().exe_op_prefix_attention_paged(s, dtype, n_seqs, _array(cu_seqlens, dev, "int32", n_seqs + 1), T, max_new, n_groups,
-                                               _array(cu_groups, dev, "int32", n_groups + 1), _array(prefix, dev, "int32", n_groups), max_group,
-                                               max_prefix, _rows(q, dev, dtype, T, H * dh, q_stride), q_stride,
-                                               _rows(kv_blocks, dev, dtype, n_blocks, block, block), n_blocks,
-                                               _array(block_table, dev, "int32", n_seqs * max_blocks), max_blocks, block_size,
-                                               _array(length, dev, "int32", n_seqs), max_own, H, Hkv, dh, scale,
-                                               _rows(out, dev, dtype, T, H * dh, out_stride), out_stride, ws, ws_bytes))
+    _check(_call.prefix_attention_paged(lib().at["op_prefix_attention_paged"], dev, s, dtype, n_seqs, cu_seqlens, T, max_new, n_groups, cu_groups, prefix,
+                                        max_group, max_prefix, q, q_stride, kv_blocks, n_blocks, block_table, max_blocks, block_size, length, max_own, H, Hkv,
+                                        dh, scale, out, out_stride, workspace, ws_bytes))
 
 
 def exe_op_kv_copy_blocks(dtype, kv_blocks, n_layers, n_blocks, block_size, Hkv, dh, copies, stream=None):
@@ -692,11 +665,8 @@ def exe_op_logprobs(dtype, logits, row_stride, rows, n, scale, tokens, n_tokens,
                     stream=None, ws_bytes=None):
     """logits: a device tensor (or address) whose rows are row_stride elements apart; workspace: a device tensor, or an address and ws_bytes."""
     dev, s = _where(stream)
-    ws, ws_bytes = _workspace(workspace, dev, ws_bytes)
-    _check(lib().exe_op_logprobs(s, dtype, _rows(logits, dev, dtype, rows, n, row_stride), row_stride, rows, n, scale,
-                                 _array(tokens, dev, "int32", rows * n_tokens), n_tokens, _array(logprobs, dev, "float32", rows * n_tokens),
-                                 _array(entropy, dev, "float32", rows), top_k, _array(top_ids, dev, "int32", rows * top_k),
-                                 _array(top_logprobs, dev, "float32", rows * top_k), ws, ws_bytes))
+    _check(_call.logprobs(lib().at["op_logprobs"], dev, s, dtype, logits, row_stride, rows, n, scale, tokens, n_tokens, logprobs, entropy, top_k, top_ids,
+                          top_logprobs, workspace, ws_bytes))
 
 
 def exe_op_argmax(logits, rows, n, out, stream=None):
