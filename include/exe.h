@@ -518,14 +518,14 @@ int exe_op_kv_copy_blocks(void* hip_stream, int32_t dtype, void* kv_blocks, int3
 /* argmax over each row of float logits [rows, n] -> int32 out [rows]; lowest index on ties */
 int exe_op_argmax(void* hip_stream, const float* logits, int32_t rows, int32_t n, int32_t* out);
 /* Log probabilities, p = softmax(scale * logits) row by row: rows of n logits (dtype, row_stride elements apart, aligned to their type),
- * scale > 0 (one over a temperature).
+ * scale > 0 (one over a temperature), at most 2.3e38.
  *  logprobs [rows, n_tokens] float: ln p of tokens [rows, n_tokens] (int32, device); a token outside of 0 .. n - 1 is never looked up, and NaN.
  *  entropy [rows] float, nullable: -sum p ln p.
  *  top_ids [rows, top_k] int32, top_logprobs [rows, top_k] float: the top_k (0 .. 64, at most n) largest logits, largest first, the lowest
  *  index on ties, and their ln p.  Logits of minus infinity are ruled out: their p is 0, they are no alternatives, and where fewer than
  *  top_k are left the rest is -1 and minus infinity.  A NaN is never an alternative either.
  * Log probabilities and entropy of a row with a NaN or plus infinity, or without any number above minus infinity, are NaN; those of alternatives
- * that are there too.  Sums in float; each row's results depend on that row alone.  What is not asked for (n_tokens 0, top_k 0) may be NULL.
+ * that are there too.  Sums in float; no row's logits reach another one's results.  What is not asked for (n_tokens 0, top_k 0) may be NULL.
  * workspace: exe_op_logprobs_workspace bytes (0 for bad arguments; it covers any alignment), 16-byte aligned, NULL if that is 0; nothing in it needs clearing; calls that may
  * overlap need one each. */
 int exe_op_logprobs(void* hip_stream, int32_t dtype, const void* logits, int64_t row_stride, int32_t rows, int32_t n, float scale,

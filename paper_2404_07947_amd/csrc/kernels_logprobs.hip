@@ -55,7 +55,8 @@ struct Sums { float M, S, Y; };
 __device__ __forceinline__ void sums_to(Sums& p, float M, float c)
 {
     if (p.M == -INFINITY) return;
-    const float d = fmaxf((p.M - M) * c, -1e30f), w = fast_exp2(d);
+    // halves, whose difference is never infinite where the scale makes it small
+    const float d = fmaxf((0.5f * p.M - 0.5f * M) * c * 2.f, -1e30f), w = fast_exp2(d);
     p.Y = w * fmaf(p.S, d, p.Y);
     p.S *= w;
     p.M = M;
@@ -157,7 +158,7 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return r;
 }
 
-// The best keys among those of the part that `take` lets through, at most LP_CAP: sorted by counting, for each, those above it.
+// The k best of `count` keys, at most LP_CAP, sorted by counting, for each, those above it; 0 where there are fewer.
 __device__ __forceinline__ void sort_keys(const u64* keys, int count, u64* top, int k)
 {
     const int tid = threadIdx.x;

@@ -2631,7 +2631,7 @@ extern "C" int exe_op_logprobs(void* hip_stream, int32_t dtype, const void* logi
     if (dtype != DT_F32 && dtype != DT_BF16) return fail(EXE_ERR_ARG, "bad dtype");
     if (rows < 0 || n < 1 || n_tokens < 0) return fail(EXE_ERR_ARG, "bad log probability arguments");
     if (top_k < 0 || top_k > LOGPROB_MAX_TOP || top_k > n) return fail(EXE_ERR_SHAPE, "%d alternatives of %d tokens", top_k, n);
-    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(EXE_ERR_ARG, "a scale of %g", (double)scale);
+    if (!(scale > 0.f) || !std::isfinite(scale * 1.442696f)) return fail(EXE_ERR_ARG, "a scale of %g", (double)scale);     // it is taken to base 2
     if (row_stride < n) return fail(EXE_ERR_SHAPE, "rows of %d logits overlap", n);
     if (rows == 0) return EXE_OK;
     if (!logits || (n_tokens > 0 && (!tokens || !logprobs)) || (top_k > 0 && (!top_ids || !top_logprobs))) return fail(EXE_ERR_ARG, "bad log probability arguments");

@@ -266,3 +266,16 @@ def test_tensors_that_would_be_misread_are_refused():
             exe.exe_op_logprobs(**{**good, **change})
     with pytest.raises(exe.ExeError):
         exe.exe_op_logprobs(**{**good, "logits": torch.zeros((4, 60000), device=DEV), "row_stride": 60000, "n": 60000})      # no workspace
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [5000, 40000, 600000])
+def test_far_apart_at_a_small_scale(dtype, n):
+    """Logits whose differences pass the largest float, which the scale brings back to a few units: in one wave, of several and of several parts."""
+    g = torch.Generator().manual_seed(n)
+    x = torch.full((3, n), -3e38)
+    x[0, n // 2], x[1, -1] = 3e38, 2e38
+    x[2] = (2 * torch.rand(n, generator=g) - 1) * 3e38
+    x = x.to(TYPES[dtype][1])
+    tokens = torch.tensor([[0, n // 2, n - 1]] * 3, dtype=torch.int32, device=DEV)
+    check(x, 2e-38, tokens, 8, call(x.to(DEV), n, 2e-38, tokens, 8))

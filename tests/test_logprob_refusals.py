@@ -42,7 +42,7 @@ def test_append_refusals(change, code):
 
 @pytest.mark.parametrize("change,code", [
     (dict(dtype=2), -1), (dict(rows=-1), -1), (dict(n=0), -1), (dict(n_tokens=-1), -1), (dict(top_k=-1), -2), (dict(top_k=65), -2), (dict(n=4, top_k=5), -2), (dict(scale=0.0), -1),
-    (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(row_stride=99), -2), (dict(logits=None), -1), (dict(tokens=None), -1),
+    (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(scale=2.4e38), -1), (dict(row_stride=99), -2), (dict(logits=None), -1), (dict(tokens=None), -1),
     (dict(logprobs=None), -1), (dict(top_ids=None), -1), (dict(top_logprobs=None), -1), (dict(logits=P + 2), -1), (dict(dtype=1, logits=P + 1), -1), (dict(n=200000, row_stride=200000), -1)])
 def test_logprob_refusals(change, code):
     refused(exe.exe_op_logprobs, LOGPROBS, code, **change)
