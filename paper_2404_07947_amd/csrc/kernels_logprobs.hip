@@ -62,17 +62,24 @@ __device__ __forceinline__ void sums_to(Sums& p, float M, float c)
     p.M = M;
 }
 
+// The given token of this thread, asked for early, and its logit, which is on its way while others are sorted: two trips to memory.
+__device__ __forceinline__ unsigned given_token(const LogprobKernelArgs& a, int64_t row)
+{
+    return a.parts == 1 && (int)threadIdx.x < a.n_tokens ? (unsigned)a.tokens[row * a.n_tokens + threadIdx.x] : 0xffffffffu;
+}
+template <typename T> __device__ __forceinline__ float given_logit(const LogprobKernelArgs& a, int64_t row, unsigned token)
+{
+    return token < a.n ? to_f32(((const T*)a.logits + row * a.row_stride)[token]) : NAN;
+}
 // The results of a row, by a workgroup: sums, and the k best keys in LDS (0: there are fewer).
-template <typename T, int THREADS> __device__ __forceinline__ void logprob_finish(const LogprobKernelArgs& a, int64_t row, Sums t, const u64* top)
+template <typename T, int THREADS> __device__ __forceinline__ void logprob_finish(const LogprobKernelArgs& a, int64_t row, Sums t, const u64* top, float given)
 {
     const float L = log2f(t.S) * LN2;
     // in 64 bits: the logits may lie further apart than the largest float
     auto logprob = [&](float x) { return (float)(((double)x - (double)t.M) * (double)a.scale - (double)L); };
-    const T* x = (const T*)a.logits + row * a.row_stride;
-    for (int i = threadIdx.x; i < a.n_tokens; i += THREADS) {
-        const unsigned tok = (unsigned)a.tokens[row * a.n_tokens + i];
-        a.logprobs[row * a.n_tokens + i] = tok < a.n ? logprob(to_f32(x[tok])) : NAN;
-    }
+    if ((int)threadIdx.x < a.n_tokens) a.logprobs[row * a.n_tokens + threadIdx.x] = logprob(given);
+    for (int i = threadIdx.x + THREADS; i < a.n_tokens; i += THREADS)
+        a.logprobs[row * a.n_tokens + i] = logprob(given_logit<T>(a, row, (unsigned)a.tokens[row * a.n_tokens + i]));
     if (a.entropy && threadIdx.x == 0) a.entropy[row] = L - t.Y / t.S * LN2;
     if ((int)threadIdx.x < a.k) {
         const u64 key = top[threadIdx.x];
@@ -177,7 +184,8 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
     constexpr int N = Part::N, WAVES = THREADS / WAVE, V = Part::V;
     constexpr bool SOME = Part::SOME;
     __shared__ u64 s_keys[LP_CAP], s_top[WAVE];
-    __shared__ Sums s_sums[WAVES];
+    __shared__ Sums s_sums[WAVES], s_row;
+    __shared__ float s_given[THREADS];
     __shared__ __align__(16) float s_best[THREADS];
     __shared__ int s_count, s_digit, s_counts[256];
     static_assert(THREADS % 256 == 0 && WAVES <= WAVE && Part::SPAN <= 1 << 16, "a count for each digit; a lane for each wave; 16 bits of a place");
@@ -189,6 +197,7 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
     Part p;
     // chunks of which this wave has something
     const int there = (int)(end - first) - __builtin_amdgcn_readfirstlane(wave) * (WAVE * V), chunks = there > 0 ? (there + THREADS * V - 1) / (THREADS * V) : 0;
+    const unsigned token = given_token(a, row);
     p.load(x, first, end, a.n, chunks);
     if (tid == 0) s_count = 0;
 
@@ -240,14 +249,18 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
     if (lane == 0) s_sums[wave] = Sums{most, S, Y};
     s_best[tid] = best;
     __syncthreads();
-    Sums t{-INFINITY, 0.f, 0.f};
-    if (wave == 0 || a.parts == 1) {
+    const float given = given_logit<T>(a, row, token);
+    auto join_waves = [&]() {                                  // by the last one, which has no part in the sorting
+        if (wave != WAVES - 1) return;
         Sums p = lane < WAVES ? s_sums[lane] : Sums{-INFINITY, 0.f, 0.f};
-        t.M = lanes_max(p.M);
-        sums_to(p, t.M, a.c);
-        t.S = wave_sum(p.S);
-        t.Y = wave_sum(p.Y);
-    }
+        const float M = lanes_max(p.M);
+        sums_to(p, M, a.c);
+        const float S = wave_sum(p.S), Y = wave_sum(p.Y);
+        if (lane == 0) {
+            if (a.parts > 1) *(f32x4*)(a.sums + (int64_t)blockIdx.x * 4) = f32x4{M, S, Y, 0.f};
+            else s_row = Sums{M, S, Y};
+        }
+    };
     if (a.k) {
         // k logits or more are no smaller than the k-th largest of the threads' best ones, of which the largest of each 64th of them will do where k is small:
         // these take part in a search for its upper 16 bits, a number no larger.
@@ -272,26 +285,27 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
                 if (n >= a.k) kth |= bit;
             }
         }
+        s_given[tid] = given;                                  // (a register to spare)
         p.renew();
         float least = order_logit(kth);
         least = least >= -3.4028235e38f ? least : -3.4028235e38f;              // those of -inf are ruled out; not a number: fewer than k
-        unsigned have[(N + 31) / 32] = {};                     // a bit for each
+        // One of each lane that has some at a time, in any order: they are sorted.
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             if (!__builtin_amdgcn_ballot_w64(tops[c] >= least)) continue;
+            unsigned have = 0;                                 // a bit for each
 #pragma unroll
-            for (int i = c * V; i < (c + 1) * V; ++i) have[i / 32] |= p.at(i) >= least ? 1u << i % 32 : 0u;
-        }
-        // One of each lane that has some at a time, in any order: they are sorted.  From memory again: a branch for each register would cost more.
-#pragma unroll
-        for (int w = 0; w < (N + 31) / 32; ++w) {
-            for (u64 some; (some = __builtin_amdgcn_ballot_w64(have[w] != 0)); have[w] &= have[w] - 1) {
+            for (int e = 0; e < V; ++e) have |= p.at(c * V + e) >= least ? 1u << e : 0u;
+            for (u64 some; (some = __builtin_amdgcn_ballot_w64(have != 0)); have &= have - 1) {
                 int at = 0;
                 if (lane == 0) at = atomicAdd(&s_count, __popcll(some));
                 at = __builtin_amdgcn_readfirstlane(at) + __builtin_amdgcn_mbcnt_hi((unsigned)(some >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)some, 0));
-                if (have[w] && at < LP_CAP) {
-                    const unsigned i = first + Part::place(w * 32 + __builtin_ctz(have[w]));
-                    s_keys[at] = logit_key(logit_order(to_f32(x[i])), i);
+                if (have && at < LP_CAP) {
+                    const int e = __builtin_ctz(have);
+                    float v = p.at(c * V);
+#pragma unroll
+                    for (int o = 1; o < V; ++o) v = e == o ? p.at(c * V + o) : v;
+                    s_keys[at] = logit_key(logit_order(v), first + Part::place(c * V) + e);
                 }
             }
         }
@@ -333,6 +347,7 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
             __syncthreads();
             count = a.k;
         }
+        join_waves();
         if (a.parts > 1) {
             sort_keys(s_keys, count, a.lists + (int64_t)blockIdx.x * a.k, a.k);
         } else {
@@ -340,11 +355,13 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
             __syncthreads();
         }
     }
-    if (a.parts > 1) {
-        if (tid == 0) *(f32x4*)(a.sums + (int64_t)blockIdx.x * 4) = f32x4{t.M, t.S, t.Y, 0.f};
-    } else {
-        logprob_finish<T, THREADS>(a, row, t, s_top);
+    if (!a.k) {
+        s_given[tid] = given;
+        join_waves();
+        __syncthreads();
     }
+    if (a.parts > 1) return;
+    logprob_finish<T, THREADS>(a, row, s_row, s_top, s_given[tid]);
 }
 
 // Lists i of up to 64, sorted, each of k keys: the k best of them all.  What the m-th of every list (k of them or more together) and the k-th of
@@ -360,6 +377,7 @@ template <typename T> __global__ __launch_bounds__(LP_JOIN_THREADS) void logprob
     const unsigned part = blockIdx.x - (unsigned)row * a.parts;
     const int lists = a.from_parts - part * LP_JOIN < LP_JOIN ? a.from_parts - part * LP_JOIN : LP_JOIN;
     const int64_t from = row * a.from_parts + part * LP_JOIN;
+    const float given = given_logit<T>(a, row, given_token(a, row));
     f32x4 s = {-INFINITY, 0.f, 0.f, 0.f};
     if (lane < lists) s = *(const f32x4*)(a.from_sums + (from + lane) * 4);
     if (a.k) {
@@ -413,7 +431,7 @@ template <typename T> __global__ __launch_bounds__(LP_JOIN_THREADS) void logprob
     if (a.parts > 1) {
         if (tid == 0) *(f32x4*)(a.sums + (int64_t)blockIdx.x * 4) = f32x4{t.M, t.S, t.Y, 0.f};
     } else {
-        logprob_finish<T, LP_JOIN_THREADS>(a, row, t, s_top);
+        logprob_finish<T, LP_JOIN_THREADS>(a, row, t, s_top, given);
     }
 }
 
