@@ -1,4 +1,5 @@
-// Log probabilities of given tokens, entropy and the largest probabilities, of rows of logits.
+// Log probabilities of given tokens, entropy and the largest probabilities, of rows of logits.  Rows of 50272, a call: 1 float 7.0 us, of which a CU needs 1.3 to take
+// 200 KB in and 2.6 for their exponentials, 256 float 12.5 (4.1 TB/s), 2048 bf16 43 (4.8 TB/s; vector instructions, exponentials a half of them).
 //
 // With the largest logit M and c = scale * log2 e: z = (x - M) * c, S = sum of 2^z, Y = sum of 2^z z; then log p = (z - log2 S) ln 2 and the
 // entropy is (log2 S - Y / S) ln 2.
@@ -100,7 +101,9 @@ template <int C, bool SOME, int I = 0, typename F> __device__ __forceinline__ vo
 }
 
 template <typename T, int THREADS, int C> struct LogitPart {
-    static constexpr bool SOME = THREADS > 256;              // else all chunks are in use
+    // Few chunks: all are in use.  Many, in float: a wave that has all of them, or all but one, of a row that begins on 16 bytes makes the sums of the first ones
+    // while the others are on their way (a row a CU of 256 of 50272 13.4 -> 12.5 us a call, one row 7.3 -> 7.0; in thirds the same).
+    static constexpr bool SOME = THREADS > 256, HALVES = THREADS > 256 && sizeof(T) == 4;
     static constexpr int V = 16 / (int)sizeof(T), N = C * V, SPAN = THREADS * N;
     uint4 raw[C];
     __device__ __forceinline__ float at(int i) const       // i: a constant after unrolling
@@ -120,13 +123,13 @@ template <typename T, int THREADS, int C> struct LogitPart {
     }
     // Logits first .. end - 1 of the row, the first on 16 bytes: up to V - 1 before the row's first one.  What is not of them is -inf.  All loads go
     // out before anything waits: those of chunks that are not there, or only in part, from the nearest whole one.
-    // Of the C chunks the first `chunks` are in use.
-    __device__ __forceinline__ void load(const T* x, unsigned first, unsigned end, unsigned n, int chunks)
+    // Of the C chunks the first `chunks` are in use (SOME), or all; LONG: there is a whole one for sure.  `fill` looks after those of chunks I .. J - 1 that are there in part or not at all.
+    template <bool SOME, bool LONG> __device__ __forceinline__ void load(const T* x, unsigned first, unsigned n, int chunks)
     {
         // whole chunks of the row: from its first or second one on, up to `high`, both counted from `first`
         const int lead = (int)((uintptr_t)x & 15) / (int)sizeof(T), low = first > n && lead ? V : 0;
         const int64_t at = first > n ? -(int64_t)lead : (int64_t)first, high = at + ((int64_t)n - at) / V * V - V - at;
-        if (high >= low) {
+        if (LONG || high >= low) {
             const char* base = (const char*)(x + at);
             const int most = high < SPAN ? (int)high : SPAN;
             each_chunk<C, SOME>(chunks, [&](auto c) {
@@ -135,8 +138,11 @@ template <typename T, int THREADS, int C> struct LogitPart {
                 raw[c] = load_chunk<true>((const uint4*)(base + (unsigned)(i * (int)sizeof(T))));
             });
         }
+    }
+    template <bool SOME, int I, int J> __device__ __forceinline__ void fill(const T* x, unsigned first, unsigned end, int chunks)
+    {
         if (first < end && end - first >= SPAN) return;        // all of them whole
-        each_chunk<C, SOME>(chunks, [&](auto c) {
+        each_chunk<J, SOME, I>(chunks, [&](auto c) {
             const unsigned i = first + place(c * V);
             if (i < end && end - i >= V) return;
             if ((int)(end - i) <= 0) {                         // nothing of it
@@ -181,8 +187,7 @@ __device__ __forceinline__ void sort_keys(const u64* keys, int count, u64* top, 
 template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, THREADS == 1024 && sizeof(T) == 2 ? 8 : 1) void logprob_part_kernel(LogprobKernelArgs a)
 {
     typedef LogitPart<T, THREADS, C> Part;
-    constexpr int N = Part::N, WAVES = THREADS / WAVE, V = Part::V;
-    constexpr bool SOME = Part::SOME;
+    constexpr int WAVES = THREADS / WAVE, V = Part::V;
     __shared__ u64 s_keys[LP_CAP], s_top[WAVE];
     __shared__ Sums s_sums[WAVES], s_row;
     __shared__ float s_given[THREADS];
@@ -198,51 +203,86 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
     // chunks of which this wave has something
     const int there = (int)(end - first) - __builtin_amdgcn_readfirstlane(wave) * (WAVE * V), chunks = there > 0 ? (there + THREADS * V - 1) / (THREADS * V) : 0;
     const unsigned token = given_token(a, row);
-    p.load(x, first, end, a.n, chunks);
     if (tid == 0) s_count = 0;
 
     float tops[C], best = -INFINITY;                           // of a chunk; of all
-    bool none = false;
 #pragma unroll
     for (int c = 0; c < C; ++c) tops[c] = -INFINITY;
-    each_chunk<C, SOME>(chunks, [&](auto c) {
-        const int i = c * V;
-        tops[c] = max3(p.at(i), p.at(i + 1), p.at(i + 2));
-        if constexpr (V == 8) tops[c] = max3(max3(tops[c], p.at(i + 3), p.at(i + 4)), p.at(i + 5), p.at(i + 6));
-        tops[c] = max3(tops[c], tops[c], p.at(i + V - 1));
-        none |= tops[c] != tops[c];
-    });
-    if (none) {                                                // all of a chunk NaN, or signalling ones, which that instruction hands on
-        each_chunk<C, SOME>(chunks, [&](auto c) {
-            tops[c] = -INFINITY;
-#pragma unroll
-            for (int i = c * V; i < (c + 1) * V; ++i) tops[c] = p.at(i) > tops[c] ? p.at(i) : tops[c];
+    // Sums of chunks I .. J - 1, about the wave's largest of them, or (HALVES) this lane's
+    auto sum_chunks = [&](auto some, auto from, auto to) {
+        constexpr bool SOME = some;
+        constexpr int I = from, J = to;
+        if constexpr (SOME == Part::SOME) {
+            p.template fill<SOME, I, J>(x, first, end, chunks);
+        } else if constexpr (J == C) {
+            p.template fill<SOME, C - 2, C>(x, first, end, chunks);
+        }
+        bool none = false;
+        each_chunk<J, SOME, I>(chunks, [&](auto c) {
+            const int i = c * V;
+            tops[c] = max3(p.at(i), p.at(i + 1), p.at(i + 2));
+            if constexpr (V == 8) tops[c] = max3(max3(tops[c], p.at(i + 3), p.at(i + 4)), p.at(i + 5), p.at(i + 6));
+            tops[c] = max3(tops[c], tops[c], p.at(i + V - 1));
+            none |= tops[c] != tops[c];
         });
-    }
+        if (none) {                                            // all of a chunk NaN, or signalling ones, which that instruction hands on
+            each_chunk<J, SOME, I>(chunks, [&](auto c) {
+                tops[c] = -INFINITY;
 #pragma unroll
-    for (int c = 0; c < C; ++c) best = fmaxf(best, tops[c]);
-    if constexpr (N > 32) p.renew();
-    const float most = lanes_max(best), R = most == -INFINITY ? 0.f : most * a.c;
-    float S = 0.f, Y = 0.f;
-    auto add = [&](float z) {
-        const float e = fast_exp2(z);
-        S += e;
-        Y = fmaf(e, fmaxf(z, -1e30f), Y);                      // 0 times minus infinity is 0 here; what is NaN is so in e
+                for (int i = c * V; i < (c + 1) * V; ++i) tops[c] = p.at(i) > tops[c] ? p.at(i) : tops[c];
+            });
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int c = I; c < J; ++c) most = fmaxf(most, tops[c]);
+        best = fmaxf(best, most);
+        if constexpr (!Part::HALVES) most = lanes_max(most);
+        if constexpr ((J - I) * V > 32) p.renew();
+        const float R = most == -INFINITY ? 0.f : most * a.c;
+        float S = 0.f, Y = 0.f;
+        auto add = [&](float z) {
+            const float e = fast_exp2(z);
+            S += e;
+            Y = fmaf(e, fmaxf(z, -1e30f), Y);                  // 0 times minus infinity is 0 here; what is NaN is so in e
+        };
+        if (!__builtin_amdgcn_ballot_w64(!(fabsf(R) < 0x1p20f))) {
+            // One operation a logit: z + off = c * x - R, where off = c * M - R, what R was rounded by, is 1/16 at most, and taken out of the sums.
+            each_chunk<J, SOME, I>(chunks, [&](auto c) {
+#pragma unroll
+                for (int i = c * V; i < (c + 1) * V; ++i) add(fmaf(p.at(i), a.c, -R));
+            });
+            const float off = most == -INFINITY ? 0.f : fmaf(most, a.c, -R), w = fast_exp2(-off);
+            Y = (Y - off * S) * w;
+            S *= w;
+        } else {
+            each_chunk<J, SOME, I>(chunks, [&](auto c) {
+#pragma unroll
+                for (int i = c * V; i < (c + 1) * V; ++i) add((p.at(i) - (most == -INFINITY ? 0.f : most)) * a.c);
+            });
+        }
+        return Sums{most, S, Y};
     };
-    if (fabsf(R) < 0x1p20f) {
-        // One operation a logit: z + off = c * x - R, where off = c * M - R, what R was rounded by, is 1/16 at most, and taken out of the sums.
-        each_chunk<C, SOME>(chunks, [&](auto c) {
-#pragma unroll
-            for (int i = c * V; i < (c + 1) * V; ++i) add(fmaf(p.at(i), a.c, -R));
-        });
-        const float off = most == -INFINITY ? 0.f : fmaf(most, a.c, -R), w = fast_exp2(-off);
-        Y = (Y - off * S) * w;
-        S *= w;
+    constexpr auto zero = std::integral_constant<int, 0>{};
+    constexpr auto all = std::integral_constant<int, C>{};
+    float S, Y, most;
+    auto join_lanes = [&](Sums q) {
+        if constexpr (Part::HALVES) sums_to(q, most, a.c);
+        S += q.S;
+        Y += q.Y;
+    };
+    S = Y = 0.f;
+    if (Part::HALVES && chunks >= C - 1 && first == 0) {
+        constexpr auto half = std::integral_constant<int, C / 2>{};
+        p.template load<false, true>(x, first, a.n, chunks);
+        const Sums q = sum_chunks(std::false_type{}, zero, half), r = sum_chunks(std::false_type{}, half, all);
+        most = lanes_max(best);
+        join_lanes(q);
+        join_lanes(r);
     } else {
-        each_chunk<C, SOME>(chunks, [&](auto c) {
-#pragma unroll
-            for (int i = c * V; i < (c + 1) * V; ++i) add((p.at(i) - most) * a.c);
-        });
+        p.template load<Part::SOME, false>(x, first, a.n, chunks);
+        const Sums q = sum_chunks(std::bool_constant<Part::SOME>{}, zero, all);
+        most = Part::HALVES ? lanes_max(best) : q.M;
+        join_lanes(q);
     }
     S = wave_sum(S);
     Y = wave_sum(Y);
