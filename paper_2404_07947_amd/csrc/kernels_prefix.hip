@@ -15,6 +15,21 @@ namespace exe {
 constexpr int PX_STEP = 16, PX_PARTS = WAVE;
 constexpr float NO_PART = -2.f, NO_KEYS = -1.f;       // in place of a sum of probabilities: a part that is not there, a row without keys
 
+// n / d for 0 <= n < 2^31 as (n + the upper half of n * mul) >> shift, where 2^shift is the first power of two from d on and mul is 2^32 (2^shift - d) / d, rounded
+// up: 2^32 + mul = 2^(32 + shift) / d + e with e <= 1, and n e < 2^31 cannot reach the next whole number.  A division by a number that is not known takes 20 to 30
+// instructions, one after the other, and a workgroup here begins with three of them (us a call, before and now: 12 groups 45.1, 44.1, float groups 11.6, 11.3).
+struct Divisor {
+    unsigned d, mul, shift;
+    static Divisor of(int64_t d)
+    {
+        unsigned s = 0;
+        while ((1ll << s) < d) ++s;
+        return Divisor{(unsigned)d, (unsigned)(((uint64_t)((1ll << s) - d) << 32) / d + 1), s};
+    }
+    __device__ __forceinline__ int quotient(int n) const { return (int)((__umulhi(mul, (unsigned)n) + (unsigned)n) >> shift); }
+    __device__ __forceinline__ int rest(int n, int q) const { return n - q * (int)d; }
+};
+
 struct PrefixKernelArgs {
     const int32_t *cu, *len, *cu_groups, *prefix;
     int n_seqs, tokens, n_groups;
@@ -31,6 +46,7 @@ struct PrefixKernelArgs {
     static constexpr int window = 0;
     int slots, own_tiles;             // of prefix tiles; tiles of a sequence's rows side by side
     unsigned shared_units, own_units; // workgroups of each kind
+    Divisor by_G, by_Hkv, by_parts, by_tiles, by_units, by_quarter;   // G, Hkv; own.parts, own_tiles; workgroups of a slot of tiles; of a token in the join
 };
 
 // A group: sequences b0 .. b1 - 1, new tokens t0 .. t1 - 1, and the positions that they share.  Those in front of every new token of the group
@@ -38,12 +54,14 @@ struct PrefixKernelArgs {
 struct PrefixGroup { int g, b0, b1, t0, t1, prefix; };
 __device__ __forceinline__ int lanes_min(int v)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const int w = __shfl_xor(v, o, WAVE);
-        v = w < v ? w : v;
-    }
-    return v;
+    auto with = [&](int w) { v = w < v ? w : v; };
+    with(dpp_move_int<0xB1>(v));
+    with(dpp_move_int<0x4E>(v));
+    with(dpp_move_int<0x141>(v));
+    with(dpp_move_int<0x140>(v));
+    const int a = __builtin_amdgcn_readlane(v, 0), b = __builtin_amdgcn_readlane(v, 16), c = __builtin_amdgcn_readlane(v, 32), d = __builtin_amdgcn_readlane(v, 48);
+    const int ab = a < b ? a : b, cd = c < d ? c : d;
+    return ab < cd ? ab : cd;
 }
 // The group of tile slot `at` (those of group g begin at floor(first token * G / rows of a tile) + g, see ChunkTile), or of sequence `at`.
 template <bool SLOT> __device__ __forceinline__ PrefixGroup find_group(const PrefixKernelArgs& a, int at, int tile_shift, int lane)
@@ -128,7 +146,7 @@ template <typename T, int DH> __device__ __forceinline__ void prefix_row(const P
 }
 
 // Query rows r0 .. r1 - 1 of a run of packed tokens from t0 on (row r: token t0 + r / G, head kvh * G + r % G) against keys k of table row b; row
-// r sees keys lo .. hi(r) - 1 of them.  Every wave takes steps of 16 keys of its own through a ring of stages in LDS, as chunk_stream_kernel does,
+// r sees keys lo .. hi(r / G) - 1 of them.  Every wave takes steps of 16 keys of its own through a ring of stages in LDS, as chunk_stream_kernel does,
 // with QB blocks of 16 rows: S^T = K . Q^T, O^T += V^T . P^T.  The result goes to part `part`.
 // WHOLE: behind the keys 0 .. lo - 1 of table row b0, which all rows see, and to the results themselves; again: computes a row once more.
 template <typename T, int DH, int QB, int WAVES, bool NT, bool WHOLE, typename F, typename R>
@@ -148,11 +166,11 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
     int last[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-        const int r = r0 + qb * 16 + qi, row = r < r1 ? r : r1 - 1, t = t0 + row / G;
-        last[qb] = hi(row);
-        load_query<T, DS>((const T*)a.q + (int64_t)(t >= 0 && t < a.tokens ? t : 0) * a.q_stride + (kvh * G + row % G) * DH, g, a.scale, qf[qb]);
+        const int r = r0 + qb * 16 + qi, row = r < r1 ? r : r1 - 1, at = a.by_G.quotient(row), t = t0 + at;
+        last[qb] = hi(at);
+        load_query<T, DS>((const T*)a.q + (int64_t)(t >= 0 && t < a.tokens ? t : 0) * a.q_stride + (kvh * G + a.by_G.rest(row, at)) * DH, g, a.scale, qf[qb]);
     }
-    const int least = hi(r0);                                            // the first row sees the fewest
+    const int least = hi(a.by_G.quotient(r0));                                            // the first row sees the fewest
     const int shared = WHOLE ? (lo + PX_STEP - 1) / PX_STEP : 0;             // steps in front
     const int steps = shared + (k.last > k.first ? (k.last - k.first + PX_STEP - 1) / PX_STEP : 0), own = steps > wave ? (steps - wave + WAVES - 1) / WAVES : 0;
     typedef RowLoader<T, DH, NT> Loader;
@@ -304,7 +322,7 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
         // 16 threads a row, features 4 * c .. +3 of every 64
 #pragma unroll
         for (int r = tid >> 4; r < 16; r += WAVES * 4) {                 // beyond 4 waves: nothing to do
-            const int c = tid & 15, row = r0 + qb * 16 + r, t = t0 + row / G;
+            const int c = tid & 15, row = r0 + qb * 16 + r, token = a.by_G.quotient(row), t = t0 + token, h = kvh * G + a.by_G.rest(row, token);
             float M = -INFINITY, L = 0.f, w[WAVES];
 #pragma unroll
             for (int i = 0; i < WAVES; ++i) M = fmaxf(M, s_ml[i][r][0]);
@@ -318,7 +336,8 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
             if constexpr (WHOLE) {
                 f32x4 v[DH / 64];
                 float most = 0.f;
-                const bool any = hi(row < r1 ? row : r1 - 1) > 0;
+                const float inv = 1.f / L;
+                const bool any = hi(token) > 0;
 #pragma unroll
                 for (int f = 0; f < DH / 64; ++f) {
                     v[f] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -326,7 +345,7 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
                     for (int i = 0; i < WAVES; ++i) v[f] += *(const f32x4*)(s_o + (i * 16 + r) * (DH + 4) + f * 64 + 4 * c) * w[i];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        v[f][e] = any ? v[f][e] / L : 0.f;
+                        v[f][e] = any ? v[f][e] * inv : 0.f;
                         most = magnitude(most, v[f][e]);
                     }
                 }
@@ -337,7 +356,7 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
                         typename Vec4<T>::type y;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) y[e] = from_f32<T>(v[f][e]);
-                        *(typename Vec4<T>::type*)((T*)a.out + (int64_t)t * a.out_stride + (kvh * G + row % G) * DH + f * 64 + 4 * c) = y;
+                        *(typename Vec4<T>::type*)((T*)a.out + (int64_t)t * a.out_stride + h * DH + f * 64 + 4 * c) = y;
                     }
                 }
                 for (int i = 0; i < 4; ++i)                              // the four rows of this wave
@@ -345,7 +364,7 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
                 continue;
             }
             if (!write) continue;
-            const int64_t at = ((int64_t)part * a.tokens + t) * a.H + kvh * G + row % G;
+            const int64_t at = ((int64_t)part * a.tokens + t) * a.H + h;
 #pragma unroll
             for (int f = 0; f < DH / 64; ++f) {
                 f32x4 v = {0.f, 0.f, 0.f, 0.f};
@@ -353,7 +372,7 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
                 for (int i = 0; i < WAVES; ++i) v += *(const f32x4*)(s_o + (i * 16 + r) * (DH + 4) + f * 64 + 4 * c) * w[i];
                 *(f32x4*)(a.tile.acc + at * DH + f * 64 + 4 * c) = v;
             }
-            if (c == 0) *(float2*)(a.tile.ml + at * 2) = float2{M, hi(row) > lo ? L : NO_KEYS};
+            if (c == 0) *(float2*)(a.tile.ml + at * 2) = float2{M, hi(token) > lo ? L : NO_KEYS};
         }
     }
     __syncthreads();                                                     // before the next tile's loads overwrite the results
@@ -361,9 +380,9 @@ __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned 
 // The same rows where there is no such part.
 __device__ __forceinline__ void no_part(const PrefixKernelArgs& a, int kvh, int t0, int r0, int r1, int part)
 {
-    const int row = r0 + threadIdx.x, t = t0 + row / a.G;
+    const int row = r0 + threadIdx.x, at = a.by_G.quotient(row), t = t0 + at;
     if (row < r1 && t >= 0 && t < a.tokens)
-        *(float2*)(a.tile.ml + (((int64_t)part * a.tokens + t) * a.H + kvh * a.G + row % a.G) * 2) = float2{-INFINITY, NO_PART};
+        *(float2*)(a.tile.ml + (((int64_t)part * a.tokens + t) * a.H + kvh * a.G + a.by_G.rest(row, at)) * 2) = float2{-INFINITY, NO_PART};
 }
 
 // Tile of the prefix for workgroup wg: of tiles with 2^SHIFT rows, those that read the same keys follow each other on one XCD.  b = -1: there is
@@ -373,14 +392,14 @@ template <int SHIFT> __device__ __forceinline__ PrefixTile find_prefix(const Pre
 {
     PrefixTile r;
     r.tile.b = -1;
-    const unsigned units = (a.Hkv * a.shared.parts + 7) & ~7, slot = wg / units, u = wg - slot * units;
-    if (u >= (unsigned)(a.Hkv * a.shared.parts)) return r;
-    const int kvh = u % a.Hkv;
-    r.part = u / a.Hkv;
+    const int slot = a.by_units.quotient(wg), u = a.by_units.rest(wg, slot);
+    if (u >= a.Hkv * a.shared.parts) return r;
+    r.part = a.by_Hkv.quotient(u);
+    const int kvh = a.by_Hkv.rest(u, r.part);
     const PrefixGroup gr = find_group<true>(a, slot, SHIFT, lane);
     if (gr.g < 0) return r;
     const int n = gr.t1 - gr.t0 < a.tokens ? gr.t1 - gr.t0 : a.tokens, rows = n * a.G;
-    const int r0 = (int)(slot - (unsigned)((int)((int64_t)gr.t0 * a.G >> SHIFT) + gr.g)) << SHIFT;
+    const int r0 = (slot - ((int)((int64_t)gr.t0 * a.G >> SHIFT) + gr.g)) << SHIFT;
     if (n <= 0 || r0 >= rows) return r;
     r.r1 = r0 + (1 << SHIFT) < rows ? r0 + (1 << SHIFT) : rows;
     const int end = gr.prefix < limit ? gr.prefix : limit;
@@ -397,15 +416,16 @@ template <int SHIFT> __device__ __forceinline__ PrefixTile find_prefix(const Pre
 // A sequence's own positions, by workgroup wg of those.
 template <typename T, int DH, int WAVES> __device__ __forceinline__ void own_rows(const PrefixKernelArgs& a, unsigned char* smem, unsigned wg, int limit, int lane)
 {
-    const int G = a.G, part = wg % a.own.parts, tile = wg / a.own.parts % a.own_tiles, head = wg / a.own.parts / a.own_tiles, kvh = head % a.Hkv, b = head / a.Hkv;
+    const int G = a.G, u = a.by_parts.quotient(wg), part = a.by_parts.rest(wg, u), head = a.by_tiles.quotient(u), tile = a.by_tiles.rest(u, head), b = a.by_Hkv.quotient(head),
+              kvh = a.by_Hkv.rest(head, b);
     const int t0 = a.cu[b], end = a.cu[b + 1], p_end = a.len[b], n = end - t0 < a.tokens ? end - t0 : a.tokens, p0 = p_end - n;
     const PrefixGroup gr = find_group<false>(a, b, 0, lane);
     if (n <= 0) return;
     const int lo = gr.prefix < limit ? gr.prefix : limit;
-    auto hi = [&](int row) { return keys_of(p0 + row / G, 0, limit).last; };
+    auto hi = [&](int token) { return keys_of(p0 + token, 0, limit).last; };
     for (int r0 = tile * 16; r0 < n * G; r0 += a.own_tiles * 16) {
         const int r1 = r0 + 16 < n * G ? r0 + 16 : n * G;
-        const KeyRange all{lo & -PX_STEP, hi(r1 - 1)};
+        const KeyRange all{lo & -PX_STEP, hi(a.by_G.quotient(r1 - 1))};
         const int parts = parts_of(all, a.own);
         if (part >= parts) no_part(a, kvh, t0, r0, r1, a.shared.parts + part);
         else stream_rows<T, DH, 1, WAVES, true, false>(a, smem, b, b, kvh, t0, r0, r1, part_of(all, a.own, part, parts), lo, hi, a.shared.parts + part, [](int) {});
@@ -429,16 +449,17 @@ template <typename T, int DH, int QB, int WAVES> __global__ __launch_bounds__(WA
 template <typename T, int DH, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void prefix_whole_kernel(PrefixKernelArgs a)
 {
     extern __shared__ __align__(16) unsigned char px_smem[];
-    const int lane = threadIdx.x & 63, limit = table_limit(a.table), G = a.G, tile = blockIdx.x % a.own_tiles, head = blockIdx.x / a.own_tiles, kvh = head % a.Hkv, b = head / a.Hkv;
+    const int lane = threadIdx.x & 63, limit = table_limit(a.table), G = a.G, head = a.by_tiles.quotient(blockIdx.x), tile = a.by_tiles.rest(blockIdx.x, head), b = a.by_Hkv.quotient(head),
+              kvh = a.by_Hkv.rest(head, b);
     const int t0 = a.cu[b], end = a.cu[b + 1], p_end = a.len[b], n = end - t0 < a.tokens ? end - t0 : a.tokens, p0 = p_end - n;
     const PrefixGroup gr = find_group<false>(a, b, 0, lane);
     if (n <= 0) return;
     const int lo = gr.prefix < limit ? gr.prefix : limit;
-    auto hi = [&](int row) { return keys_of(p0 + row / G, 0, limit).last; };
+    auto hi = [&](int token) { return keys_of(p0 + token, 0, limit).last; };
     auto again = [&](int row) { prefix_row<T, DH>(a, gr, b, p0 + row / G, t0 + row / G, kvh * G + row % G, lane); };
     for (int r0 = tile * 16; r0 < n * G; r0 += a.own_tiles * 16) {
         const int r1 = r0 + 16 < n * G ? r0 + 16 : n * G;
-        stream_rows<T, DH, 1, WAVES, false, true>(a, px_smem, gr.g < 0 || !lo ? b : gr.b0, b, kvh, t0, r0, r1, KeyRange{lo & -PX_STEP, hi(r1 - 1)}, lo, hi, 0, again);
+        stream_rows<T, DH, 1, WAVES, false, true>(a, px_smem, gr.g < 0 || !lo ? b : gr.b0, b, kvh, t0, r0, r1, KeyRange{lo & -PX_STEP, hi(a.by_G.quotient(r1 - 1))}, lo, hi, 0, again);
     }
 }
 // More rows, in tiles of 128, in front of own positions.  Bound by MFMAs and softmax, as chunk_tile_kernel is: 64 sequences and 96 tokens of 32 heads over 8 x 128 on
@@ -458,8 +479,8 @@ template <typename T, int DH> __global__ __launch_bounds__(CT_WAVES * 64, 2) voi
 template <typename T, int DH> __global__ __launch_bounds__(256) void prefix_join_kernel(PrefixKernelArgs a)
 {
     constexpr int PER = DH / 4, SUBS = 64 / PER;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = (a.H + 3) / 4;
-    const int t = blockIdx.x / quarter, h = (blockIdx.x - t * quarter) * 4 + wave;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int t = a.by_quarter.quotient(blockIdx.x), h = a.by_quarter.rest(blockIdx.x, t) * 4 + wave;
     if (h >= a.H) return;
     const int parts = a.shared.parts + a.own.parts, sub = lane / PER, f = lane % PER * 4;
     const int64_t at = (int64_t)t * a.H + h, step = (int64_t)a.tokens * a.H;
@@ -603,6 +624,9 @@ template <typename T, int DH> static hipError_t launch_prefix(const PrefixAttnAr
     k.tile = {rows, a.workspace, a.workspace + (size_t)(p.shared.parts + p.own.parts) * rows * DH};
     k.slots = (int)p.slots; k.own_tiles = p.own_tiles;
     k.shared_units = (unsigned)p.shared_units; k.own_units = (unsigned)p.own_units;
+    k.by_G = Divisor::of(k.G); k.by_Hkv = Divisor::of(k.Hkv);
+    k.by_parts = Divisor::of(std::max(p.own.parts, 1)); k.by_tiles = Divisor::of(p.own_tiles);
+    k.by_units = Divisor::of(std::max<int64_t>(8, ceil_div((int64_t)k.Hkv * p.shared.parts, 8) * 8)); k.by_quarter = Divisor::of(ceil_div(a.H, 4));
     hipError_t e;
     if (p.whole) {
         if constexpr (sizeof(T) == 4 && DH == 128) return launch_whole<T, DH, 4>(k, wgs, s);
