@@ -494,8 +494,8 @@ uint64_t exe_op_chunk_attention_paged_workspace(int32_t dtype, int32_t n_seqs, i
  * (exe_seq_fork), many questions on one document, a system prompt in front of all.  Each group's prefix is read once, for all of its rows.
  * Group g are sequences cu_groups[g] .. cu_groups[g + 1] - 1 (cu_groups [n_groups + 1], device, from 0, not falling, up to n_seqs; a group may be empty
  * or of one, sequences behind the last group share nothing), whose first prefix[g] (device) positions hold the same keys and values.  Of these the ones in front of
- * every new token of the group are read through the block table of the group's first sequence, so the other sequences' entries for blocks that lie
- * in the prefix are not looked at; the positions behind are each sequence's own, as is all that prefix[g] names beyond the shortest context of its group, or
+ * every new token of the group are read through the block table of the group's first sequence with new tokens, so the other sequences' entries for blocks that
+ * lie in the prefix are not looked at (nor anything of a sequence without new tokens: a continuation that has ended may stay in its group); the positions behind are each sequence's own, as is all that prefix[g] names beyond the shortest context of its group, or
  * below 0.  A prefix may end inside a block: the sequences then have blocks of their own there, as forks have.
  * max_new (new tokens of a sequence), max_group (new tokens of a group), max_prefix and max_own (a sequence's positions behind its prefix, the new ones
  * among them) size the launch and the workspace; where they are wrong, it is slower, not wrong.  Probabilities have 16 bits in the product with bf16

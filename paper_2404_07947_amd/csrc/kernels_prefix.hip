@@ -50,8 +50,9 @@ struct PrefixKernelArgs {
 };
 
 // A group: sequences b0 .. b1 - 1, new tokens t0 .. t1 - 1, and the positions that they share.  Those in front of every new token of the group
-// count: what a call passes beyond is a sequence's own.  Group n_groups is what lies behind the last one, without a prefix.
-struct PrefixGroup { int g, b0, b1, t0, t1, prefix; };
+// count: what a call passes beyond is a sequence's own.  They are read through table row `front`, of the first sequence that has new tokens: nothing of one
+// without any is looked at, so a continuation that has ended may stay in its place.  Group n_groups is what lies behind the last one, without a prefix.
+struct PrefixGroup { int g, b0, b1, t0, t1, prefix, front; };
 __device__ __forceinline__ int lanes_min(int v)
 {
     auto with = [&](int w) { v = w < v ? w : v; };
@@ -79,13 +80,16 @@ template <bool SLOT> __device__ __forceinline__ PrefixGroup find_group(const Pre
         first = first < 0 ? 0 : first < a.n_seqs ? first : a.n_seqs;
         const int token = __shfl(c, first, WAVE), n = __shfl(c, lane + 1, WAVE) - c;
         r.g = __popcll(__builtin_amdgcn_ballot_w64(lane <= a.n_groups && before(first, token, lane))) - 1;
-        if (r.g < 0) return PrefixGroup{-1, 0, 0, 0, 0, 0};
+        if (r.g < 0) return PrefixGroup{-1, 0, 0, 0, 0, 0, 0};
         r.b0 = __builtin_amdgcn_readlane(first, r.g);
         r.b1 = __builtin_amdgcn_readlane(first, r.g + 1);
         r.t0 = __builtin_amdgcn_readlane(token, r.g);
         r.t1 = __builtin_amdgcn_readlane(token, r.g + 1);
         least = __builtin_amdgcn_readlane(shared, r.g);
-        const int p0 = lanes_min(lane >= r.b0 && lane < r.b1 && n > 0 ? l - n : 0x7fffffff);
+        const bool counts = lane >= r.b0 && lane < r.b1 && n > 0;
+        const unsigned long long some = __builtin_amdgcn_ballot_w64(counts);
+        r.front = some ? __builtin_ctzll(some) : r.b0;
+        const int p0 = lanes_min(counts ? l - n : 0x7fffffff);
         least = p0 < least ? p0 : least;
     } else {
         auto first_of = [&](int g) {
@@ -97,24 +101,30 @@ template <bool SLOT> __device__ __forceinline__ PrefixGroup find_group(const Pre
             return before(first, SLOT ? a.cu[first] : 0, g);
         });
         r.g = __builtin_amdgcn_readfirstlane(r.g);
-        if (r.g < 0) return PrefixGroup{-1, 0, 0, 0, 0, 0};
+        if (r.g < 0) return PrefixGroup{-1, 0, 0, 0, 0, 0, 0};
         r.b0 = first_of(r.g);
         r.b1 = first_of(r.g + 1);
         r.t0 = a.cu[r.b0];
         r.t1 = a.cu[r.b1];
         least = r.g < a.n_groups ? a.prefix[r.g] : 0;
         int p0 = 0x7fffffff;
+        r.front = 0x7fffffff;
         if (least > 0) {
             for (int b = r.b0 + lane; b < r.b1; b += WAVE) {
-                const int n = a.cu[b + 1] - a.cu[b], p = a.len[b] - n;
-                if (n > 0 && p < p0) p0 = p;
+                const int n = a.cu[b + 1] - a.cu[b];
+                if (n <= 0) continue;
+                const int p = a.len[b] - n;
+                p0 = p < p0 ? p : p0;
+                r.front = b < r.front ? b : r.front;
             }
             p0 = lanes_min(p0);
+            r.front = lanes_min(r.front);
         }
+        if (r.front == 0x7fffffff) r.front = r.b0;
         least = p0 < least ? p0 : least;
     }
     auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    return PrefixGroup{scalar(r.g), scalar(r.b0), scalar(r.b1), scalar(r.t0), scalar(r.t1), scalar(r.g < a.n_groups && least > 0 ? least : 0)};
+    return PrefixGroup{scalar(r.g), scalar(r.b0), scalar(r.b1), scalar(r.t0), scalar(r.t1), scalar(r.g < a.n_groups && least > 0 ? least : 0), scalar(r.front)};
 }
 
 __device__ __forceinline__ int parts_of(KeyRange k, const PrefixKernelArgs::Cut& cut)
@@ -141,14 +151,14 @@ template <typename T, int DH> __device__ __forceinline__ void prefix_row(const P
 {
     const int64_t head = (int64_t)DH << a.table.shift;
     chunk_row<T, DH>((const T*)a.q + (int64_t)t * a.q_stride + h * DH, (const T*)a.kv_blocks + h / a.G * head, 2 * a.Hkv * head, a.Hkv * head, a.table.shift,
-                     [&](int j) { return a.table.block(j < gr.prefix ? gr.b0 : b, j); }, keys_of(p, 0, table_limit(a.table)), a.scale * LOG2E, lane,
+                     [&](int j) { return a.table.block(j < gr.prefix ? gr.front : b, j); }, keys_of(p, 0, table_limit(a.table)), a.scale * LOG2E, lane,
                      (T*)a.out + (int64_t)t * a.out_stride + h * DH);
 }
 
 // Query rows r0 .. r1 - 1 of a run of packed tokens from t0 on (row r: token t0 + r / G, head kvh * G + r % G) against keys k of table row b; row
 // r sees keys lo .. hi(r / G) - 1 of them.  Every wave takes steps of 16 keys of its own through a ring of stages in LDS, as chunk_stream_kernel does,
 // with QB blocks of 16 rows: S^T = K . Q^T, O^T += V^T . P^T.  The result goes to part `part`.
-// WHOLE: behind the keys 0 .. lo - 1 of table row b0, which all rows see, and to the results themselves; again: computes a row once more.
+// WHOLE: behind the keys 0 .. lo - 1 of table row b0 (the front one), which all rows see, and to the results themselves; again: computes a row once more.
 template <typename T, int DH, int QB, int WAVES, bool NT, bool WHOLE, typename F, typename R>
 __device__ __forceinline__ void stream_rows(const PrefixKernelArgs& a, unsigned char* smem, int b0, int b, int kvh, int t0, int r0, int r1,
                                             KeyRange k, int lo, F hi, int part, R again)
@@ -409,7 +419,7 @@ template <int SHIFT> __device__ __forceinline__ PrefixTile find_prefix(const Pre
         no_part(a, kvh, gr.t0, r0, r.r1, r.part);
         return r;
     }
-    r.tile = ChunkTile{gr.b0, kvh, gr.t0, r.r1, 0, r0};
+    r.tile = ChunkTile{gr.front, kvh, gr.t0, r.r1, 0, r0};
     r.k = part_of(all, a.shared, r.part, parts);
     return r;
 }
@@ -459,7 +469,7 @@ template <typename T, int DH, int WAVES> __global__ __launch_bounds__(WAVES * 64
     auto again = [&](int row) { prefix_row<T, DH>(a, gr, b, p0 + row / G, t0 + row / G, kvh * G + row % G, lane); };
     for (int r0 = tile * 16; r0 < n * G; r0 += a.own_tiles * 16) {
         const int r1 = r0 + 16 < n * G ? r0 + 16 : n * G;
-        stream_rows<T, DH, 1, WAVES, false, true>(a, px_smem, gr.g < 0 || !lo ? b : gr.b0, b, kvh, t0, r0, r1, KeyRange{lo & -PX_STEP, hi(a.by_G.quotient(r1 - 1))}, lo, hi, 0, again);
+        stream_rows<T, DH, 1, WAVES, false, true>(a, px_smem, gr.g < 0 || !lo ? b : gr.front, b, kvh, t0, r0, r1, KeyRange{lo & -PX_STEP, hi(a.by_G.quotient(r1 - 1))}, lo, hi, 0, again);
     }
 }
 // More rows, in tiles of 128, in front of own positions.  Bound by MFMAs and softmax, as chunk_tile_kernel is: 64 sequences and 96 tokens of 32 heads over 8 x 128 on

@@ -1,5 +1,5 @@
 """Attention over prefixes that the sequences of a group share, against 64 bits.  What lies behind a sequence's end, and the blocks that only a
-group's first sequence is read through, are NaN or no blocks in all other tables."""
+group's first sequence with new tokens is read through, are NaN or no blocks in all other tables."""
 import numpy as np
 import pytest
 import torch
@@ -36,8 +36,10 @@ class Groups(Batch):
     def fill(self):
         super().fill()
         for g, (p, _) in enumerate(self.groups):
-            for b in range(self.cu_groups[g] + 1, self.cu_groups[g + 1]):
-                for i in range(p // self.block):                      # never looked at: no block, or one of NaN
+            members = range(self.cu_groups[g], self.cu_groups[g + 1])
+            front = next((b for b in members if self.seqs[b][0]), -1)
+            for b in members:
+                for i in range(p // self.block if b != front else 0):     # never looked at: no block, or one of NaN
                     self.pool[self.table[b, i]] = float("nan")
                     self.table[b, i] = self.n_blocks - 1 if i % 2 else -5
         return self
@@ -46,6 +48,9 @@ class Groups(Batch):
         super().device()
         self.d_groups = torch.as_tensor(self.cu_groups).to(DEV)
         self.d_prefix = torch.tensor(self.prefix, dtype=torch.int32, device=DEV)
+        for b, (n, _) in enumerate(self.seqs):                            # of a sequence without new tokens nothing is looked at
+            if n == 0:
+                self.d_len[b] = -9 if b % 2 else (1 << 31) - 1
         return self
 
     def sizes(self):
@@ -75,6 +80,7 @@ CASES = {
     "ragged": [(500, ONES(5)), (16, ONES(1)), (0, ONES(3)), (33, ONES(17, 40)), (1, ONES(2)), (1000, ONES(2))],
     "drafted": [(200, [(4, 9), (1, 1), (3, 3), (7, 50)]), (31, [(2, 2), (5, 5)])],
     "empty": [(100, [(0, 3), (1, 5), (0, 0), (2, 2)]), (50, []), (40, [(0, 1)]), (60, [(1, 1)])],
+    "ended": [(90, [(0, 3), (0, 0)] + ONES(4)), (200, [(0, 9)] * 40 + ONES(35))],
     "chunks": [(150, [(40, 60), (1, 10), (33, 33)]), (15, [(100, 101)])],
     "long": [(5000, ONES(3, 600)), (2500, ONES(6, 2000))],
 }
