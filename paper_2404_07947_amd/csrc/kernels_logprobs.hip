@@ -1,5 +1,7 @@
 // Log probabilities of given tokens, entropy and the largest probabilities, of rows of logits.  Rows of 50272, a call: 1 float 7.0 us, of which a CU needs 1.3 to take
-// 200 KB in and 2.6 for their exponentials, 256 float 12.5 (4.1 TB/s), 2048 bf16 43 (4.8 TB/s; vector instructions, exponentials a half of them).
+// 200 KB in and 2.6 for their exponentials, 256 float 12.5 (4.1 TB/s), 2048 bf16 40.5 (5.1 TB/s; vector instructions four fifths
+// of the time, of which 13 a logit, 8 in the sums).  One pass over the registers for the maximum and the sums, about a number that follows the lane's largest logit,
+// has a tenth fewer of them and is slower (43), since it waits chunk by chunk.
 //
 // With the largest logit M and c = scale * log2 e: z = (x - M) * c, S = sum of 2^z, Y = sum of 2^z z; then log p = (z - log2 S) ln 2 and the
 // entropy is (log2 S - Y / S) ln 2.
@@ -123,7 +125,8 @@ template <typename T, int THREADS, int C> struct LogitPart {
     }
     // Logits first .. end - 1 of the row, the first on 16 bytes: up to V - 1 before the row's first one.  What is not of them is -inf.  All loads go
     // out before anything waits: those of chunks that are not there, or only in part, from the nearest whole one.
-    // Of the C chunks the first `chunks` are in use (SOME), or all; LONG: there is a whole one for sure.  `fill` looks after those of chunks I .. J - 1 that are there in part or not at all.
+    // Of the C chunks the first `chunks` are in use (SOME), or all; LONG: there is a whole one for sure.  `fill`
+    // looks after those of chunks I .. J - 1 that are there in part or not at all: none, where the first `whole` are so in all lanes of the wave.
     template <bool SOME, bool LONG> __device__ __forceinline__ void load(const T* x, unsigned first, unsigned n, int chunks)
     {
         // whole chunks of the row: from its first or second one on, up to `high`, both counted from `first`
@@ -139,9 +142,9 @@ template <typename T, int THREADS, int C> struct LogitPart {
             });
         }
     }
-    template <bool SOME, int I, int J> __device__ __forceinline__ void fill(const T* x, unsigned first, unsigned end, int chunks)
+    template <bool SOME, int I, int J> __device__ __forceinline__ void fill(const T* x, unsigned first, unsigned end, int chunks, int whole)
     {
-        if (first < end && end - first >= SPAN) return;        // all of them whole
+        if (whole >= (SOME ? chunks : C)) return;
         each_chunk<J, SOME, I>(chunks, [&](auto c) {
             const unsigned i = first + place(c * V);
             if (i < end && end - i >= V) return;
@@ -202,6 +205,8 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
     Part p;
     // chunks of which this wave has something
     const int there = (int)(end - first) - __builtin_amdgcn_readfirstlane(wave) * (WAVE * V), chunks = there > 0 ? (there + THREADS * V - 1) / (THREADS * V) : 0;
+    // those that are whole in all of its lanes; none where the first ones begin in front of the row
+    const int whole = first > end || there < WAVE * V ? 0 : (there - WAVE * V) / (THREADS * V) + 1;
     const unsigned token = given_token(a, row);
     if (tid == 0) s_count = 0;
 
@@ -213,9 +218,9 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
         constexpr bool SOME = some;
         constexpr int I = from, J = to;
         if constexpr (SOME == Part::SOME) {
-            p.template fill<SOME, I, J>(x, first, end, chunks);
+            p.template fill<SOME, I, J>(x, first, end, chunks, whole);
         } else if constexpr (J == C) {
-            p.template fill<SOME, C - 2, C>(x, first, end, chunks);
+            p.template fill<SOME, C - 2, C>(x, first, end, chunks, whole);
         }
         bool none = false;
         each_chunk<J, SOME, I>(chunks, [&](auto c) {
@@ -304,17 +309,22 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
     if (a.k) {
         // k logits or more are no smaller than the k-th largest of the threads' best ones, of which the largest of each 64th of them will do where k is small:
         // these take part in a search for its upper 16 bits, a number no larger.
-        f32x4 b4 = *(const f32x4*)(s_best + 4 * lane);
+        f32x4 b4;
+        if (a.k > 1) {
+            b4 = *(const f32x4*)(s_best + 4 * lane);
 #pragma unroll
-        for (int i = 1; i < THREADS / 256; ++i) {
-            const f32x4 more = *(const f32x4*)(s_best + 256 * i + 4 * lane);
+            for (int i = 1; i < THREADS / 256; ++i) {
+                const f32x4 more = *(const f32x4*)(s_best + 256 * i + 4 * lane);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) b4[e] = fmaxf(b4[e], more[e]);
+                for (int e = 0; e < 4; ++e) b4[e] = fmaxf(b4[e], more[e]);
+            }
         }
         unsigned kth = 0;
-        if (a.k <= 32) {
+        if (a.k == 1) {
+            kth = logit_order(lanes_max(s_sums[lane % WAVES].M));            // the largest of all, at hand (2048 bf16 rows of 50272 41.4 -> 40.5 us)
+        } else if (a.k <= 32) {
             const unsigned o = logit_order(fmaxf(fmaxf(b4[0], b4[1]), fmaxf(b4[2], b4[3])));
-            for (unsigned bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
+            for (unsigned bit = 1u << 31; bit >= 1u << 16; bit >>= 1)          // (two bits a step, by three counts: 0.3 us more)
                 if (__popcll(__builtin_amdgcn_ballot_w64(o >= (kth | bit))) >= a.k) kth |= bit;
         } else {
             const unsigned o[4] = {logit_order(b4[0]), logit_order(b4[1]), logit_order(b4[2]), logit_order(b4[3])};
