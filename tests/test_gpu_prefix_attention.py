@@ -310,3 +310,12 @@ def test_random_batches(seed):
     loose = [(1, int(rng.integers(1, 200))) for _ in range(int(rng.integers(0, 3)))]
     b = Groups(groups, H, Hkv, dh, block, ["bf16", "f32"][seed % 2], seed=seed, loose=loose or [(1, 3)], extra_rows=int(rng.integers(0, 3))).fill().device()
     check(b.attend(), *b.want(), (groups, loose))
+
+
+@pytest.mark.parametrize("heads", [(33, 1), (64, 1), (128, 1), (66, 2), (192, 3)])
+def test_many_heads_over_one(heads):
+    """Rows of one token in several tiles, and tiles that hold parts of two tokens."""
+    for dtype, dh in (("bf16", 128), ("bf16", 64), ("f32", 64)):
+        b = Groups([(90, [(1, 1), (0, 5), (3, 20)]), (257, [(1, 1)])], *heads, dh, 16, dtype, seed=heads[0], loose=[(1, 33)]).fill().device()
+        check(b.attend(), *b.want())
+        check(b.attend(max_group=1, max_new=1), *b.want())
