@@ -497,28 +497,31 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void prefix_join
     const int64_t at = (int64_t)t * a.H + h, step = (int64_t)a.tokens * a.H;
     const int packed = a.cu[a.n_seqs];
     const float2 x = lane < parts ? *(const float2*)(a.tile.ml + (at + lane * step) * 2) : float2{-INFINITY, NO_PART};
+    const float* acc = a.tile.acc + at * DH + f;
+    auto part = [&](int k) { return *(const f32x4*)(acc + (k < parts ? k : parts - 1) * step * DH); };
+    const f32x4 early[2] = {part(sub), part(SUBS + sub)};                // need no weights (12 groups 43.1 -> 42.6 us)
+    asm volatile("" ::: "memory");                                       // not after the wait for those
     if (t >= packed) return;
     const float M = wave_max(x.x), w = x.y == NO_PART ? -1.f : fast_exp2(x.x - (M == -INFINITY ? 0.f : M)), L = wave_sum(x.y < 0.f ? 0.f : x.y * w);
     const bool none = __builtin_amdgcn_ballot_w64(x.y == NO_KEYS);
-    const float* acc = a.tile.acc + at * DH + f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     int first = 0;
-    auto take = [&](auto count) {                                        // parts of which the loads are on their way together
-        constexpr int U = count;
-        f32x4 p[U];
-        float wk[U];
+    auto add = [&](const f32x4* p, auto count) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int k = first + u * SUBS + sub, at = k < parts ? k : parts - 1;
-            const float wa = __shfl(w, at, WAVE);
-            wk[u] = k < parts ? wa : -1.f;
-            p[u] = *(const f32x4*)(acc + at * step * DH);
+        for (int u = 0; u < count; ++u) {
+            const int k = first + u * SUBS + sub;
+            const float wk = __shfl(w, k < parts ? k : parts - 1, WAVE);
+            if (k < parts && wk >= 0.f) v += p[u] * wk;
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (wk[u] >= 0.f) v += p[u] * wk[u];
-        first += U * SUBS;
+        first += count * SUBS;
     };
+    auto take = [&](auto count) {                                        // parts of which the loads are on their way together
+        f32x4 p[count];
+#pragma unroll
+        for (int u = 0; u < count; ++u) p[u] = part(first + u * SUBS + sub);
+        add(p, count);
+    };
+    add(early, std::integral_constant<int, 2>{});
     // us of a call, one after the other / 8 of them: 8 sequences of 32 heads over 4 and 3746 shared positions, 64 parts 19.0 / 15.5, 17 of 24 over 3 and 11011 27.5 /
     // 19.0; up to 4 each: more loads than parts (12 groups 42.9 / 43.5).
     while (parts - first > 4 * SUBS) take(std::integral_constant<int, 8>{});
