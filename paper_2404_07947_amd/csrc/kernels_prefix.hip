@@ -475,7 +475,7 @@ template <typename T, int DH, int WAVES> __global__ __launch_bounds__(WAVES * 64
 }
 // More rows, in tiles of 128, in front of own positions.  Bound by MFMAs and softmax, as chunk_tile_kernel is: 64 sequences and 96 tokens of 32 heads over 8 x 128 on
 // a document of 30001 positions 77 to 80 us, 1000 TFLOP/s in the tiles, then 18 us for the own positions' 81 MB (among the tiles, whose places on a CU they
-// take, 95 to 127 us; in front of them 79), and 7 for the join.  12 groups of 1 to 16 sequences 41 us, 4.8 TB/s.
+// take, 95 to 127 us; in front of them 79), and 6.6 for the join.  12 groups of 1 to 16 sequences 41 us, 4.8 TB/s.
 template <typename T, int DH> __global__ __launch_bounds__(CT_WAVES * 64, 2) void prefix_tile_kernel(PrefixKernelArgs a)
 {
     extern __shared__ __align__(16) unsigned char px_smem[];
