@@ -597,7 +597,8 @@ static PrefixPlan prefix_plan(const PrefixAttnArgs& a)
     if (p.waves == 2) target = ceil_div(keys, 768);
     target = target < 128 ? 128 : target;
     // Parts are whole: where what they are rounded up by would begin a second round, longer ones, up to twice, if those fit one (us: 32 sequences of 32 heads over
-    // 8 x 128 and 6000 shared positions 29.4 -> 22.4, 16 of 32 over 4 x 64 and 8000 21.4 -> 17.8, 24 of 16 heads and 4000 23.1 -> 21.4).  Where own positions alone are more than a
+    // 8 x 128 and 6000 shared positions 29.4 -> 22.4, 16 of 32 over 4 x 64 and 8000 21.4 -> 17.8, 24 of 16 heads and 4000 23.1 -> 21.4; of 47 shapes 25 by 3 to
+    // 20 % faster, two slower, by 2 and 5 %).  Up to three times as long: between 20 % faster and 65 % slower (47 of 24 heads over 8 x 64 and 15556 27.6, 45.7).  Where own positions alone are more than a
     // round, fewer or more parts were not better (the document 83; 79 to 98 by a target of 448 to 1024 workgroups, the ragged groups 45; 45 to 50).
     auto count = [&](int64_t t) { return tiles * ceil_div(a.max_prefix, t) + own * own_rows * ceil_div(a.max_own, t); };
     if (p.waves == 4)
