@@ -222,21 +222,12 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
         } else if constexpr (J == C) {
             p.template fill<SOME, C - 2, C>(x, first, end, chunks, whole);
         }
-        bool none = false;
         each_chunk<J, SOME, I>(chunks, [&](auto c) {
             const int i = c * V;
             tops[c] = max3(p.at(i), p.at(i + 1), p.at(i + 2));
             if constexpr (V == 8) tops[c] = max3(max3(tops[c], p.at(i + 3), p.at(i + 4)), p.at(i + 5), p.at(i + 6));
             tops[c] = max3(tops[c], tops[c], p.at(i + V - 1));
-            none |= tops[c] != tops[c];
         });
-        if (none) {                                            // all of a chunk NaN, or signalling ones, which that instruction hands on
-            each_chunk<J, SOME, I>(chunks, [&](auto c) {
-                tops[c] = -INFINITY;
-#pragma unroll
-                for (int i = c * V; i < (c + 1) * V; ++i) tops[c] = p.at(i) > tops[c] ? p.at(i) : tops[c];
-            });
-        }
         float most = -INFINITY;
 #pragma unroll
         for (int c = I; c < J; ++c) most = fmaxf(most, tops[c]);
@@ -263,6 +254,16 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
             each_chunk<J, SOME, I>(chunks, [&](auto c) {
 #pragma unroll
                 for (int i = c * V; i < (c + 1) * V; ++i) add((p.at(i) - (most == -INFINITY ? 0.f : most)) * a.c);
+            });
+        }
+        if (S != S) {
+            // A NaN (or plus infinity).  Of a signalling NaN and a number the instruction makes a quiet NaN, and of that and the next number the latter: the first is
+            // lost.  So by comparisons, for the alternatives' sake: the sums are NaN, about whatever maximum.
+            each_chunk<J, SOME, I>(chunks, [&](auto c) {
+                tops[c] = -INFINITY;
+#pragma unroll
+                for (int i = c * V; i < (c + 1) * V; ++i) tops[c] = p.at(i) > tops[c] ? p.at(i) : tops[c];
+                best = fmaxf(best, tops[c]);
             });
         }
         return Sums{most, S, Y};

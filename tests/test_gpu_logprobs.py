@@ -279,3 +279,26 @@ def test_far_apart_at_a_small_scale(dtype, n):
     x = x.to(TYPES[dtype][1])
     tokens = torch.tensor([[0, n // 2, n - 1]] * 3, dtype=torch.int32, device=DEV)
     check(x, 2e-38, tokens, 8, call(x.to(DEV), n, 2e-38, tokens, 8))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [300, 3000, 9000, 40000, 600000])
+def test_signalling_nan_beside_the_largest(dtype, n):
+    """A signalling NaN at every place of a 16-byte chunk, the largest logit at every other one; beside plus infinity; all of a chunk but one."""
+    t = TYPES[dtype][1]
+    bits, nan, minus_nan = (torch.int32, 0x7f800001, 0xff800001 - (1 << 32)) if dtype == "f32" else (torch.int16, 0x7f81, 0xff81 - (1 << 16))
+    chunk = 16 // t.itemsize
+    places = [(i, j) for i in range(chunk) for j in range(chunk) if i != j]
+    x = torch.randn((len(places) + 2, n), generator=torch.Generator().manual_seed(n)).to(t)
+    at = n // 2 // chunk * chunk
+    raw = x.view(bits)
+    for r, (i, j) in enumerate(places):
+        x[r, at + j] = 100.0
+        raw[r, at + i] = nan
+    x[-2, at], x[-2, at + 1], x[-1, at + chunk - 1] = math.inf, 50.0, 60.0
+    raw[-2, at + 3], raw[-1, at:at + chunk - 1] = nan, minus_nan
+    tokens = torch.full((len(x), 1), at, dtype=torch.int32, device=DEV)
+    for k in (1, 5, 40):
+        lp, en, ids, top = call(x.to(DEV), n, 1.0, tokens, k)
+        assert torch.equal(ids.cpu(), best(x, k))
+        assert bool(lp.isnan().all()) and bool(en.isnan().all()) and bool(top.isnan().all())
