@@ -77,13 +77,19 @@ template <typename T> __device__ __forceinline__ float given_logit(const Logprob
 // The results of a row, by a workgroup: sums, and the k best keys in LDS (0: there are fewer).
 template <typename T, int THREADS> __device__ __forceinline__ void logprob_finish(const LogprobKernelArgs& a, int64_t row, Sums t, const u64* top, float given)
 {
+    // The largest logit's own term is 1, but comes out as 1 - 2^-24 where the rounding of its sums' reference is taken out again: no probability above 1,
+    // no entropy below 0.  (Comparisons: a NaN stays one.)
+    if (t.S > 0.f && t.S < 1.f) t.S = 1.f;
     const float L = log2f(t.S) * LN2;
     // in 64 bits: the logits may lie further apart than the largest float
     auto logprob = [&](float x) { return (float)(((double)x - (double)t.M) * (double)a.scale - (double)L); };
     if ((int)threadIdx.x < a.n_tokens) a.logprobs[row * a.n_tokens + threadIdx.x] = logprob(given);
     for (int i = threadIdx.x + THREADS; i < a.n_tokens; i += THREADS)
         a.logprobs[row * a.n_tokens + i] = logprob(given_logit<T>(a, row, (unsigned)a.tokens[row * a.n_tokens + i]));
-    if (a.entropy && threadIdx.x == 0) a.entropy[row] = L - t.Y / t.S * LN2;
+    if (a.entropy && threadIdx.x == 0) {
+        const float h = L - t.Y / t.S * LN2;
+        a.entropy[row] = h < 0.f ? 0.f : h;
+    }
     if ((int)threadIdx.x < a.k) {
         const u64 key = top[threadIdx.x];
         a.top_ids[row * a.k + threadIdx.x] = key ? (int)~(unsigned)key : -1;

@@ -302,3 +302,21 @@ def test_signalling_nan_beside_the_largest(dtype, n):
         lp, en, ids, top = call(x.to(DEV), n, 1.0, tokens, k)
         assert torch.equal(ids.cpu(), best(x, k))
         assert bool(lp.isnan().all()) and bool(en.isnan().all()) and bool(top.isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 700, 3000, 9000, 40000, 60000, 600000])
+def test_no_probability_above_one_and_no_entropy_below_zero(dtype, n):
+    """Rows with one token left, of many magnitudes; rows so peaked that the others vanish, or nearly."""
+    g = torch.Generator().manual_seed(n)
+    rows = 64 if n < 100000 else 16
+    at = torch.randint(0, n, (rows, 1), generator=g)
+    left = torch.full((rows, n), -math.inf).scatter_(1, at, torch.randn((rows, 1), generator=g) * 10.0 ** torch.linspace(-3, 30, rows)[:, None])
+    peaked = torch.randn((rows, n), generator=g).scatter_(1, at, torch.linspace(5, 120, rows)[:, None])
+    tokens = at.int().to(DEV)
+    for x in (left.to(TYPES[dtype][1]), peaked.to(TYPES[dtype][1])):
+        for scale in (1.0, 0.7, 1.3, 3.0):
+            got = call(x.to(DEV), n, scale, tokens, 1)
+            lp, en, ids, top = got
+            assert bool((lp <= 0).all()) and bool((top <= 0).all()) and bool((en >= 0).all())
+            check(x, scale, tokens, 1, got)
