@@ -59,7 +59,9 @@ template <int DH, int N, typename F> __device__ __forceinline__ void head_norm(F
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = at(e) * s;
         if (!rms) center();
-        r = rsqrtf(sum([](float a) { return a * a; }) * (1.f / DH) + eps * s * s);
+        // Equal elements have no deviations, and are 0 by an eps that the scale takes below a float (a deviation that is one is 2^-25 of the largest element or more)
+        const float scaled = sum([](float a) { return a * a; }) * (1.f / DH) + eps * s * s;
+        r = eps > 0.f && scaled < 0x1p-100f ? 0.f : rsqrtf(scaled);
     }
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] *= r;

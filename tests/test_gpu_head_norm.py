@@ -279,3 +279,17 @@ def test_tensors_that_would_be_misread_are_refused():
                    dict(gain=gain.cpu()), dict(x=x[:, 1:])):
         with pytest.raises(AssertionError):
             exe.exe_op_head_norm_rotary(**{**good, **change})
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh,start", [(64, 0), (128, 0), (64, 1), (128, 1)])
+def test_equal_elements_have_no_deviations(dtype, dh, start):
+    """0 / sqrt(0 + eps), wherever the elements lie; 0 / 0 without an eps."""
+    sizes = [0.0, 1e-40, 1e-30, 1 / 3, 1.0, -1e4 / 3, 1e10 / 3, 2.0 ** 30, -1e20, 2.0 ** 100 / 3, 1e38]
+    x = torch.tensor(sizes)[None, :, None].expand(1, -1, dh).to(TYPES[dtype][1])
+    buf = torch.zeros(x.numel() + start, dtype=x.dtype, device=DEV)
+    buf[start:] = x.flatten().to(DEV)
+    dx = buf[start:].view(1, -1)
+    for eps in (1.0, 1e-6, 1e-30, 1e-34, 1e-38, 1e-44):
+        assert bool((call(dx, len(sizes), dh, 0, None, 0, eps, 0, 0, None, None, 1.0) == 0).all())
+    assert bool(call(dx, len(sizes), dh, 0, None, 0, 0.0, 0, 0, None, None, 1.0).isnan().all())
