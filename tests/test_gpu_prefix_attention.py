@@ -319,3 +319,24 @@ def test_many_heads_over_one(heads):
         b = Groups([(90, [(1, 1), (0, 5), (3, 20)]), (257, [(1, 1)])], *heads, dh, 16, dtype, seed=heads[0], loose=[(1, 33)]).fill().device()
         check(b.attend(), *b.want())
         check(b.attend(max_group=1, max_new=1), *b.want())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh,n", [(64, 3), (128, 3), (64, 40), (128, 40)])
+def test_values_near_a_floats_end(dtype, dh, n):
+    """Values whose sums pass the largest float.  All the same: their mean, to a half step of float for each of a row's keys, 16 for each 64 of them (sums of
+    weights, their inverse, the factor of what was there before) and 4 more; in bf16 a half step for the weights, the result and the tile's sum of weights too."""
+    b = Groups([(50, ONES(n, 4)), (33, ONES(2, 9))], 4, 2, dh, 16, dtype)
+    for v in b.v:
+        v.fill_(3.0e38)
+    b.fill().device()
+    got = b.attend().cpu().double()
+    keys = max(L for _, L in b.seqs)
+    bound = (keys + 16 * -(-keys // 64) + 4) * 2.0 ** -24 + (3 * 2.0 ** -8 if dtype == "bf16" else 0.0)
+    off = (got / float(torch.tensor(3.0e38).to(b.t)) - 1).abs().max()
+    assert bool(off <= bound), (float(off), bound)
+    b = Groups([(50, ONES(n, 4)), (33, ONES(2, 9))], 4, 2, dh, 16, dtype)
+    for v in b.v:
+        v.mul_(6e37)                                                      # of both signs, up to 5 times as large
+    b.fill().device()
+    check(b.attend(), *b.want())
