@@ -45,8 +45,8 @@ struct PrefixKernelArgs {
     struct Cut { int parts, keys; } shared, own;
     struct { int64_t rows; float *acc, *ml; } tile;
     static constexpr int window = 0;
-    int slots, own_tiles;             // of prefix tiles; tiles of a sequence's rows side by side
-    unsigned shared_units, own_units; // workgroups of each kind
+    int own_tiles;                    // of a sequence's rows, side by side
+    unsigned shared_units;            // workgroups of prefix tiles
     Divisor by_G, by_Hkv, by_parts, by_tiles, by_units, by_quarter;   // G, Hkv; own.parts, own_tiles; workgroups of a slot of tiles; of a token in the join
 };
 
@@ -662,8 +662,8 @@ template <typename T, int DH> static hipError_t launch_prefix(const PrefixAttnAr
     k.out = a.out; k.out_stride = a.out_stride;
     k.shared = p.shared; k.own = p.own;
     k.tile = {rows, a.workspace, a.workspace + (size_t)(p.shared.parts + p.own.parts) * rows * DH};
-    k.slots = (int)p.slots; k.own_tiles = p.own_tiles;
-    k.shared_units = (unsigned)p.shared_units; k.own_units = (unsigned)p.own_units;
+    k.own_tiles = p.own_tiles;
+    k.shared_units = (unsigned)p.shared_units;
     k.by_G = Divisor::of(k.G); k.by_Hkv = Divisor::of(k.Hkv);
     k.by_parts = Divisor::of(std::max(p.own.parts, 1)); k.by_tiles = Divisor::of(p.own_tiles);
     k.by_units = Divisor::of(std::max<int64_t>(8, ceil_div((int64_t)k.Hkv * p.shared.parts, 8) * 8)); k.by_quarter = Divisor::of(ceil_div(a.H, 4));
