@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import paper_2404_07947_amd as exe
+import workload as wl
 from chunk_util import DEV, TYPES, U
 
 pytestmark = pytest.mark.gpu
@@ -320,3 +321,20 @@ def test_no_probability_above_one_and_no_entropy_below_zero(dtype, n):
             lp, en, ids, top = got
             assert bool((lp <= 0).all()) and bool((top <= 0).all()) and bool((en >= 0).all())
             check(x, scale, tokens, 1, got)
+
+
+def test_logits_of_a_models_own_steps():
+    """What exe_encode and exe_decode_step hand out goes straight in: the first alternative is the token that they return."""
+    shape = wl.tiny_shape()
+    m = exe.Model(exe.config_from_shape(shape, kv_pool_bytes=1 << 24, max_seqs=8, max_batch_tokens=128, max_batch_seqs=8), [t.to(DEV) for t in wl.make_weights(shape, seed=1)])
+    lens = np.array([9, 20, 5], dtype=np.int32)
+    logits = torch.empty((3, shape.vocab), device=DEV)
+    tokens = np.random.default_rng(0).integers(0, shape.vocab, lens.sum()).astype(np.int32)
+    nxt = m.encode([0, 1, 2], lens, tokens, reserve_lengths=lens + 16, out_device=logits)
+    for step in range(1, 5):
+        given = torch.as_tensor(nxt[:, None].copy()).to(DEV)
+        got = call(logits, shape.vocab, 0.8, given, 5)
+        check(logits.cpu(), 0.8, given, 5, got)
+        assert np.array_equal(got[2][:, 0].cpu().numpy(), nxt) and torch.equal(got[0][:, 0], got[3][:, 0])
+        nxt = m.decode_step([0, 1, 2], nxt, lens + step, out_device=logits)
+    m.close()

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+import chunk_util
 import paper_2404_07947_amd as exe
 from chunk_util import DEV, Batch, check
 
@@ -340,3 +341,16 @@ def test_values_near_a_floats_end(dtype, dh, n):
         v.mul_(6e37)                                                      # of both signs, up to 5 times as large
     b.fill().device()
     check(b.attend(), *b.want())
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("heads,n", [((4, 4), 9), ((4, 4), 16), ((8, 2), 5), ((6, 2), 10), ((16, 1), 2)])
+def test_probabilities_keep_16_bits_for_up_to_32_rows(dh, heads, n, monkeypatch):
+    """bf16: the bound of `want` with what two numbers of 8 bits leave of a probability, 2^-16, in place of a half step, and that of the result.  Few keys and a small
+    scale, so that the other roundings do not cover it."""
+    b = Groups([(21, ONES(n))], *heads, dh, 16, "bf16").fill().device()
+    monkeypatch.setitem(chunk_util.HALF, "bf16", 2.0 ** -16)
+    want, tol = b.want(scale=1e-3)
+    got = b.attend(scale=1e-3).cpu().double()
+    over = (got - want).abs() - tol - 2.0 ** -8 * (want.abs() + tol) * (1 + 1e-6)
+    assert bool((over <= 0).all()), float(over.max())
