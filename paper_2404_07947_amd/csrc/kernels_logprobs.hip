@@ -16,7 +16,7 @@
 namespace exe {
 
 typedef unsigned long long u64;
-constexpr int LP_JOIN_THREADS = 256, LP_CAP = 256, LP_JOIN = 64;
+constexpr int LP_JOIN_THREADS = 256, LP_CAP = 512, LP_JOIN = 64;      // LP_CAP: all logits of a part in which fewer than 64 threads have some
 constexpr float LN2 = 0.69314718055994530942f;
 
 struct LogprobKernelArgs {
@@ -181,15 +181,18 @@ __device__ __forceinline__ float max3(float a, float b, float c)
 }
 
 // The k best of `count` keys, at most LP_CAP, sorted by counting, for each, those above it; 0 where there are fewer.
-__device__ __forceinline__ void sort_keys(const u64* keys, int count, u64* top, int k)
+template <int THREADS> __device__ __forceinline__ void sort_keys(const u64* keys, int count, u64* top, int k)
 {
     const int tid = threadIdx.x;
-    if (tid < count) {
-        const u64 mine = keys[tid];
+    auto sort = [&](int i) {
+        if (i >= count) return;
+        const u64 mine = keys[i];
         int above = 0;
         for (int j = 0; j < count; ++j) above += keys[j] > mine;
         if (above < k) top[above] = mine;
-    }
+    };
+    sort(tid);
+    if (LP_CAP > THREADS && count > THREADS) sort(tid + THREADS);
     if (tid >= count && tid < k) top[tid] = 0;
 }
 
@@ -314,8 +317,9 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
         }
     };
     if (a.k) {
-        // k logits or more are no smaller than the k-th largest of the threads' best ones, of which the largest of each 64th of them will do where k is small:
-        // these take part in a search for its upper 16 bits, a number no larger.
+        // k logits or more are no smaller than the k-th largest of the threads' best ones, of which the largest of each 64th of them will do where k is small and so many
+        // 64ths have one: these take part in a search for its upper 16 bits, a number no larger.  (Short parts of 256 threads may have fewer, which leaves all their
+        // logits: 64 rows of 300 floats, k 20, 62 us with them sorted in memory, 5.2 by the threads' best.)
         f32x4 b4;
         if (a.k > 1) {
             b4 = *(const f32x4*)(s_best + 4 * lane);
@@ -329,8 +333,8 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
         unsigned kth = 0;
         if (a.k == 1) {
             kth = logit_order(lanes_max(s_sums[lane % WAVES].M));            // the largest of all, at hand (2048 bf16 rows of 50272 41.4 -> 40.5 us)
-        } else if (a.k <= 32) {
-            const unsigned o = logit_order(fmaxf(fmaxf(b4[0], b4[1]), fmaxf(b4[2], b4[3])));
+        } else if (const float of4 = fmaxf(fmaxf(b4[0], b4[1]), fmaxf(b4[2], b4[3])); a.k <= 32 && (THREADS > 256 || __popcll(__builtin_amdgcn_ballot_w64(of4 > -INFINITY)) >= a.k)) {
+            const unsigned o = logit_order(of4);
             for (unsigned bit = 1u << 31; bit >= 1u << 16; bit >>= 1)          // (two bits a step, by three counts: 0.3 us more)
                 if (__popcll(__builtin_amdgcn_ballot_w64(o >= (kth | bit))) >= a.k) kth |= bit;
         } else {
@@ -406,9 +410,9 @@ template <typename T, int THREADS, int C> __global__ __launch_bounds__(THREADS, 
         }
         join_waves();
         if (a.parts > 1) {
-            sort_keys(s_keys, count, a.lists + (int64_t)blockIdx.x * a.k, a.k);
+            sort_keys<THREADS>(s_keys, count, a.lists + (int64_t)blockIdx.x * a.k, a.k);
         } else {
-            sort_keys(s_keys, count, s_top, a.k);
+            sort_keys<THREADS>(s_keys, count, s_top, a.k);
             __syncthreads();
         }
     }
@@ -464,7 +468,7 @@ template <typename T> __global__ __launch_bounds__(LP_JOIN_THREADS) void logprob
         __syncthreads();
         u64* top = a.parts > 1 ? a.lists + (int64_t)blockIdx.x * a.k : s_top;
         if (s_count <= LP_CAP) {
-            sort_keys(s_keys, s_count, top, a.k);
+            sort_keys<LP_JOIN_THREADS>(s_keys, s_count, top, a.k);
         } else if (wave == 0) {
             int next = 0;
             for (int i = 0; i < a.k; ++i) {

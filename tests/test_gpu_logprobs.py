@@ -338,3 +338,18 @@ def test_logits_of_a_models_own_steps():
         assert np.array_equal(got[2][:, 0].cpu().numpy(), nxt) and torch.equal(got[0][:, 0], got[3][:, 0])
         nxt = m.decode_step([0, 1, 2], nxt, lens + step, out_device=logits)
     m.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [257, 300, 495, 511, 512, 513, 1023, 1100, 2100])
+def test_rows_that_few_threads_hold(dtype, n):
+    """Parts in which fewer than k threads, or 64ths of them, have a logit; as many candidates as are sorted at once, and one more."""
+    g = torch.Generator().manual_seed(n)
+    x = (torch.randn((5, n), generator=g) * 2.5).to(TYPES[dtype][1])
+    x[1], x[2] = 0.5, torch.arange(n).to(x.dtype) / n
+    x[3, torch.rand(n, generator=g) < 0.5] = -math.inf
+    x[4, 30:] = -math.inf
+    tokens = torch.full((5, 1), 7, dtype=torch.int32, device=DEV)
+    x[3, 7] = 1.0
+    for k in (2, 17, 20, 32, 33, 40, 64):
+        check(x, 1.0, tokens, k, call(x.to(DEV), n, 1.0, tokens, k))
