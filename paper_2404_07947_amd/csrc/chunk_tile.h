@@ -187,12 +187,30 @@ __device__ __forceinline__ void tile_rows(const Args& a, unsigned char* ct_smem,
             const unsigned char* sV = tV + v_row * RB + (v_q & 1) * 8;
 #pragma unroll
             for (int ks = 0; ks < KB / 2; ++ks) {
-                // one rounding to bf16 per probability, half a step of the result's own type
-                bf16x8 pf[QB];
+                // One rounding to bf16 per probability, half a step of the result's own type.  WHOLE: two numbers of it, what is cut off and what that leaves, 15 bits
+                // and more, as the rows of smaller groups and own positions have them (prefix_stream_kernel): how many sequences share a prefix does not
+                // decide how exact they are.  Half as many products again, for a document of 30001 positions 95 us instead of 82; off by 1.66e-3
+                // of the result instead of 2.3e-3, of which its own rounding to bf16 is 1.66e-3.
+                bf16x8 pf[QB], low[QB];
 #pragma unroll
-                for (int qb = 0; qb < QB; ++qb)
+                for (int qb = 0; qb < QB; ++qb) {
+                    auto p = [&](int e) { return s[qb][2 * ks + (e >> 2)][e & 3]; };
+                    if constexpr (WHOLE) {
+                        u32x4 high;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) pf[qb][e] = (bf16_t)s[qb][2 * ks + (e >> 2)][e & 3];
+                        for (int e = 0; e < 8; e += 2) {
+                            const unsigned x = __float_as_uint(p(e)), y = __float_as_uint(p(e + 1));
+                            high[e / 2] = __builtin_amdgcn_perm(y, x, 0x07060302);               // the upper halves
+                            low[qb][e] = (bf16_t)(p(e) - __uint_as_float(x & 0xffff0000u));
+                            low[qb][e + 1] = (bf16_t)(p(e + 1) - __uint_as_float(y & 0xffff0000u));
+                        }
+                        pf[qb] = __builtin_bit_cast(bf16x8, high);
+                        sum[qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, low[qb], sum[qb], 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) pf[qb][e] = (bf16_t)p(e);
+                    }
+                }
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) sum[qb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[qb], sum[qb], 0, 0, 0);
 #pragma unroll
@@ -200,6 +218,10 @@ __device__ __forceinline__ void tile_rows(const Args& a, unsigned char* ct_smem,
                     const int at = ((2 * dt + (v_q >> 1)) ^ pf_swz<RB>(v_row)) << 4;
                     uint2 lo = pf_read_tr(sV + ks * 32 * RB + at), hi = pf_read_tr(sV + (ks * 32 + 16) * RB + at);
                     bf16x8 fv = __builtin_bit_cast(bf16x8, uint4{lo.x, lo.y, hi.x, hi.y});
+                    if constexpr (WHOLE) {
+#pragma unroll
+                        for (int qb = 0; qb < QB; ++qb) o[qb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv, low[qb], o[qb][dt], 0, 0, 0);
+                    }
 #pragma unroll
                     for (int qb = 0; qb < QB; ++qb) o[qb][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv, pf[qb], o[qb][dt], 0, 0, 0);
                 }
@@ -241,7 +263,7 @@ __device__ __forceinline__ void tile_rows(const Args& a, unsigned char* ct_smem,
             __builtin_amdgcn_sched_group_barrier(VECTOR, 20 * QB * KB, 0);
 #pragma unroll
             for (int i = 0; i < KB / 2 * DT; ++i) {
-                __builtin_amdgcn_sched_group_barrier(MATRIX, QB, 0);
+                __builtin_amdgcn_sched_group_barrier(MATRIX, WHOLE ? 2 * QB : QB, 0);
                 __builtin_amdgcn_sched_group_barrier(LDS_READ, 2, 0);
             }
             __builtin_amdgcn_s_setprio(0);

@@ -473,9 +473,10 @@ template <typename T, int DH, int WAVES> __global__ __launch_bounds__(WAVES * 64
         stream_rows<T, DH, 1, WAVES, false, true>(a, px_smem, gr.g < 0 || !lo ? b : gr.front, b, kvh, t0, r0, r1, KeyRange{lo & -PX_STEP, hi(a.by_G.quotient(r1 - 1))}, lo, hi, 0, again);
     }
 }
-// More rows, in tiles of 128, in front of own positions.  Bound by MFMAs and softmax, as chunk_tile_kernel is: 64 sequences and 96 tokens of 32 heads over 8 x 128 on
-// a document of 30001 positions 77 to 80 us, 1000 TFLOP/s in the tiles, then 18 us for the own positions' 81 MB (among the tiles, whose places on a CU they
-// take, 95 to 127 us; in front of them 79), and 6.6 for the join.  12 groups of 1 to 16 sequences 41 us, 4.8 TB/s.
+// More rows, in tiles of 128, in front of own positions.  Bound by MFMAs and softmax, as chunk_tile_kernel is, with half as many products again for the probabilities'
+// lower bits: 64 sequences and 96 tokens of 32 heads over 8 x 128 on a document of 30001 positions 91 us, of which the own positions' 81 MB, behind the tiles, take 18
+// (among them, whose places on a CU they take, 15 to 45 more; in front of them as long), and 6.4 for the join; 60002 more positions 165 us, 860 TFLOP/s.  12 groups of 1 to 16
+// sequences 45 us, 4.4 TB/s, 5.1 behind the start.
 template <typename T, int DH> __global__ __launch_bounds__(CT_WAVES * 64, 2) void prefix_tile_kernel(PrefixKernelArgs a)
 {
     extern __shared__ __align__(16) unsigned char px_smem[];
@@ -571,8 +572,8 @@ static PrefixPlan prefix_plan(const PrefixAttnArgs& a)
 {
     PrefixPlan p{};
     const int64_t G = a.H / a.Hkv, rows = (int64_t)a.max_group * G;
-    // Tiles of 128 rows beyond 32 (us, streaming in blocks of 64 and of 32 rows, tiles: 12 groups of 1 to 16 sequences, 32 heads over 8 x 128, 400 to 3000
-    // shared positions 41, 48, 43; 96 rows of 32 heads each over 30000 230, 278, 189; 32 rows 121, 110, 107; 80 rows of 8 heads 41, 55, 38).
+    // Tiles of 128 rows beyond 32 (us, streaming in blocks of 32 rows / tiles: 12 groups of 1 to 16 sequences, 32 heads over 8 x 128, 400 to 3000 shared positions
+    // 51 / 48; over 30000 positions 96 sequences of 32 heads 234 / 132, 24 of 32 over 8 62 / 48, 10 of 32 over 8 38.6 / 38.3; 32 rows 35.0 / 35.6 and 105 / 104).
     p.qb = a.n_groups == 0 || rows <= 16 ? 1 : rows <= 32 || a.dtype == DT_F32 ? 2 : 8;
     p.slots = (int64_t)a.tokens * G / (16 * p.qb) + a.n_groups + 1;
     const int64_t most = (int64_t)a.tokens * G / (16 * p.qb) + a.n_groups, each = a.n_groups * ceil_div(rows, 16 * p.qb), tiles = (each < most ? each : most) * a.Hkv;

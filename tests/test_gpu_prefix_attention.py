@@ -354,3 +354,15 @@ def test_probabilities_keep_16_bits_for_up_to_32_rows(dh, heads, n, monkeypatch)
     got = b.attend(scale=1e-3).cpu().double()
     over = (got - want).abs() - tol - 2.0 ** -8 * (want.abs() + tol) * (1 + 1e-6)
     assert bool((over <= 0).all()), float(over.max())
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("heads,n", [((4, 4), 40), ((8, 2), 33), ((16, 1), 9)])
+def test_probabilities_keep_15_bits_for_more_rows(dh, heads, n, monkeypatch):
+    """As above: what is cut off a probability after 8 bits, up to a whole step, is rounded to 8 bits of its own."""
+    b = Groups([(21, ONES(n))], *heads, dh, 16, "bf16").fill().device()
+    monkeypatch.setitem(chunk_util.HALF, "bf16", 2.0 ** -15)
+    want, tol = b.want(scale=1e-3)
+    got = b.attend(scale=1e-3).cpu().double()
+    over = (got - want).abs() - tol - 2.0 ** -8 * (want.abs() + tol) * (1 + 1e-6)
+    assert bool((over <= 0).all()), float(over.max())
