@@ -1,5 +1,5 @@
-// Log probabilities of given tokens, entropy and the largest probabilities, of rows of logits.  Rows of 50272, a call: 1 float 7.0 us, of which a CU needs 1.3 to take
-// 200 KB in and 2.6 for their exponentials, 256 float 12.5 (4.1 TB/s), 2048 bf16 40.5 (5.1 TB/s; vector instructions four fifths
+// Log probabilities of given tokens, entropy and the largest probabilities, of rows of logits.  Rows of 50272, a call: 1 float 7.0 us, of which loads and
+// sums of 200 KB by one CU are 2.8 (by the difference to a row of 12000), 256 float 12.4 (4.1 TB/s), 2048 bf16 41.5 (5.0 TB/s; vector instructions four fifths
 // of the time, of which 13 a logit, 8 in the sums).  One pass over the registers for the maximum and the sums, about a number that follows the lane's largest logit,
 // has a tenth fewer of them and is slower (43), since it waits chunk by chunk.
 //
@@ -508,9 +508,9 @@ static LogprobPlan logprob_plan(const LogprobArgs& a)
     LogprobPlan p{256, 1, parts_of(n, 256 * v), 0};
     const int most = 32 / v;
     while (p.chunks < most && p.parts > 1 && (p.parts > LP_JOIN || (int64_t)p.parts * a.rows > 256)) p.parts = parts_of(n, 256 * v * (p.chunks *= 2));
-    // Rows of several such parts: more threads save the second launch.  us of both launches / with more threads: bf16, 2048 rows of 50272 47.5 + 6.0 / 45.2,
-    // 256 rows 12.8 + 5.3 / 11.2, 700 of 128256 47.6 + 7.4 / 42.2 + 5.2, 1000 of 12000 13.4 + 5.8 / 11.7; float, a row a CU at most: 1 row of 50272 4.0 + 4.2 / 7.7,
-    // 64 rows 8.3 + 4.3 / 11.9, 256 rows 14.2 + 4.7 / 14.6, but 1000 rows 48 + 9 / 63.
+    // Rows of several such parts: more threads save the second launch.  us of a call by such parts / with more threads, k 20: bf16, 2048 rows of 50272 64.2 / 47.6, 256 rows
+    // 16.2 / 10.7, 1 row 9.6 / 8.2, 700 of 128256 (two parts) 53.1 / 43.0, 1000 of 12000 17.4 / 11.5; float, a row a CU at most: 1 row of 50272 9.5 / 7.9, 64 rows 12.5 / 9.4,
+    // 256 rows 18.7 / 12.9, but 300 rows 20.4 / 20.1, 512 27.1 / 24.0, 1000 43.5 / 43.9, 2000 78.5 / 81.3, 256 of 64000 (two parts) 20.6 / 22.5.
     if (n > 256 * 32) {
         const int chunks = a.dtype == DT_F32 ? 13 : 8, threads = a.dtype == DT_BF16 && n <= 512 * v * chunks ? 512 : 1024;
         const unsigned parts = parts_of(n, threads * v * chunks);
